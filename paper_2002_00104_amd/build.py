@@ -12,16 +12,21 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpwlq.so")
 CALL_SOURCE = os.path.join(CSRC, "pwlq_call.c")
 CALL = os.path.join(HERE, "_pwlq_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = [os.path.join(CSRC, "pwlq_api.hip")]
-HEADERS = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith(".h")] + [
-           os.path.join(os.path.dirname(HERE), "include", "pwlq.h"),
+BLOCK = os.path.join(CSRC, "block")
+SOURCES = [os.path.join(BLOCK, f) for f in ("library.hip", "adapter.hip", "norm.hip", "pack.hip")]
+BLOCK_HEADERS = [os.path.join(BLOCK, f) for f in ("launch.h", "rows.h")] + [
+    os.path.join(os.path.dirname(HERE), "include", f) for f in ("pwlq.h", "pwlq_block.h")]
+# pwlq_api.hip is part of library.hip
+HEADERS = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".h", ".hip"))] + [
+           os.path.join(BLOCK, "calls.h"), *BLOCK_HEADERS,
            os.path.join(os.path.dirname(HERE), "include", "pwlq_bench.h")]
+OBJECTS = os.path.join(HERE, "_build")
 
 # -ffp-contract=off: the canonical code arithmetic must not be fused; fused
 # operations are written explicitly where wanted.  Packed binary32 VALU forms
 # are disabled for the device compile.
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-ffp-contract=off", "-fno-fast-math",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
@@ -51,11 +56,27 @@ def stale(built: str = LIB, sources=None) -> bool:
     return any(os.path.getmtime(p) > t for p in sources or SOURCES + HEADERS)
 
 
+def compile_library(lib: str, flags, force: bool, kind: str = "") -> None:
+    """Compiles the sources beside each other, those whose object is older than what it is made of, and links them."""
+    os.makedirs(OBJECTS, exist_ok=True)
+    running, objects = [], []
+    for src in SOURCES:
+        obj = os.path.join(OBJECTS, os.path.basename(src) + kind + ".o")
+        objects.append(obj)
+        headers = HEADERS if src == SOURCES[0] else BLOCK_HEADERS
+        if force or stale(obj, [src, *headers]):
+            cmd = [hipcc(), *flags, "-c", src, "-o", obj]
+            running.append((cmd, subprocess.Popen(cmd)))
+    failed = [subprocess.CalledProcessError(p.returncode, cmd) for cmd, p in running if p.wait() != 0]
+    if failed:
+        raise failed[0]
+    subprocess.run([hipcc(), *flags, "-shared", *objects, "-o", lib], check=True)
+
+
 def build(force: bool = True, extra=()) -> str:
     if force or stale():
-        cmd = [hipcc(), *HIPCC_FLAGS, *extra, *SOURCES, "-o", LIB]
-        subprocess.run(cmd, check=True)
-    if force or stale(CALL, [CALL_SOURCE]):
+        compile_library(LIB, [*HIPCC_FLAGS, *extra], force or bool(extra))
+    if force or stale(CALL, [CALL_SOURCE, os.path.join(os.path.dirname(HERE), "include", "pwlq_block.h")]):
         subprocess.run(["gcc", "-O2", "-std=c11", "-Wall", "-Wextra", "-fPIC", "-shared",
                         "-I" + sysconfig.get_paths()["include"], CALL_SOURCE, "-o", CALL], check=True)
     return LIB
@@ -63,7 +84,7 @@ def build(force: bool = True, extra=()) -> str:
 
 def build_sanitized() -> str:
     flags = [f for f in HIPCC_FLAGS if f != "-O3"]
-    subprocess.run([hipcc(), *flags, *HOST_SAN_FLAGS, *SOURCES, "-o", LIB_SAN], check=True)
+    compile_library(LIB_SAN, [*flags, *HOST_SAN_FLAGS], True, ".san")
     return LIB_SAN
 
 

@@ -1,0 +1,93 @@
+// k_pack_rows: rows of activations to 8 bits with a step each.  k_unpack_rows: the values they stand for.
+//
+//   a = max|x|,  step = a/127,  code = rne(x * (127/a))
+// The codes are the operand of the integer inner product (its s_x is 1: the step is a factor of the output row) and
+// the activation checkpoint of a backward pass, at half the bytes of bfloat16 or a quarter of binary32's.
+//
+// Both are bound by memory.  A row is read once: it stays in its workgroup's registers between the maximum and
+// the rounding.
+#include "launch.h"
+#include "rows.h"
+
+namespace pwlq_block {
+namespace {
+
+template <typename T, int E, bool VEC>
+__global__ __launch_bounds__(1024) void k_pack_rows(const T *x, int64_t stride, int64_t rows, int cols, int8_t *codes, float *step)
+{
+    __shared__ uint32_t slots[2][16];
+    const int threads = blockDim.x, thread = threadIdx.x;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+        float v[E];
+        load_row<T, E, VEC>(x + row * stride, cols, threads, thread, v);
+        const Step s = step_of(block_max(largest(v), slots[turn], threads));
+        store_codes<E, VEC>(codes + row * cols, cols, threads, thread, v, s.factor);
+        if (thread == 0) step[row] = s.step;
+    }
+}
+
+template <typename T, int E, bool VEC>
+__global__ __launch_bounds__(1024) void k_unpack_rows(const int8_t *codes, const float *step, int64_t rows, int cols, T *out, int64_t stride)
+{
+    const int threads = blockDim.x, thread = threadIdx.x;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        float v[E];
+        load_row<int8_t, E, VEC>(codes + row * cols, cols, threads, thread, v);
+        const float s = step[row];
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] *= s;
+        store_row<T, E, VEC>(out + row * stride, cols, threads, thread, v);
+    }
+}
+
+inline int threads_for(int cols, int E) { return (cols + 64 * E - 1) / (64 * E) * 64; }
+
+// Elements of a thread: 16 up to 16384 columns (a workgroup holds 1024 threads), else what the longest rows need.
+template <typename T, bool VEC>
+void pack_as(const pwlq_rows &x, int64_t rows, int K, int8_t *codes, float *step, hipStream_t stream)
+{
+    const unsigned grid = row_grid(rows);
+#define PWLQ_PACK(E) \
+    k_pack_rows<T, E, VEC><<<grid, threads_for(K, E), 0, stream>>>((const T *)x.data, x.stride, rows, K, codes, step)
+    if (K <= 512) PWLQ_PACK(8);
+    else if (K <= 16384) PWLQ_PACK(16);
+    else PWLQ_PACK(64);
+#undef PWLQ_PACK
+}
+
+template <typename T, bool VEC>
+void unpack_as(const int8_t *codes, const float *step, int64_t rows, int K, const pwlq_rows &out, hipStream_t stream)
+{
+    const unsigned grid = row_grid(rows);
+#define PWLQ_UNPACK(E) \
+    k_unpack_rows<T, E, VEC><<<grid, threads_for(K, E), 0, stream>>>(codes, step, rows, K, (T *)out.data, out.stride)
+    if (K <= 512) PWLQ_UNPACK(8);
+    else if (K <= 16384) PWLQ_UNPACK(16);
+    else PWLQ_UNPACK(64);
+#undef PWLQ_UNPACK
+}
+
+} // namespace
+
+void pack_rows(const pwlq_rows &x, int64_t rows, int K, int8_t *codes, float *step, hipStream_t stream)
+{
+    const bool vec = K % 8 == 0 && vectors(x, rows) && ((uintptr_t)codes & 7) == 0;
+#define PWLQ_AS(T) (vec ? pack_as<T, true>(x, rows, K, codes, step, stream) : pack_as<T, false>(x, rows, K, codes, step, stream))
+    if (x.type == PWLQ_F32) PWLQ_AS(float);
+    else if (x.type == PWLQ_BF16) PWLQ_AS(bf16);
+    else PWLQ_AS(f16);
+#undef PWLQ_AS
+}
+
+void unpack_rows(const int8_t *codes, const float *step, int64_t rows, int K, const pwlq_rows &out, hipStream_t stream)
+{
+    const bool vec = K % 8 == 0 && vectors(out, rows) && ((uintptr_t)codes & 7) == 0;
+#define PWLQ_AS(T) (vec ? unpack_as<T, true>(codes, step, rows, K, out, stream) : unpack_as<T, false>(codes, step, rows, K, out, stream))
+    if (out.type == PWLQ_F32) PWLQ_AS(float);
+    else if (out.type == PWLQ_BF16) PWLQ_AS(bf16);
+    else PWLQ_AS(f16);
+#undef PWLQ_AS
+}
+
+} // namespace pwlq_block

@@ -30,6 +30,9 @@ EXPORTS = (
     "pwlq_select_analytic_list",
     "pwlq_mse_workspace_bytes", "pwlq_mse_list_workspace_bytes", "pwlq_mse", "pwlq_mse_list",
     "pwlq_linear_workspace_bytes", "pwlq_linear_i8",
+    "pwlq_pack_rows", "pwlq_unpack_rows", "pwlq_norm_block", "pwlq_norm_block_backward_workspace_bytes",
+    "pwlq_norm_block_backward", "pwlq_adapter_workspace_bytes", "pwlq_adapter",
+    "pwlq_adapter_backward_workspace_bytes", "pwlq_adapter_backward",
     "pwlq_last_error", "pwlq_last_search_shape", "pwlq_profile_enable",
     "pwlq_profile_last_ms", "pwlq_profile_ms", "pwlq_kernel_name", "pwlq_last_search_kernel",
     "pwlq_last_kernels",
@@ -106,6 +109,12 @@ def _load() -> ctypes.CDLL:
     lib.pwlq_linear_i8.restype = ci
     lib.pwlq_linear_i8.argtypes = [vp, i64, i64, ctypes.c_float, ctypes.c_float, vp, vp, i64, ci,
                                    vp, vp, vp, vp, vp, sz, vp]
+    lib.pwlq_norm_block_backward_workspace_bytes.restype = sz
+    lib.pwlq_norm_block_backward_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.pwlq_adapter_workspace_bytes.restype = sz
+    lib.pwlq_adapter_workspace_bytes.argtypes = [i64, i64, ci]
+    lib.pwlq_adapter_backward_workspace_bytes.restype = sz
+    lib.pwlq_adapter_backward_workspace_bytes.argtypes = [i64, i64, i64, ci, ci]
     lib.pwlq_last_error.restype = ctypes.c_char_p
     lib.pwlq_last_error.argtypes = []
     lib.pwlq_last_search_shape.restype = None
