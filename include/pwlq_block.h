@@ -14,6 +14,7 @@
  *     the columns of a row next to each other, so a block of columns of a wider
  *     matrix can be passed as it stands.  Outputs must not overlap inputs or
  *     each other, where a call does not say otherwise.
+ *   - A workspace-size query that answers 0 means that the call takes NULL.
  *   - Sums, norms and gradients of parameters are held in binary32; a value is
  *     rounded to a narrower type once, where it is stored.
  *   - 8-bit rows: value = code * step[row], symmetric, codes -127..127.

@@ -1,4 +1,4 @@
-"""Builds libpwlq.so (HIP, gfx950) in-tree with hipcc, and the module that calls it from Python with gcc."""
+"""Builds libpwlq.so (HIP, gfx950) in-tree with hipcc, and the modules that call it from Python with gcc and g++."""
 from __future__ import annotations
 
 import os
@@ -13,6 +13,8 @@ LIB = os.path.join(HERE, "libpwlq.so")
 CALL_SOURCE = os.path.join(CSRC, "pwlq_call.c")
 CALL = os.path.join(HERE, "_pwlq_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 BLOCK = os.path.join(CSRC, "block")
+BINDING_SOURCE = os.path.join(BLOCK, "binding.cpp")
+BINDING = os.path.join(HERE, "_pwlq_block" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = [os.path.join(BLOCK, f) for f in ("library.hip", "adapter.hip", "norm.hip", "pack.hip")]
 BLOCK_HEADERS = [os.path.join(BLOCK, f) for f in ("launch.h", "rows.h")] + [
     os.path.join(os.path.dirname(HERE), "include", f) for f in ("pwlq.h", "pwlq_block.h")]
@@ -73,12 +75,25 @@ def compile_library(lib: str, flags, force: bool, kind: str = "") -> None:
     subprocess.run([hipcc(), *flags, "-shared", *objects, "-o", lib], check=True)
 
 
+def build_binding() -> None:
+    """The module that calls pwlq_block.h with tensors: torch's headers and libraries, and libpwlq.so beside it."""
+    import torch
+    from torch.utils import cpp_extension
+    subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-fvisibility=hidden",
+                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                    "-I" + sysconfig.get_paths()["include"], *("-isystem" + p for p in cpp_extension.include_paths()),
+                    BINDING_SOURCE, "-o", BINDING, "-L" + HERE, "-lpwlq", "-Wl,-rpath,$ORIGIN",
+                    *("-L" + p for p in cpp_extension.library_paths()), "-lc10", "-ltorch_cpu", "-ltorch_python"], check=True)
+
+
 def build(force: bool = True, extra=()) -> str:
     if force or stale():
         compile_library(LIB, [*HIPCC_FLAGS, *extra], force or bool(extra))
-    if force or stale(CALL, [CALL_SOURCE, os.path.join(os.path.dirname(HERE), "include", "pwlq_block.h")]):
+    if force or stale(CALL, [CALL_SOURCE]):
         subprocess.run(["gcc", "-O2", "-std=c11", "-Wall", "-Wextra", "-fPIC", "-shared",
                         "-I" + sysconfig.get_paths()["include"], CALL_SOURCE, "-o", CALL], check=True)
+    if force or stale(BINDING, [BINDING_SOURCE, *BLOCK_HEADERS]):
+        build_binding()
     return LIB
 
 

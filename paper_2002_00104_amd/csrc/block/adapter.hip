@@ -12,6 +12,8 @@
 #include "launch.h"
 #include "rows.h"
 
+#pragma clang fp contract(fast)
+
 namespace pwlq_block {
 namespace {
 
@@ -320,6 +322,76 @@ __global__ __launch_bounds__(256) void k_adapter_second_token(SecondArgs a)
     else store_columns<TW>(a.out, row * a.out_stride, col, a.C, y, VEC);
 }
 
+// Both products of one row in one launch, for 256 columns: the row's H is computed by each of its workgroups anew, which costs
+// reading down again from L2 but no second launch and no wait for it.  Wavefronts share the ranks of the first product, half
+// wavefronts (eight columns a lane) those of the second.
+struct TokenArgs {
+    const void *x, *down, *up, *base;
+    void *out;
+    int64_t x_stride, base_stride, out_stride, K, C;
+    const float *x_step, *base_step, *scale;
+    const int32_t *ids;
+    float *h;
+    int R, adapters, base_type, out_type;
+};
+constexpr int kTokenThreads = 512, kTokenColumns = 256, kTokenGroups = kTokenThreads / 32, kTokenRanks = 64;
+
+template <typename TX, typename TW, bool VEC>
+__global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
+{
+    __shared__ float hs[kTokenRanks];
+    __shared__ v8f sums[kTokenGroups][32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = threadIdx.x >> 5;
+    const int64_t row = blockIdx.y, col0 = (int64_t)blockIdx.x * kTokenColumns, col = col0 + 8 * (threadIdx.x & 31);
+    const int id = a.ids[row];
+    float base = 0.0f;
+    if (a.base && threadIdx.x < kTokenColumns && col0 + threadIdx.x < a.C) {
+        const int64_t at = row * a.base_stride + col0 + threadIdx.x;
+        base = (a.base_type == PWLQ_F32 ? ((const float *)a.base)[at] : widen(((const TW *)a.base)[at])) * (a.base_step ? a.base_step[row] : 1.0f);
+    }
+    v8f y = v8f(0);
+    if (id >= 0 && id < a.adapters) {
+        const TW *up = (const TW *)a.up + (int64_t)id * a.R * a.C;
+        const typename Vec8<TW>::type ahead = piece<TW, VEC>(up + (int64_t)min(group, a.R - 1) * a.C, col, a.C);
+        const TX *x = (const TX *)a.x + row * a.x_stride;
+        const float scale = a.x_step ? a.scale[id] * a.x_step[row] : a.scale[id];
+        for (int r = wave; r < a.R; r += kTokenThreads / 64) {
+            const TW *w = (const TW *)a.down + ((int64_t)id * a.R + r) * a.K;
+            v8f t = v8f(0);
+            int64_t k = 8 * lane;
+            for (; k + 3 * 512 < a.K; k += 4 * 512) {
+                typename Vec8<TX>::type xv[4];
+                typename Vec8<TW>::type wv[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    xv[i] = piece<TX, VEC>(x, k + 512 * i, a.K);
+                    wv[i] = piece<TW, VEC>(w, k + 512 * i, a.K);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t += widen(xv[i]) * widen(wv[i]);
+            }
+            for (; k < a.K; k += 512) t += widen(piece<TX, VEC>(x, k, a.K)) * widen(piece<TW, VEC>(w, k, a.K));
+            const float s = wave_sum(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
+            if (lane == 0) hs[r] = s * scale;
+        }
+        __syncthreads();
+        if (blockIdx.x == 0 && threadIdx.x < a.R) a.h[row * a.R + threadIdx.x] = hs[threadIdx.x];
+        if (group < a.R) y = hs[group] * widen(ahead);
+        for (int r = group + kTokenGroups; r < a.R; r += kTokenGroups) y += hs[r] * widen(piece<TW, VEC>(up + (int64_t)r * a.C, col, a.C));
+    } else if (blockIdx.x == 0 && threadIdx.x < a.R) {
+        a.h[row * a.R + threadIdx.x] = 0.0f;
+    }
+    sums[group][threadIdx.x & 31] = y;
+    __syncthreads();
+    if (threadIdx.x >= kTokenColumns || col0 + threadIdx.x >= a.C) return;
+    float s = 0.0f;
+#pragma unroll
+    for (int g = 0; g < kTokenGroups; ++g) s += ((const float *)sums[g])[threadIdx.x];
+    const int64_t at = row * a.out_stride + col0 + threadIdx.x;
+    if (a.out_type == PWLQ_F32) ((float *)a.out)[at] = base + s;
+    else ((TW *)a.out)[at] = (TW)(base + s);
+}
+
 // --------------------------------------------------------------------------
 // outer products
 // --------------------------------------------------------------------------
@@ -597,16 +669,61 @@ void outer(const pwlq_rows &x, int64_t T, int64_t C, int R, int adapters, const 
 
 bool whole_vectors(int64_t C, const void *w) { return C % 8 == 0 && aligned16(w); }
 
+// Whether few rows go through one launch.
+bool by_token(const pwlq_adapter_args &a)
+{
+    return a.T <= kTokenRows && a.R <= kTokenRanks;
+}
+
+template <typename TX, typename TW> void token_as(const TokenArgs &a, int64_t rows, bool vec, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((a.C + kTokenColumns - 1) / kTokenColumns), (unsigned)rows);
+    if (vec) k_adapter_token<TX, TW, true><<<grid, kTokenThreads, 0, stream>>>(a);
+    else k_adapter_token<TX, TW, false><<<grid, kTokenThreads, 0, stream>>>(a);
+}
+
+void token(const pwlq_adapter_args &a, hipStream_t stream)
+{
+    TokenArgs t = {};
+    t.x = a.x.data;
+    t.down = a.down;
+    t.up = a.up;
+    t.base = a.base.data;
+    t.out = a.out.data;
+    t.x_stride = a.x.stride;
+    t.base_stride = a.base.stride;
+    t.out_stride = a.out.stride;
+    t.K = a.K;
+    t.C = a.N;
+    t.x_step = a.x.step;
+    t.base_step = a.base.data ? a.base.step : nullptr;
+    t.scale = a.scale;
+    t.ids = a.ids;
+    t.h = a.h;
+    t.R = a.R;
+    t.adapters = a.adapters;
+    t.base_type = a.base.type;
+    t.out_type = a.out.type;
+    const bool vec = whole_vectors(a.K, a.down) && whole_vectors(a.N, a.up) && vectors(a.x, a.T), packed = a.x.type == PWLQ_I8;
+    if (a.weight_type == PWLQ_F32) packed ? token_as<int8_t, float>(t, a.T, vec, stream) : token_as<float, float>(t, a.T, vec, stream);
+    else if (a.weight_type == PWLQ_BF16) packed ? token_as<int8_t, bf16>(t, a.T, vec, stream) : token_as<bf16, bf16>(t, a.T, vec, stream);
+    else packed ? token_as<int8_t, f16>(t, a.T, vec, stream) : token_as<f16, f16>(t, a.T, vec, stream);
+}
+
 } // namespace
 
 size_t adapter_workspace(int64_t T, int64_t K, int R)
 {
     const int splits = first_splits(T, K, R);
-    return splits > 1 ? (size_t)splits * (size_t)T * (size_t)R * sizeof(float) : 256;
+    return splits > 1 ? (size_t)splits * (size_t)T * (size_t)R * sizeof(float) : 0;
 }
 
 void adapter_forward(const pwlq_adapter_args &a, void *workspace, hipStream_t stream)
 {
+    if (by_token(a)) {
+        token(a, stream);
+        return;
+    }
     FirstArgs f = {};
     f.x = a.x.data;
     f.w = a.down;
@@ -644,7 +761,7 @@ void adapter_forward(const pwlq_adapter_args &a, void *workspace, hipStream_t st
 
 size_t adapter_backward_workspace(int64_t T, int64_t K, int64_t N, int R, int adapters)
 {
-    return T ? BackwardSpace(nullptr, T, K, N, R, adapters).bytes : 256;
+    return T ? BackwardSpace(nullptr, T, K, N, R, adapters).bytes : 0;
 }
 
 void adapter_backward(const pwlq_adapter_backward_args &a, void *workspace, hipStream_t stream)

@@ -31,6 +31,7 @@ int check_sizes(int64_t T, int64_t cols, int64_t most)
 
 int check_room(const void *workspace, size_t bytes, size_t need)
 {
+    if (!need) return PWLQ_OK;
     if (!workspace) return fail(PWLQ_EWORKSPACE, "workspace is NULL (%zu bytes needed)", need);
     if (((uintptr_t)workspace & 255) != 0) return fail(PWLQ_EWORKSPACE, "workspace is not 256-byte aligned");
     if (bytes < need) return fail(PWLQ_EWORKSPACE, "workspace holds %zu bytes, %zu needed", bytes, need);

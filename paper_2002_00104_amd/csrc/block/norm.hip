@@ -10,6 +10,8 @@
 #include "launch.h"
 #include "rows.h"
 
+#pragma clang fp contract(fast)
+
 namespace pwlq_block {
 namespace {
 
@@ -271,8 +273,9 @@ void norm_block(const pwlq_norm_args &a, hipStream_t stream)
 // Partial rows in the workspace: d_pre's, d_post's, then d_gate's.
 size_t norm_backward_workspace(int64_t T, int64_t D, int64_t gate_rows)
 {
-    const int64_t wgs = T ? (T + backward_span(T) - 1) / backward_span(T) : 0;
-    return (size_t)(3 * wgs + gate_rows) * (size_t)D * sizeof(float) + 256;
+    if (!T) return 0;
+    const int64_t wgs = (T + backward_span(T) - 1) / backward_span(T);
+    return (size_t)(3 * wgs + gate_rows) * (size_t)D * sizeof(float);
 }
 
 void norm_backward(const pwlq_norm_backward_args &a, void *workspace, hipStream_t stream)

@@ -66,14 +66,16 @@ def test_workspace_sizes(calls):
     for T in (0, 1, 16, 17, 63, 64, 65, 511, 513, 4096, 100000):
         for K in (1, 63, 128, 4096, 11008):
             for R in (1, 16, 17, 256):
-                assert calls.pwlq_adapter_workspace_bytes(T, K, R) > 0
+                # parts of long reductions only
+                if T <= 16 or K <= 512:
+                    assert calls.pwlq_adapter_workspace_bytes(T, K, R) == 0
                 for n in (1, 32):
                     # the adapters' gradients come in parts only where rows leave something to split
                     need = calls.pwlq_adapter_backward_workspace_bytes(T, K, 1000, R, n)
-                    assert need >= (4 * T * R if T else 1)
+                    assert need >= 4 * T * R and (need > 0) == (T > 0)
             for G in {0, 1, T}:
                 if G <= T:
-                    assert calls.pwlq_norm_block_backward_workspace_bytes(T, min(K, 16384), G) >= 4 * G
+                    assert calls.pwlq_norm_block_backward_workspace_bytes(T, min(K, 16384), G) >= (4 * G if T else 0)
     assert calls.pwlq_adapter_workspace_bytes(-1, 8, 8) == 0
     assert calls.pwlq_adapter_workspace_bytes(8, 8, 257) == 0
     assert calls.pwlq_adapter_backward_workspace_bytes(8, 8, 8, 8, 0) == 0
@@ -128,7 +130,7 @@ def test_norms(calls):
 
 
 def test_adapters(calls):
-    ok = Adapter(4, 64, 48, 8, 2, BF16, FAKE, FAKE, FAKE, FAKE, rows(64), rows(48, F32, step=FAKE), rows(48), FAKE)
+    ok = Adapter(40, 1024, 48, 8, 2, BF16, FAKE, FAKE, FAKE, FAKE, rows(1024), rows(48, F32, step=FAKE), rows(48), FAKE)
 
     def call(workspace=FAKE, room=ROOM, **kw):
         return calls.pwlq_adapter(ctypes.byref(changed(ok, **kw)), workspace, room, None)
@@ -137,13 +139,13 @@ def test_adapters(calls):
     assert calls.pwlq_adapter(None, FAKE, ROOM, None) == ENULL
     for name in ("down", "up", "ids", "scale", "h"):
         assert call(**{name: None}) == ENULL, name
-    assert call(x=rows(64, I8)) == ENULL and call(out=rows(48, data=None)) == ENULL
+    assert call(x=rows(1024, I8)) == ENULL and call(out=rows(48, data=None)) == ENULL
     assert call(R=0) == EINVAL and call(R=257) == EINVAL and call(adapters=0) == EINVAL and call(adapters=65536) == EINVAL
     assert call(K=0) == EINVAL and call(N=0) == EINVAL and call(N=(1 << 22) + 1) == EINVAL and call(T=-1) == EINVAL
     assert call(T=1 << 26, N=1 << 22) == EINVAL and call(T=1 << 26, K=1 << 22) == EINVAL
     assert call(weight_type=I8) == EINVAL and call(weight_type=F16) == EINVAL and call(down=FAKE + 1) == EINVAL
-    assert call(x=rows(64, F32)) == EINVAL and call(out=rows(48, I8, step=FAKE)) == EINVAL and call(base=rows(48, F16)) == EINVAL
-    assert call(x=rows(64, stride=60)) == EINVAL and call(x=rows(64, step=FAKE)) == EINVAL
+    assert call(x=rows(1024, F32)) == EINVAL and call(out=rows(48, I8, step=FAKE)) == EINVAL and call(base=rows(48, F16)) == EINVAL
+    assert call(x=rows(1024, stride=1020)) == EINVAL and call(x=rows(1024, step=FAKE)) == EINVAL
     assert call(workspace=None) == EWORKSPACE and call(workspace=FAKE + 8) == EWORKSPACE and call(room=8) == EWORKSPACE
 
     ok = AdapterBackward(40, 64, 48, 8, 2, BF16, FAKE, FAKE, FAKE, FAKE, rows(48), rows(64, I8, step=FAKE), rows(64, F32), rows(64, F32),

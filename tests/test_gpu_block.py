@@ -468,7 +468,8 @@ def test_what_is_refused(B):
     with pytest.raises(pwlq.PwlqError):
         B.adapter(x, f(2, 257, 64), f(2, 257, 48), ids, scale)
     with pytest.raises(pwlq.PwlqError):
-        B.adapter(x, down, up, ids, scale, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+        B.adapter(f(40, 1024), f(2, 4, 1024), up, torch.zeros(40, dtype=torch.int32, device="cuda"), scale,
+                  workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         B.norm_block_backward(None, None, x, x, pre_weight=w)
     with pytest.raises(ValueError):
