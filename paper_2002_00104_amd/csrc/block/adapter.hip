@@ -17,7 +17,11 @@
 namespace pwlq_block {
 namespace {
 
-constexpr int kRows = 32;              // rows of a tile of the first and the second product: two of the matrix instructions'
+constexpr int kRows = 32;              // rows of a tile of the first product: two of the matrix instructions'
+
+// Nothing is moved across: the loads above it are issued before what uses them.  The compiler would otherwise put each beside its use,
+// which saves registers and waits for memory once per load.
+__device__ inline void loads_first() { __builtin_amdgcn_sched_barrier(0); }
 
 __device__ inline int64_t clamp_row(int64_t row, int64_t rows) { return row < rows ? row : rows - 1; }
 
@@ -25,14 +29,12 @@ __device__ inline int64_t clamp_row(int64_t row, int64_t rows) { return row < ro
 struct Adapters {
     int id;                            // of the lane's row; -1: none
     uint64_t left;                     // rows not yet visited
-    __device__ Adapters(const int32_t *ids, int64_t row0, int64_t rows, int adapters, int count)
+    // `v`: the lane's id, by load()
+    static __device__ int load(const int32_t *ids, int64_t row0, int64_t rows) { return ids[clamp_row(row0 + (threadIdx.x & 63), rows)]; }
+    __device__ Adapters(int v, int64_t row0, int64_t rows, int adapters, int count)
     {
         const int lane = threadIdx.x & 63;
-        id = -1;
-        if (lane < count && row0 + lane < rows) {
-            const int v = ids[row0 + lane];
-            if (v >= 0 && v < adapters) id = v;
-        }
+        id = lane < count && row0 + lane < rows && v >= 0 && v < adapters ? v : -1;
         left = __ballot(id >= 0);
     }
     __device__ bool next(int &adapter, uint64_t &mine)
@@ -64,17 +66,29 @@ __device__ inline v4f multiply(v8f x, v8f w, v4f acc)
     return acc;
 }
 
-// Eight elements from column k on; those from `cols` on are 0.
-template <typename T, bool VEC> __device__ inline typename Vec8<T>::type piece(const T *row, int64_t k, int64_t cols)
+// Eight elements from column `col` on, without a branch, so that several loads can be under way: columns beyond the last are
+// read from it.
+template <typename T, bool VEC> __device__ inline typename Vec8<T>::type columns8(const T *row, int64_t col, int64_t cols)
 {
     typedef typename Vec8<T>::type V;
-    if constexpr (VEC) return k < cols ? *(const V *)(row + k) : V(0);
+    if constexpr (VEC) return *(const V *)(row + min(col, cols - 8));
     else {
         union { V v; T e[8]; } u;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u.e[i] = k + i < cols ? row[k + i] : T(0);
+        for (int i = 0; i < 8; ++i) u.e[i] = row[min(col + i, cols - 1)];
         return u.v;
     }
+}
+// The same with 0 for the columns beyond: elements of a reduction.
+template <typename T, bool VEC> __device__ inline typename Vec8<T>::type piece(const T *row, int64_t k, int64_t cols)
+{
+    typedef typename Vec8<T>::type V;
+    union { V v; T e[8]; } u;
+    u.v = columns8<T, VEC>(row, k, cols);
+    if constexpr (VEC) return k < cols ? u.v : V(0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u.e[i] = k + i < cols ? u.e[i] : T(0);
+    return u.v;
 }
 
 struct FirstArgs {
@@ -86,11 +100,18 @@ struct FirstArgs {
     float *out;                        // [splits, rows, R]: a sum for each part of the reduction
 };
 
+// Column of half `half` of a lane's sixteen elements in a step of 64: four lanes read 64 bytes of a row in one instruction.
+template <typename TX> __device__ inline int half_at(int q, int half) { return sizeof(TX) == 1 ? 16 * q + 8 * half : 32 * half + 8 * q; }
+
 // A tile of 32 rows by 16 RT ranks, and a part of the reduction.  The four wavefronts take its steps of 64 elements in turn
-// (a lane 16 neighbouring ones of a row, so four lanes read 128 bytes of bfloat16) and add up in LDS.
+// and add up in LDS.  Several steps' loads are issued before the first one's products: a wavefront waits for memory
+// once per batch.
 template <typename TX, typename TW, int RT, bool VEC>
 __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
 {
+    constexpr int kBatch = sizeof(TW) == 2 ? (RT == 1 ? 4 : 2) : (RT == 1 ? 2 : 1);
+    typedef typename Vec8<TX>::type XV;
+    typedef typename Vec8<TW>::type WV;
     __shared__ float sums[4][kRows][16 * RT];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
     const int64_t row0 = (int64_t)(blockIdx.x / a.slots) * kRows;
@@ -101,7 +122,7 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
 #pragma unroll
     for (int m = 0; m < 2; ++m) xr[m] = (const TX *)a.x + clamp_row(row0 + 16 * m + l, a.rows) * a.stride;
 
-    Adapters of(a.ids, row0, a.rows, a.adapters, kRows);
+    Adapters of(Adapters::load(a.ids, row0, a.rows), row0, a.rows, a.adapters, kRows);
     if (slot == 0) {                                   // rows without an adapter
         const uint64_t none = ~of.left;
         for (int i = threadIdx.x; i < kRows * 16 * RT; i += 256) {
@@ -123,32 +144,42 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
             for (int n = 0; n < RT; ++n) acc[m][n] = v4f(0);
         int64_t k = k0 + 64 * wave;
         if constexpr (VEC) {
-            for (; k + 64 <= k1; k += 256) {
-                const int64_t c = k + 16 * q;
+            for (; k + 256 * (kBatch - 1) + 64 <= k1; k += 256 * kBatch) {
+                XV x[kBatch][2][2];
+                WV w[kBatch][2][RT];
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    typename Operand<TW>::type x[2];
+                for (int b = 0; b < kBatch; ++b)
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) x[m] = operand<TW, TX>(*(const typename Vec8<TX>::type *)(xr[m] + c + 8 * half));
+                    for (int half = 0; half < 2; ++half) {
+                        const int64_t c = k + 256 * b + half_at<TX>(q, half);
 #pragma unroll
-                    for (int n = 0; n < RT; ++n) {
-                        const typename Operand<TW>::type w = *(const typename Vec8<TW>::type *)(wr[n] + c + 8 * half);
+                        for (int m = 0; m < 2; ++m) x[b][half][m] = *(const XV *)(xr[m] + c);
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) acc[m][n] = multiply(x[m], w, acc[m][n]);
+                        for (int n = 0; n < RT; ++n) w[b][half][n] = *(const WV *)(wr[n] + c);
                     }
-                }
+                loads_first();
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            const typename Operand<TW>::type xm = operand<TW, TX>(x[b][half][m]);
+#pragma unroll
+                            for (int n = 0; n < RT; ++n) acc[m][n] = multiply(xm, w[b][half][n], acc[m][n]);
+                        }
             }
         }
         for (; k < k1; k += 256) {
-            const int64_t c = k + 16 * q;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
+                const int64_t c = k + half_at<TX>(q, half);
                 typename Operand<TW>::type x[2];
 #pragma unroll
-                for (int m = 0; m < 2; ++m) x[m] = operand<TW, TX>(piece<TX, VEC>(xr[m], c + 8 * half, k1));
+                for (int m = 0; m < 2; ++m) x[m] = operand<TW, TX>(piece<TX, VEC>(xr[m], c, k1));
 #pragma unroll
                 for (int n = 0; n < RT; ++n) {
-                    const typename Operand<TW>::type w = piece<TW, VEC>(wr[n], c + 8 * half, k1);
+                    const WV w = piece<TW, VEC>(wr[n], c, k1);
 #pragma unroll
                     for (int m = 0; m < 2; ++m) acc[m][n] = multiply(x[m], w, acc[m][n]);
                 }
@@ -186,8 +217,12 @@ struct SecondArgs {
     int R, splits, adapters, out_type, column_tiles;
 };
 
-// A wavefront does 32 rows by 128 columns, with binary32 matrix instructions: H stays in binary32, and a lane's eight
-// neighbouring columns are eight instructions, so neither W nor Y needs a transposition and both move in vectors.
+// A wavefront does 16 rows by 128 columns, with binary32 matrix instructions: H stays in binary32, and a lane's eight
+// neighbouring columns are eight instructions, so neither W nor Y needs a transposition and both move in vectors.  The ranks
+// come sixteen at a time, their products added to the row's sum where the row has the adapter.
+constexpr int kSecondRows = 16;
+__host__ __device__ inline int second_pitch(int R) { return (R + 15) / 16 * 16 + 1; }
+
 template <typename T> __device__ inline void store_columns(void *data, int64_t at, int64_t col, int64_t cols, v8f v, bool vec)
 {
     T *p = (T *)data + at + col;
@@ -203,76 +238,107 @@ template <typename T> __device__ inline void store_columns(void *data, int64_t a
 template <typename TW, typename TB, bool VEC>
 __global__ __launch_bounds__(256) void k_adapter_second(SecondArgs a)
 {
+    typedef typename Vec8<TW>::type WV;
+    typedef typename Vec8<TB>::type BV;
     extern __shared__ float hs[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
-    const int64_t row0 = (int64_t)(blockIdx.x / a.column_tiles) * kRows;
-    const int tile = blockIdx.x % a.column_tiles, pitch = (a.R + 3) / 4 * 4 + 1;
+    const int64_t row0 = (int64_t)(blockIdx.x / a.column_tiles) * kSecondRows;
+    const int tile = blockIdx.x % a.column_tiles, pitch = second_pitch(a.R);
     const int64_t col = ((int64_t)tile * (blockDim.x / 64) + wave) * 128 + 8 * l;
 
-    v8f acc[2][4];
+    const int id = Adapters::load(a.ids, row0, a.rows);
+    BV base[4];
+    if (a.base) {
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+        for (int i = 0; i < 4; ++i)
+            base[i] = columns8<TB, VEC>((const TB *)a.base + clamp_row(row0 + 4 * q + i, a.rows) * a.base_stride, col, a.C);
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t row = clamp_row(row0 + 16 * m + 4 * q + i, a.rows);
-            acc[m][i] = a.base ? widen(piece<TB, VEC>((const TB *)a.base + row * a.base_stride, col, a.C)) : v8f(0);
-        }
-    for (int i = threadIdx.x; i < kRows * (pitch - 1); i += blockDim.x) {
-        const int row = i / (pitch - 1), r = i % (pitch - 1);
-        float s = 0.0f;
-        if (row0 + row < a.rows && r < a.R) {
-            const int64_t at = (row0 + row) * a.R + r;
-            for (int p = 0; p < a.splits; ++p) s += a.h[p * a.rows * a.R + at];
-            if (tile == 0 && a.h_out) a.h_out[at] = s;
-        }
-        hs[row * pitch + r] = s;
+        for (int i = 0; i < 4; ++i) base[i] = BV(0);
     }
+    float factor[4];                                   // without factors any number that can be read
+    const float *from = a.base_step ? a.base_step : a.h;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) factor[i] = from[a.base_step ? clamp_row(row0 + 4 * q + i, a.rows) : 0];
+    loads_first();
+    Adapters of(id, row0, a.rows, a.adapters, kSecondRows);
+    // the ranks r0 to r0 + 15 of one adapter's W, those beyond R 0
+    auto ranks = [&](int adapter, int r0, WV (&v)[4]) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            v[s] = columns8<TW, VEC>((const TW *)a.w + ((int64_t)adapter * a.R + min(r0 + 4 * s + q, a.R - 1)) * a.C, col, a.C);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) v[s] = r0 + 4 * s + q < a.R ? v[s] : WV(0);
+    };
+    int adapter = 0;
+    uint64_t mine = 0;
+    bool more = of.next(adapter, mine);
+    WV w[4];
+    ranks(adapter, 0, w);
+
+    for (int row = threadIdx.x >> 4; row < kSecondRows; row += blockDim.x >> 4)
+        for (int r = l; r < pitch - 1; r += 16) {
+            const int64_t at = clamp_row(row0 + row, a.rows) * a.R + min(r, a.R - 1);
+            float s = 0.0f;
+            for (int p = 0; p < a.splits; p += 4) {
+                float v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = a.h[min(p + j, a.splits - 1) * a.rows * a.R + at];
+                loads_first();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s += p + j < a.splits ? v[j] : 0.0f;
+            }
+            if (r >= a.R) s = 0.0f;
+            else if (tile == 0 && a.h_out && row0 + row < a.rows) a.h_out[at] = s;
+            hs[row * pitch + r] = s;
+        }
     __syncthreads();
+    v8f acc[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = widen(base[i]);
     if (a.base_step) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[m][i] *= a.base_step[clamp_row(row0 + 16 * m + 4 * q + i, a.rows)];
+        for (int i = 0; i < 4; ++i) acc[i] *= factor[i];
     }
-    Adapters of(a.ids, row0, a.rows, a.adapters, kRows);
-    int adapter;
-    uint64_t mine;
-    while (of.next(adapter, mine)) {
-        const TW *w = (const TW *)a.w + (int64_t)adapter * a.R * a.C;
-        v4f y[2][8];
+    int r0 = 0;
+    while (more) {
+        v8f wv[4];
+        float h[4];
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[m][j] = v4f(0);
-        for (int step = 0; step < pitch - 1; step += 4) {
-            const int r = step + q;
-            v8f wv = widen(piece<TW, VEC>(w + (int64_t)min(r, a.R - 1) * a.C, col, a.C));
-            if (r >= a.R) wv = v8f(0);
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const float h = hs[(16 * m + l) * pitch + r];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[m][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(h, wv[j], y[m][j], 0, 0, 0);
-            }
+        for (int s = 0; s < 4; ++s) {
+            wv[s] = widen(w[s]);
+            h[s] = hs[l * pitch + r0 + 4 * s + q];
         }
+        const uint64_t rows = mine;
+        r0 += 16;
+        if (r0 >= a.R) {
+            r0 = 0;
+            more = of.next(adapter, mine);
+        }
+        if (more) ranks(adapter, r0, w);
+        v4f y[8];
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int j = 0; j < 8; ++j) y[j] = v4f(0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if ((mine >> (16 * m + 4 * q + i)) & 1) {
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[m][i][j] += y[m][j][i];
-                }
-    }
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
+            for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[s], wv[s][j], y[j], 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t row = row0 + 16 * m + 4 * q + i;
-            if (row >= a.rows) continue;
-            if (a.out_type == PWLQ_F32) store_columns<float>(a.out, row * a.out_stride, col, a.C, acc[m][i], VEC);
-            else store_columns<TW>(a.out, row * a.out_stride, col, a.C, acc[m][i], VEC);
+            const bool own = (rows >> (4 * q + i)) & 1;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[i][j] += own ? y[j][i] : 0.0f;
         }
+    }
+    if (a.out_type == PWLQ_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (row0 + 4 * q + i < a.rows) store_columns<float>(a.out, (row0 + 4 * q + i) * a.out_stride, col, a.C, acc[i], VEC);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (row0 + 4 * q + i < a.rows) store_columns<TW>(a.out, (row0 + 4 * q + i) * a.out_stride, col, a.C, acc[i], VEC);
+    }
 }
 
 // --------------------------------------------------------------------------
@@ -322,9 +388,8 @@ __global__ __launch_bounds__(256) void k_adapter_second_token(SecondArgs a)
     else store_columns<TW>(a.out, row * a.out_stride, col, a.C, y, VEC);
 }
 
-// Both products of one row in one launch, for 256 columns: the row's H is computed by each of its workgroups anew, which costs
-// reading down again from L2 but no second launch and no wait for it.  Wavefronts share the ranks of the first product, half
-// wavefronts (eight columns a lane) those of the second.
+// Both products of one row in one launch, for 512 columns: the row's H is computed by each of its workgroups anew, which costs
+// reading down again from L2 but no second launch and no wait for it.  The sixteen wavefronts share the ranks of both products.
 struct TokenArgs {
     const void *x, *down, *up, *base;
     void *out;
@@ -334,15 +399,18 @@ struct TokenArgs {
     float *h;
     int R, adapters, base_type, out_type;
 };
-constexpr int kTokenThreads = 512, kTokenColumns = 256, kTokenGroups = kTokenThreads / 32, kTokenRanks = 64;
+constexpr int kTokenThreads = 1024, kTokenColumns = 512, kTokenWaves = kTokenThreads / 64, kTokenRanks = 64;
 
 template <typename TX, typename TW, bool VEC>
 __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
 {
+    typedef typename Vec8<TX>::type XV;
+    typedef typename Vec8<TW>::type WV;
+    constexpr int kAhead = sizeof(TW) == 2 ? 8 : 4;            // vectors of a lane in flight
     __shared__ float hs[kTokenRanks];
-    __shared__ v8f sums[kTokenGroups][32];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = threadIdx.x >> 5;
-    const int64_t row = blockIdx.y, col0 = (int64_t)blockIdx.x * kTokenColumns, col = col0 + 8 * (threadIdx.x & 31);
+    __shared__ v8f sums[kTokenWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = blockIdx.y, col0 = (int64_t)blockIdx.x * kTokenColumns, col = col0 + 8 * lane;
     const int id = a.ids[row];
     float base = 0.0f;
     if (a.base && threadIdx.x < kTokenColumns && col0 + threadIdx.x < a.C) {
@@ -352,41 +420,50 @@ __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
     v8f y = v8f(0);
     if (id >= 0 && id < a.adapters) {
         const TW *up = (const TW *)a.up + (int64_t)id * a.R * a.C;
-        const typename Vec8<TW>::type ahead = piece<TW, VEC>(up + (int64_t)min(group, a.R - 1) * a.C, col, a.C);
+        const WV ahead = piece<TW, VEC>(up + (int64_t)min(wave, a.R - 1) * a.C, col, a.C);
         const TX *x = (const TX *)a.x + row * a.x_stride;
         const float scale = a.x_step ? a.scale[id] * a.x_step[row] : a.scale[id];
-        for (int r = wave; r < a.R; r += kTokenThreads / 64) {
+        for (int r = wave; r < a.R; r += kTokenWaves) {
             const TW *w = (const TW *)a.down + ((int64_t)id * a.R + r) * a.K;
             v8f t = v8f(0);
-            int64_t k = 8 * lane;
-            for (; k + 3 * 512 < a.K; k += 4 * 512) {
-                typename Vec8<TX>::type xv[4];
-                typename Vec8<TW>::type wv[4];
+            int64_t k = 0;
+            if constexpr (VEC) {
+                // vectors beyond the row are read from its last one and count nothing
+                for (; k < a.K; k += 512 * kAhead) {
+                    XV xv[kAhead];
+                    WV wv[kAhead];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    xv[i] = piece<TX, VEC>(x, k + 512 * i, a.K);
-                    wv[i] = piece<TW, VEC>(w, k + 512 * i, a.K);
+                    for (int i = 0; i < kAhead; ++i) {
+                        const int64_t c = min(k + 512 * i + 8 * lane, a.K - 8);
+                        xv[i] = *(const XV *)(x + c);
+                        wv[i] = *(const WV *)(w + c);
+                    }
+                    loads_first();
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        const v8f p = widen(xv[i]) * widen(wv[i]);
+                        t += k + 512 * i + 8 * lane < a.K ? p : v8f(0);
+                    }
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) t += widen(xv[i]) * widen(wv[i]);
+            } else {
+                for (k = 8 * lane; k < a.K; k += 512) t += widen(piece<TX, VEC>(x, k, a.K)) * widen(piece<TW, VEC>(w, k, a.K));
             }
-            for (; k < a.K; k += 512) t += widen(piece<TX, VEC>(x, k, a.K)) * widen(piece<TW, VEC>(w, k, a.K));
             const float s = wave_sum(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
             if (lane == 0) hs[r] = s * scale;
         }
         __syncthreads();
         if (blockIdx.x == 0 && threadIdx.x < a.R) a.h[row * a.R + threadIdx.x] = hs[threadIdx.x];
-        if (group < a.R) y = hs[group] * widen(ahead);
-        for (int r = group + kTokenGroups; r < a.R; r += kTokenGroups) y += hs[r] * widen(piece<TW, VEC>(up + (int64_t)r * a.C, col, a.C));
+        if (wave < a.R) y = hs[wave] * widen(ahead);
+        for (int r = wave + kTokenWaves; r < a.R; r += kTokenWaves) y += hs[r] * widen(piece<TW, VEC>(up + (int64_t)r * a.C, col, a.C));
     } else if (blockIdx.x == 0 && threadIdx.x < a.R) {
         a.h[row * a.R + threadIdx.x] = 0.0f;
     }
-    sums[group][threadIdx.x & 31] = y;
+    sums[wave][lane] = y;
     __syncthreads();
     if (threadIdx.x >= kTokenColumns || col0 + threadIdx.x >= a.C) return;
     float s = 0.0f;
 #pragma unroll
-    for (int g = 0; g < kTokenGroups; ++g) s += ((const float *)sums[g])[threadIdx.x];
+    for (int g = 0; g < kTokenWaves; ++g) s += ((const float *)sums[g])[threadIdx.x];
     const int64_t at = row * a.out_stride + col0 + threadIdx.x;
     if (a.out_type == PWLQ_F32) ((float *)a.out)[at] = base + s;
     else ((TW *)a.out)[at] = (TW)(base + s);
@@ -406,13 +483,17 @@ struct OuterArgs {
     int32_t *present;                  // [splits, adapters]: whether the part has rows of the adapter; NULL where there is one part
 };
 
-// 16 RT ranks by 128 columns of one adapter's gradient, over a part of the rows.  As in the second product a lane's eight
-// neighbouring columns are eight binary32 matrix instructions; a step is four rows, and the four wavefronts take sixteen rows
-// of 64 each.  Rows of other adapters are zeroed in both operands (an infinity there times 0 would be NaN).
+// 16 RT ranks by 128 columns of one adapter's gradient, over a part of the rows.  The rows of the adapter are listed in LDS
+// first, 512 at a time, so that no other row is read.  As in the second product a lane's eight neighbouring columns are eight
+// binary32 matrix instructions; a step is four rows, and a wavefront has several steps' loads in flight.
+constexpr int kListed = 512;
+
 template <typename TX, int RT, bool VEC>
 __global__ __launch_bounds__(256) void k_adapter_outer(OuterArgs a)
 {
+    constexpr int kSteps = RT == 4 ? 4 : 8;
     __shared__ v4f sums[2][RT * 8][64];
+    __shared__ int list[kListed];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
     const int64_t col = (int64_t)(blockIdx.x % a.column_tiles) * 128 + 8 * l;
     const int r0 = blockIdx.x / a.column_tiles * 16 * RT, adapter = blockIdx.y, split = blockIdx.z;
@@ -422,36 +503,52 @@ __global__ __launch_bounds__(256) void k_adapter_outer(OuterArgs a)
     for (int n = 0; n < RT; ++n)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[n][j] = v4f(0);
-    uint64_t any = 0;
-    for (int64_t t = t0; t < t1; t += 64) {
-        const bool is = t + lane < t1 && a.ids[t + lane] == adapter;
-        const uint64_t mine = __ballot(is);
-        any |= mine;
-        if (!((mine >> (16 * wave)) & 0xffff)) continue;
-        typename Vec8<TX>::type x[4];
-        float h[4][RT];
+    bool any = false;
+    for (int64_t t = t0; t < t1; t += kListed) {
+        int id[kListed / 64];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int64_t row = clamp_row(t + 16 * wave + 4 * s + q, a.rows);
-            x[s] = piece<TX, VEC>((const TX *)a.x + row * a.stride, col, a.C);
+        for (int g = 0; g < kListed / 64; ++g) id[g] = a.ids[clamp_row(t + 64 * g + lane, t1)];
+        loads_first();
+        int count = 0;
+        __syncthreads();
 #pragma unroll
-            for (int n = 0; n < RT; ++n) h[s][n] = a.h[row * a.R + min(r0 + 16 * n + l, a.R - 1)] * (a.step ? a.step[row] : 1.0f);
+        for (int g = 0; g < kListed / 64; ++g) {
+            const uint64_t mine = __ballot(id[g] == adapter && t + 64 * g + lane < t1);
+            if (g % 4 == wave && ((mine >> lane) & 1)) list[count + __builtin_popcountll(mine & ((1ull << lane) - 1))] = 64 * g + lane;
+            count += __builtin_popcountll(mine);
         }
+        __syncthreads();
+        any |= count != 0;
+        for (int first = 4 * kSteps * wave; first < count; first += 16 * kSteps) {
+            typename Vec8<TX>::type x[kSteps];
+            float h[kSteps][RT], step[kSteps];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const bool own = (mine >> (16 * wave + 4 * s + q)) & 1;
-            v8f xv = widen(x[s]);
-            if (!own) xv = v8f(0);
+            for (int s = 0; s < kSteps; ++s) {
+                const int64_t row = t + list[min(first + 4 * s + q, count - 1)];
+                x[s] = columns8<TX, VEC>((const TX *)a.x + row * a.stride, col, a.C);
 #pragma unroll
-            for (int n = 0; n < RT; ++n) {
-                const float hv = own ? h[s][n] : 0.0f;
+                for (int n = 0; n < RT; ++n) h[s][n] = a.h[row * a.R + min(r0 + 16 * n + l, a.R - 1)];
+                if constexpr (sizeof(TX) == 1) step[s] = a.step[row];
+            }
+            loads_first();
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(hv, xv[j], acc[n][j], 0, 0, 0);
+            for (int s = 0; s < kSteps; ++s) {
+                const bool own = first + 4 * s + q < count;
+                v8f xv = widen(x[s]);
+                if (!own) xv = v8f(0);
+#pragma unroll
+                for (int n = 0; n < RT; ++n) {
+                    float hv = h[s][n];
+                    if constexpr (sizeof(TX) == 1) hv *= step[s];
+                    hv = own ? hv : 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(hv, xv[j], acc[n][j], 0, 0, 0);
+                }
             }
         }
     }
     if (a.present) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) a.present[split * a.adapters + adapter] = any != 0;
+        if (blockIdx.x == 0 && threadIdx.x == 0) a.present[split * a.adapters + adapter] = any;
         if (!any) return;
     }
     if (wave >= 2) {
@@ -503,13 +600,26 @@ struct JoinArgs {
 };
 __global__ __launch_bounds__(256) void k_adapter_join(JoinArgs a)
 {
-    const int which = blockIdx.z, adapter = blockIdx.y;
+    const int which = blockIdx.z, adapter = blockIdx.y, lane = threadIdx.x & 63;
     const int64_t each = a.each[which], n = each * a.adapters;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < each; i += (int64_t)gridDim.x * 256) {
+    const float *part = a.part[which] + adapter * each;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i - lane < each; i += (int64_t)gridDim.x * 256) {
+        const int64_t at = min(i, each - 1);
         float s = 0.0f;
-        for (int p = 0; p < a.splits[which]; ++p)
-            if (a.present[which][p * a.adapters + adapter]) s += a.part[which][p * n + adapter * each + i];
-        a.out[which][adapter * each + i] = s;
+        for (int p0 = 0; p0 < a.splits[which]; p0 += 64) {
+            uint64_t parts = __ballot(p0 + lane < a.splits[which] && a.present[which][(p0 + lane) * a.adapters + adapter]);
+            while (parts) {                              // four loads at a time
+                float v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[j] = parts ? part[(p0 + __builtin_ctzll(parts)) * n + at] : 0.0f;
+                    parts &= parts - 1;
+                }
+                loads_first();
+                s += (v[0] + v[1]) + (v[2] + v[3]);
+            }
+        }
+        if (i < each) a.out[which][adapter * each + i] = s;
     }
 }
 
@@ -540,8 +650,8 @@ int64_t first_chunk(int64_t K, int splits) { return ((K + splits - 1) / splits +
 // Parts of the rows for an outer product.
 int64_t outer_span(int64_t T, int64_t C, int R)
 {
-    const int64_t wgs = (C + 127) / 128 * rank_blocks(R);
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((640 + wgs - 1) / wgs, (T + 63) / 64));
+    const int64_t wgs = (C + 127) / 128 * rank_blocks(R), most = rank_tiles(R) == 4 ? 256 : 640;
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((most + wgs - 1) / wgs, (T + 63) / 64));
     return ((T + splits - 1) / splits + 63) / 64 * 64;
 }
 int outer_splits(int64_t T, int64_t C, int R) { return (int)((T + outer_span(T, C, R) - 1) / outer_span(T, C, R)); }
@@ -612,10 +722,10 @@ template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipSt
         else k_adapter_second_token<TW, TB, false><<<grid, 256, 0, stream>>>(a);
         return;
     }
-    const int64_t tiles = (a.rows + kRows - 1) / kRows, columns = (a.C + 127) / 128;
+    const int64_t tiles = (a.rows + kSecondRows - 1) / kSecondRows, columns = (a.C + 127) / 128;
     const int waves = tiles * columns < 2048 ? 1 : 4;
     a.column_tiles = (int)((columns + waves - 1) / waves);
-    const size_t lds = sizeof(float) * kRows * ((a.R + 3) / 4 * 4 + 1);
+    const size_t lds = sizeof(float) * kSecondRows * second_pitch(a.R);
     const unsigned grid = (unsigned)(tiles * a.column_tiles);
     if (vec) k_adapter_second<TW, TB, true><<<grid, 64 * waves, lds, stream>>>(a);
     else k_adapter_second<TW, TB, false><<<grid, 64 * waves, lds, stream>>>(a);

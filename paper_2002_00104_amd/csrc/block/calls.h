@@ -53,7 +53,7 @@ int check_adapter(int64_t T, int64_t K, int64_t N, int R, int adapters, int type
     if (R < 1 || R > 256) return fail(PWLQ_EINVAL, "R=%d outside [1,256]", R);
     if (adapters < 1 || adapters > 65535) return fail(PWLQ_EINVAL, "adapters=%d outside [1,65535]", adapters);
     if (!float_type(type)) return fail(PWLQ_EINVAL, "weight_type=%d is none of the float types", type);
-    if ((T + 31) / 32 * ((N > K ? N : K) / 128 + 4) * 64 > 0xffffffffLL) return fail(PWLQ_EINVAL, "grid too large");
+    if ((T + 15) / 16 * ((N > K ? N : K) / 128 + 4) * 64 > 0xffffffffLL) return fail(PWLQ_EINVAL, "grid too large");
     if (!down || !up || !scale || (T && !ids)) return fail(PWLQ_ENULL, "an input pointer is NULL");
     if (((uintptr_t)down | (uintptr_t)up) % (uintptr_t)pwlq_block::type_size(type) != 0)
         return fail(PWLQ_EINVAL, "down or up is not aligned to its elements");
