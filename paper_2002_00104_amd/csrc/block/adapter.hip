@@ -79,16 +79,20 @@ template <typename T, bool VEC> __device__ inline typename Vec8<T>::type columns
         return u.v;
     }
 }
-// The same with 0 for the columns beyond: elements of a reduction.
-template <typename T, bool VEC> __device__ inline typename Vec8<T>::type piece(const T *row, int64_t k, int64_t cols)
+// Of those eight, the ones before `end`, and 0 for the others: elements of a reduction.
+template <typename T, bool VEC> __device__ inline typename Vec8<T>::type before(typename Vec8<T>::type v, int64_t col, int64_t end)
 {
     typedef typename Vec8<T>::type V;
+    if constexpr (VEC) return col < end ? v : V(0);
     union { V v; T e[8]; } u;
-    u.v = columns8<T, VEC>(row, k, cols);
-    if constexpr (VEC) return k < cols ? u.v : V(0);
+    u.v = v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u.e[i] = k + i < cols ? u.e[i] : T(0);
+    for (int i = 0; i < 8; ++i) u.e[i] = col + i < end ? u.e[i] : T(0);
     return u.v;
+}
+template <typename T, bool VEC> __device__ inline typename Vec8<T>::type piece(const T *row, int64_t col, int64_t cols)
+{
+    return before<T, VEC>(columns8<T, VEC>(row, col, cols), col, cols);
 }
 
 struct FirstArgs {
@@ -109,13 +113,14 @@ template <typename TX> __device__ inline int half_at(int q, int half) { return s
 template <typename TX, typename TW, int RT, bool VEC>
 __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
 {
-    constexpr int kBatch = sizeof(TW) == 2 ? (RT == 1 ? 4 : 2) : (RT == 1 ? 2 : 1);
+    constexpr int kBatch = sizeof(TW) == 2 || RT == 1 ? 2 : 1;
     typedef typename Vec8<TX>::type XV;
     typedef typename Vec8<TW>::type WV;
     __shared__ float sums[4][kRows][16 * RT];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
-    const int64_t row0 = (int64_t)(blockIdx.x / a.slots) * kRows;
-    const int slot = blockIdx.x % a.slots, r0 = blockIdx.y * 16 * RT;
+    const unsigned tiles = gridDim.x / a.slots;        // slots outermost: most tiles have work in the first alone, and the chip's
+    const int64_t row0 = (int64_t)(blockIdx.x % tiles) * kRows;    // eight dies take workgroups in turn
+    const int slot = blockIdx.x / tiles, r0 = blockIdx.y * 16 * RT;
     const int64_t k0 = (int64_t)blockIdx.z * a.chunk, k1 = min(k0 + a.chunk, a.K);
     float *out = a.out + (int64_t)blockIdx.z * a.rows * a.R;
     const TX *xr[2];
@@ -142,49 +147,48 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int n = 0; n < RT; ++n) acc[m][n] = v4f(0);
-        int64_t k = k0 + 64 * wave;
-        if constexpr (VEC) {
-            for (; k + 256 * (kBatch - 1) + 64 <= k1; k += 256 * kBatch) {
-                XV x[kBatch][2][2];
-                WV w[kBatch][2][RT];
+        // steps [k, k + 256 kBatch) of this wavefront's; `whole`: all of them lie inside the part
+        auto batch = [&](int64_t k, auto whole) {
+            XV x[kBatch][2][2];
+            WV w[kBatch][2][RT];
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int64_t c = k + 256 * b + half_at<TX>(q, half);
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) x[b][half][m] = whole ? *(const XV *)(xr[m] + c) : columns8<TX, VEC>(xr[m], c, a.K);
+#pragma unroll
+                    for (int n = 0; n < RT; ++n) w[b][half][n] = whole ? *(const WV *)(wr[n] + c) : columns8<TW, VEC>(wr[n], c, a.K);
+                }
+            loads_first();
+            if constexpr (!whole) {
 #pragma unroll
                 for (int b = 0; b < kBatch; ++b)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int64_t c = k + 256 * b + half_at<TX>(q, half);
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) x[b][half][m] = *(const XV *)(xr[m] + c);
+                        for (int m = 0; m < 2; ++m) x[b][half][m] = before<TX, VEC>(x[b][half][m], c, k1);
 #pragma unroll
-                        for (int n = 0; n < RT; ++n) w[b][half][n] = *(const WV *)(wr[n] + c);
+                        for (int n = 0; n < RT; ++n) w[b][half][n] = before<TW, VEC>(w[b][half][n], c, k1);
                     }
-                loads_first();
-#pragma unroll
-                for (int b = 0; b < kBatch; ++b)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half)
-#pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            const typename Operand<TW>::type xm = operand<TW, TX>(x[b][half][m]);
-#pragma unroll
-                            for (int n = 0; n < RT; ++n) acc[m][n] = multiply(xm, w[b][half][n], acc[m][n]);
-                        }
             }
-        }
-        for (; k < k1; k += 256) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int64_t c = k + half_at<TX>(q, half);
-                typename Operand<TW>::type x[2];
+            for (int b = 0; b < kBatch; ++b)
 #pragma unroll
-                for (int m = 0; m < 2; ++m) x[m] = operand<TW, TX>(piece<TX, VEC>(xr[m], c, k1));
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int n = 0; n < RT; ++n) {
-                    const WV w = piece<TW, VEC>(wr[n], c, k1);
+                    for (int m = 0; m < 2; ++m) {
+                        const typename Operand<TW>::type xm = operand<TW, TX>(x[b][half][m]);
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) acc[m][n] = multiply(x[m], w, acc[m][n]);
-                }
-            }
-        }
+                        for (int n = 0; n < RT; ++n) acc[m][n] = multiply(xm, w[b][half][n], acc[m][n]);
+                    }
+        };
+        int64_t k = k0 + 64 * wave;
+        if constexpr (VEC)
+            for (; k + 256 * (kBatch - 1) + 64 <= k1; k += 256 * kBatch) batch(k, std::true_type());
+        for (; k < k1; k += 256 * kBatch) batch(k, std::false_type());
         __syncthreads();
 #pragma unroll
         for (int m = 0; m < 2; ++m)
@@ -204,6 +208,83 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
 }
 
 // --------------------------------------------------------------------------
+// products of H
+// --------------------------------------------------------------------------
+// The second and the outer products multiply H, which stays in binary32, with elements of a narrower type.  Sixteen reduction
+// elements of 16 rows by 128 columns: a lane holds eight neighbouring columns of each of its four elements, so a matrix
+// instruction j of eight takes everyone's column j, neither operand needs a transposition, and loads and stores are vectors.
+//   bfloat16 and codes: h is the sum of three bfloat16 (its leading, middle and last eight bits, cut off: exact), so three
+//     instructions of sixteen elements give the products of binary32 in 48 cycles a column; infinite elements come out as NaN
+//   others: four binary32 instructions of four elements, 128 cycles
+template <typename T> constexpr bool in_thirds = std::is_same<T, bf16>::value || std::is_same<T, int8_t>::value;
+// Which of the sixteen elements a lane of quarter q holds as its i-th.
+template <typename T> __device__ inline int element_of(int q, int i) { return in_thirds<T> ? 4 * q + i : 4 * i + q; }
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+struct Thirds { uint32_t w[3][2]; };   // two elements to a word
+
+__device__ inline uint32_t upper_halves(uint32_t second, uint32_t first) { return __builtin_amdgcn_perm(second, first, 0x07060302u); }
+__device__ inline uint32_t lower_halves(uint32_t second, uint32_t first) { return __builtin_amdgcn_perm(second, first, 0x05040100u); }
+// The part of h that its first eight bits leave.
+__device__ inline float rest(float h)
+{
+    const float top = __uint_as_float(__float_as_uint(h) & 0xffff0000u);
+    return top == h ? 0.0f : h - top;
+}
+__device__ inline Thirds thirds(const float (&h)[4])
+{
+    Thirds t;
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = h[i];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+        t.w[p][0] = upper_halves(__float_as_uint(v[1]), __float_as_uint(v[0]));
+        t.w[p][1] = upper_halves(__float_as_uint(v[3]), __float_as_uint(v[2]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = rest(v[i]);
+    }
+    return t;
+}
+__device__ inline v4s words(uint32_t a, uint32_t b)
+{
+    union { uint32_t w[2]; v4s v; } u = {{a, b}};
+    return u.v;
+}
+// Eight bfloat16 as four words.
+__device__ inline void as_words(v8bf v, uint32_t (&w)[4]) { __builtin_memcpy(w, &v, 16); }
+__device__ inline void as_words(v2u v, uint32_t (&w)[4])
+{
+    const v8f f = widen(v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = upper_halves(__float_as_uint(f[2 * j + 1]), __float_as_uint(f[2 * j]));
+}
+
+// y[j] += sum over the sixteen elements of h times column j of x; `h`: H of the lane's row and elements.
+template <typename T> __device__ inline void product16(const Thirds &h, const typename Vec8<T>::type (&x)[4], v4f (&y)[8])
+{
+    uint32_t w[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) as_words(x[i], w[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const v4s c = j & 1 ? words(upper_halves(w[1][j / 2], w[0][j / 2]), upper_halves(w[3][j / 2], w[2][j / 2]))
+                            : words(lower_halves(w[1][j / 2], w[0][j / 2]), lower_halves(w[3][j / 2], w[2][j / 2]));
+#pragma unroll
+        for (int p = 2; p >= 0; --p) y[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(words(h.w[p][0], h.w[p][1]), c, y[j], 0, 0, 0);
+    }
+}
+template <typename T> __device__ inline void product16(const float (&h)[4], const typename Vec8<T>::type (&x)[4], v4f (&y)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const v8f c = widen(x[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[i], c[j], y[j], 0, 0, 0);
+    }
+}
+
+// --------------------------------------------------------------------------
 // second product
 // --------------------------------------------------------------------------
 struct SecondArgs {
@@ -214,12 +295,13 @@ struct SecondArgs {
     int64_t base_stride, out_stride, rows, C;
     const float *base_step;
     const int32_t *ids;
-    int R, splits, adapters, out_type, column_tiles;
+    bool has_base;                     // else base is memory that can be read as a row of C elements, its stride 0
+    int R, splits, adapters, out_type, walks;     // walks: workgroups that share the columns of a tile of rows
 };
 
-// A wavefront does 16 rows by 128 columns, with binary32 matrix instructions: H stays in binary32, and a lane's eight
-// neighbouring columns are eight instructions, so neither W nor Y needs a transposition and both move in vectors.  The ranks
-// come sixteen at a time, their products added to the row's sum where the row has the adapter.
+// A wavefront does 16 rows by 128 columns.  The ranks come sixteen at a time, their products added to the row's sum where the
+// row has the adapter.  A workgroup walks along its
+// rows, H in LDS; the next tile's base and W are on their way while one is computed and stored.
 constexpr int kSecondRows = 16;
 __host__ __device__ inline int second_pitch(int R) { return (R + 15) / 16 * 16 + 1; }
 
@@ -241,40 +323,39 @@ __global__ __launch_bounds__(256) void k_adapter_second(SecondArgs a)
     typedef typename Vec8<TW>::type WV;
     typedef typename Vec8<TB>::type BV;
     extern __shared__ float hs[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
-    const int64_t row0 = (int64_t)(blockIdx.x / a.column_tiles) * kSecondRows;
-    const int tile = blockIdx.x % a.column_tiles, pitch = second_pitch(a.R);
-    const int64_t col = ((int64_t)tile * (blockDim.x / 64) + wave) * 128 + 8 * l;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x / 64, l = lane & 15, q = lane >> 4;
+    const int64_t row0 = (int64_t)(blockIdx.x / a.walks) * kSecondRows;
+    const int walk = blockIdx.x % a.walks, pitch = second_pitch(a.R);
+    int64_t tile = walk * waves + wave;                // of 128 columns
+    const int64_t tiles = (a.C + 127) / 128, stride = (int64_t)a.walks * waves;
 
-    const int id = Adapters::load(a.ids, row0, a.rows);
-    BV base[4];
-    if (a.base) {
+    // what a tile needs from memory: base, and the first adapter's first ranks (0 beyond R)
+    auto load_base = [&](int64_t col, BV (&v)[4]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            base[i] = columns8<TB, VEC>((const TB *)a.base + clamp_row(row0 + 4 * q + i, a.rows) * a.base_stride, col, a.C);
-    } else {
+            v[i] = columns8<TB, VEC>((const TB *)a.base + clamp_row(row0 + 4 * q + i, a.rows) * a.base_stride, col, a.C);
+    };
+    auto load_ranks = [&](int adapter, int r0, int64_t col, WV (&v)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) base[i] = BV(0);
-    }
+        for (int i = 0; i < 4; ++i)
+            v[i] = columns8<TW, VEC>((const TW *)a.w + ((int64_t)adapter * a.R + min(r0 + element_of<TW>(q, i), a.R - 1)) * a.C, col, a.C);
+    };
+    const int id = Adapters::load(a.ids, row0, a.rows);
     float factor[4];                                   // without factors any number that can be read
     const float *from = a.base_step ? a.base_step : a.h;
 #pragma unroll
     for (int i = 0; i < 4; ++i) factor[i] = from[a.base_step ? clamp_row(row0 + 4 * q + i, a.rows) : 0];
+    BV base[4];
+    load_base(128 * tile + 8 * l, base);
     loads_first();
-    Adapters of(id, row0, a.rows, a.adapters, kSecondRows);
-    // the ranks r0 to r0 + 15 of one adapter's W, those beyond R 0
-    auto ranks = [&](int adapter, int r0, WV (&v)[4]) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-            v[s] = columns8<TW, VEC>((const TW *)a.w + ((int64_t)adapter * a.R + min(r0 + 4 * s + q, a.R - 1)) * a.C, col, a.C);
-#pragma unroll
-        for (int s = 0; s < 4; ++s) v[s] = r0 + 4 * s + q < a.R ? v[s] : WV(0);
-    };
+    const Adapters all(id, row0, a.rows, a.adapters, kSecondRows);
+    Adapters of = all;
     int adapter = 0;
     uint64_t mine = 0;
-    bool more = of.next(adapter, mine);
+    of.next(adapter, mine);
+    const int first_adapter = adapter;
     WV w[4];
-    ranks(adapter, 0, w);
+    load_ranks(adapter, 0, 128 * tile + 8 * l, w);
 
     for (int row = threadIdx.x >> 4; row < kSecondRows; row += blockDim.x >> 4)
         for (int r = l; r < pitch - 1; r += 16) {
@@ -289,55 +370,57 @@ __global__ __launch_bounds__(256) void k_adapter_second(SecondArgs a)
                 for (int j = 0; j < 4; ++j) s += p + j < a.splits ? v[j] : 0.0f;
             }
             if (r >= a.R) s = 0.0f;
-            else if (tile == 0 && a.h_out && row0 + row < a.rows) a.h_out[at] = s;
+            else if (walk == 0 && a.h_out && row0 + row < a.rows) a.h_out[at] = s;
             hs[row * pitch + r] = s;
         }
     __syncthreads();
-    v8f acc[4];
+    for (; tile < tiles; tile += stride) {
+        const int64_t col = 128 * tile + 8 * l;
+        v8f acc[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = widen(base[i]);
-    if (a.base_step) {
+        for (int i = 0; i < 4; ++i) acc[i] = a.has_base ? widen(base[i]) * (a.base_step ? factor[i] : 1.0f) : v8f(0);
+        load_base(col + 128 * stride, base);               // of the next tile (of the last columns after the last one)
+        of = all;
+        bool more = of.next(adapter, mine);
+        int r0 = 0;
+        while (more) {
+            WV now[4];
+            float h[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] *= factor[i];
-    }
-    int r0 = 0;
-    while (more) {
-        v8f wv[4];
-        float h[4];
+            for (int i = 0; i < 4; ++i) {
+                const int r = r0 + element_of<TW>(q, i);
+                now[i] = r < a.R ? w[i] : WV(0);
+                h[i] = hs[l * pitch + r];
+            }
+            const uint64_t rows = mine;
+            r0 += 16;
+            if (r0 >= a.R) {
+                r0 = 0;
+                more = of.next(adapter, mine);
+            }
+            load_ranks(more ? adapter : first_adapter, r0, more ? col : col + 128 * stride, w);
+            loads_first();
+            v4f y[8];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            wv[s] = widen(w[s]);
-            h[s] = hs[l * pitch + r0 + 4 * s + q];
+            for (int j = 0; j < 8; ++j) y[j] = v4f(0);
+            if constexpr (in_thirds<TW>) product16<TW>(thirds(h), now, y);
+            else product16<TW>(h, now, y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool own = (rows >> (4 * q + i)) & 1;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[i][j] += own ? y[j][i] : 0.0f;
+            }
         }
-        const uint64_t rows = mine;
-        r0 += 16;
-        if (r0 >= a.R) {
-            r0 = 0;
-            more = of.next(adapter, mine);
+        if (a.out_type == PWLQ_F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (row0 + 4 * q + i < a.rows) store_columns<float>(a.out, (row0 + 4 * q + i) * a.out_stride, col, a.C, acc[i], VEC);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (row0 + 4 * q + i < a.rows) store_columns<TW>(a.out, (row0 + 4 * q + i) * a.out_stride, col, a.C, acc[i], VEC);
         }
-        if (more) ranks(adapter, r0, w);
-        v4f y[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = v4f(0);
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[s], wv[s][j], y[j], 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool own = (rows >> (4 * q + i)) & 1;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[i][j] += own ? y[j][i] : 0.0f;
-        }
-    }
-    if (a.out_type == PWLQ_F32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (row0 + 4 * q + i < a.rows) store_columns<float>(a.out, (row0 + 4 * q + i) * a.out_stride, col, a.C, acc[i], VEC);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (row0 + 4 * q + i < a.rows) store_columns<TW>(a.out, (row0 + 4 * q + i) * a.out_stride, col, a.C, acc[i], VEC);
     }
 }
 
@@ -373,7 +456,7 @@ __global__ __launch_bounds__(256) void k_adapter_second_token(SecondArgs a)
     const int64_t row = blockIdx.y, col = (int64_t)blockIdx.x * 512 + 8 * lane;
     const int id = a.ids[row];
     v8f y = v8f(0), base = v8f(0);
-    if (a.base && wave == 0) base = widen(piece<TB, VEC>((const TB *)a.base + row * a.base_stride, col, a.C));
+    if (a.has_base && wave == 0) base = widen(piece<TB, VEC>((const TB *)a.base + row * a.base_stride, col, a.C));
     if (id >= 0 && id < a.adapters) {
         const TW *w = (const TW *)a.w + (int64_t)id * a.R * a.C;
 #pragma unroll 4
@@ -475,128 +558,180 @@ __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
 struct OuterArgs {
     const float *h;                    // [rows, R]
     const void *x;
-    int64_t stride, rows, C, span;     // span: rows of a workgroup, a multiple of 64
+    int64_t stride, rows, C, span;     // span: rows of a workgroup
     const float *step;
     const int32_t *ids;
-    int R, adapters, column_tiles, splits;
+    int R, adapters, column_tiles, rank_blocks;
     float *out;                        // [splits, adapters, R, C]
     int32_t *present;                  // [splits, adapters]: whether the part has rows of the adapter; NULL where there is one part
+    bool flags;                        // whether this product writes them: both have the same rows
 };
 
-// 16 RT ranks by 128 columns of one adapter's gradient, over a part of the rows.  The rows of the adapter are listed in LDS
-// first, 512 at a time, so that no other row is read.  As in the second product a lane's eight neighbouring columns are eight
-// binary32 matrix instructions; a step is four rows, and a wavefront has several steps' loads in flight.
+// 16 RT ranks by 128 columns of the adapters' gradients, over a part of the rows: for each adapter that has some of them, one
+// after the other.  Its rows are listed in LDS first, 512 at a time, so that no other row is read; the four wavefronts take
+// sixteen of them each in turn, the next ones' loads under way, and add up in LDS.
 constexpr int kListed = 512;
 
-template <typename TX, int RT, bool VEC>
-__global__ __launch_bounds__(256) void k_adapter_outer(OuterArgs a)
+template <int RT> struct OuterLds {
+    v4f sums[2][RT * 8][64];
+    int list[kListed];
+};
+
+template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const OuterArgs &a, int tile, int split, OuterLds<RT> &lds)
 {
-    constexpr int kSteps = RT == 4 ? 4 : 8;
-    __shared__ v4f sums[2][RT * 8][64];
-    __shared__ int list[kListed];
+    constexpr int kUnits = RT == 4 ? 1 : 2;            // of sixteen rows, under way at once
+    typedef typename Vec8<TX>::type XV;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
-    const int64_t col = (int64_t)(blockIdx.x % a.column_tiles) * 128 + 8 * l;
-    const int r0 = blockIdx.x / a.column_tiles * 16 * RT, adapter = blockIdx.y, split = blockIdx.z;
+    const int64_t col = (int64_t)(tile % a.column_tiles) * 128 + 8 * l;
+    const int r0 = tile / a.column_tiles * 16 * RT;
     const int64_t t0 = split * a.span, t1 = min(t0 + a.span, a.rows);
+    struct Rows {
+        XV x[kUnits][4];
+        float h[kUnits][4][RT], step[kUnits][4];
+    };
+    float *const part = a.out + (int64_t)split * a.adapters * a.R * a.C;
+    int32_t *const present = a.present && a.flags && tile == 0 ? a.present + (int64_t)split * a.adapters : nullptr;
+    if (present)
+        for (int i = threadIdx.x; i < a.adapters; i += 256) present[i] = 0;
     v4f acc[RT][8];
+    for (int adapter = -1, next;; adapter = next) {
+        next = a.adapters;
 #pragma unroll
-    for (int n = 0; n < RT; ++n)
+        for (int n = 0; n < RT; ++n)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[n][j] = v4f(0);
-    bool any = false;
-    for (int64_t t = t0; t < t1; t += kListed) {
-        int id[kListed / 64];
+            for (int j = 0; j < 8; ++j) acc[n][j] = v4f(0);
+        for (int64_t t = t0; t < t1; t += kListed) {
+            int id[kListed / 64];
 #pragma unroll
-        for (int g = 0; g < kListed / 64; ++g) id[g] = a.ids[clamp_row(t + 64 * g + lane, t1)];
-        loads_first();
-        int count = 0;
-        __syncthreads();
-#pragma unroll
-        for (int g = 0; g < kListed / 64; ++g) {
-            const uint64_t mine = __ballot(id[g] == adapter && t + 64 * g + lane < t1);
-            if (g % 4 == wave && ((mine >> lane) & 1)) list[count + __builtin_popcountll(mine & ((1ull << lane) - 1))] = 64 * g + lane;
-            count += __builtin_popcountll(mine);
-        }
-        __syncthreads();
-        any |= count != 0;
-        for (int first = 4 * kSteps * wave; first < count; first += 16 * kSteps) {
-            typename Vec8<TX>::type x[kSteps];
-            float h[kSteps][RT], step[kSteps];
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const int64_t row = t + list[min(first + 4 * s + q, count - 1)];
-                x[s] = columns8<TX, VEC>((const TX *)a.x + row * a.stride, col, a.C);
-#pragma unroll
-                for (int n = 0; n < RT; ++n) h[s][n] = a.h[row * a.R + min(r0 + 16 * n + l, a.R - 1)];
-                if constexpr (sizeof(TX) == 1) step[s] = a.step[row];
-            }
+            for (int g = 0; g < kListed / 64; ++g) id[g] = a.ids[clamp_row(t + 64 * g + lane, t1)];
             loads_first();
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const bool own = first + 4 * s + q < count;
-                v8f xv = widen(x[s]);
-                if (!own) xv = v8f(0);
+            for (int g = 0; g < kListed / 64; ++g)
+                if (id[g] > adapter) next = min(next, id[g]);
+            if (adapter < 0) continue;
+            int count = 0;
+            __syncthreads();
 #pragma unroll
-                for (int n = 0; n < RT; ++n) {
-                    float hv = h[s][n];
-                    if constexpr (sizeof(TX) == 1) hv *= step[s];
-                    hv = own ? hv : 0.0f;
+            for (int g = 0; g < kListed / 64; ++g) {
+                const uint64_t mine = __ballot(id[g] == adapter && t + 64 * g + lane < t1);
+                if (g % 4 == wave && ((mine >> lane) & 1)) lds.list[count + __builtin_popcountll(mine & ((1ull << lane) - 1))] = 64 * g + lane;
+                count += __builtin_popcountll(mine);
+            }
+            __syncthreads();
+            auto load = [&](int first, Rows &v) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(hv, xv[j], acc[n][j], 0, 0, 0);
+                for (int u = 0; u < kUnits; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t row = t + lds.list[min(first + 16 * u + element_of<TX>(q, i), count - 1)];
+                        v.x[u][i] = columns8<TX, VEC>((const TX *)a.x + row * a.stride, col, a.C);
+#pragma unroll
+                        for (int n = 0; n < RT; ++n) v.h[u][i][n] = a.h[row * a.R + min(r0 + 16 * n + l, a.R - 1)];
+                        if constexpr (sizeof(TX) == 1) v.step[u][i] = a.step[row];
+                    }
+            };
+            int first = 16 * kUnits * wave;
+            if (first >= count) continue;
+            Rows now, after;
+            load(first, now);
+            for (; first < count; first += 64 * kUnits, now = after) {
+                load(first + 64 * kUnits, after);          // beyond the list: its last row, not used
+                loads_first();
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u) {
+                    bool own[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        own[i] = first + 16 * u + element_of<TX>(q, i) < count;
+                        now.x[u][i] = own[i] ? now.x[u][i] : XV(0);
+                    }
+#pragma unroll
+                    for (int n = 0; n < RT; ++n) {
+                        float h[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            h[i] = now.h[u][i][n];
+                            if constexpr (sizeof(TX) == 1) h[i] *= now.step[u][i];
+                            h[i] = own[i] ? h[i] : 0.0f;
+                        }
+                        if constexpr (in_thirds<TX>) product16<TX>(thirds(h), now.x[u], acc[n]);
+                        else product16<TX>(h, now.x[u], acc[n]);
+                    }
                 }
             }
         }
-    }
-    if (a.present) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) a.present[split * a.adapters + adapter] = any;
-        if (!any) return;
-    }
-    if (wave >= 2) {
 #pragma unroll
-        for (int n = 0; n < RT; ++n)
+        for (int d = 32; d; d >>= 1) next = min(next, __shfl_xor(next, d));
+        next = __builtin_amdgcn_readfirstlane(next);
+        // adapters without rows here: nothing in a part, zeros where there are no parts
+        if (!a.present)
+            for (int none = adapter + 1; none < next; ++none)
+                for (int i = threadIdx.x; i < 16 * RT * 128; i += 256) {
+                    const int r = r0 + i / 128;
+                    const int64_t c = (int64_t)(tile % a.column_tiles) * 128 + i % 128;
+                    if (r < a.R && c < a.C) part[((int64_t)none * a.R + r) * a.C + c] = 0.0f;
+                }
+        if (adapter >= 0) {
+            if (present && (int)threadIdx.x == adapter % 256) present[adapter] = 1;
+            if (wave >= 2) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sums[wave - 2][8 * n + j][lane] = acc[n][j];
-    }
-    __syncthreads();
-    if (wave < 2) {
+                for (int n = 0; n < RT; ++n)
 #pragma unroll
-        for (int n = 0; n < RT; ++n)
+                    for (int j = 0; j < 8; ++j) lds.sums[wave - 2][8 * n + j][lane] = acc[n][j];
+            }
+            __syncthreads();
+            if (wave < 2) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[n][j] += sums[wave][8 * n + j][lane];
-    }
-    __syncthreads();
-    if (wave == 1) {
+                for (int n = 0; n < RT; ++n)
 #pragma unroll
-        for (int n = 0; n < RT; ++n)
+                    for (int j = 0; j < 8; ++j) acc[n][j] += lds.sums[wave][8 * n + j][lane];
+            }
+            __syncthreads();
+            if (wave == 1) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sums[0][8 * n + j][lane] = acc[n][j];
-    }
-    __syncthreads();
-    if (wave) return;
-    float *out = a.out + ((int64_t)split * a.adapters + adapter) * a.R * a.C;
+                for (int n = 0; n < RT; ++n)
 #pragma unroll
-    for (int n = 0; n < RT; ++n) {
+                    for (int j = 0; j < 8; ++j) lds.sums[0][8 * n + j][lane] = acc[n][j];
+            }
+            __syncthreads();
+            if (wave == 0) {
+                float *out = part + (int64_t)adapter * a.R * a.C;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[n][j] += sums[0][8 * n + j][lane];
+                for (int n = 0; n < RT; ++n) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = r0 + 16 * n + 4 * q + i;
-            v8f v;
+                    for (int j = 0; j < 8; ++j) acc[n][j] += lds.sums[0][8 * n + j][lane];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = acc[n][j][i];
-            if (r < a.R) store_columns<float>(out, (int64_t)r * a.C, col, a.C, v, VEC);
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = r0 + 16 * n + 4 * q + i;
+                        v8f v;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] = acc[n][j][i];
+                        if (r < a.R) store_columns<float>(out, (int64_t)r * a.C, col, a.C, v, VEC);
+                    }
+                }
+            }
         }
+        if (next >= a.adapters) return;
     }
 }
 
-// Parts of one or two gradients added up in order.
+// Both gradients in one launch: the second fills the chip while the first one's last workgroups end.
+template <typename TX, typename TY, int RT, bool VEC>
+__global__ __launch_bounds__(256) void k_adapter_outer(OuterArgs up, OuterArgs down)
+{
+    __shared__ OuterLds<RT> lds;
+    const int ups = up.column_tiles * up.rank_blocks;
+    if ((int)blockIdx.x < ups) outer_tile<TY, RT, VEC>(up, blockIdx.x, blockIdx.y, lds);
+    else outer_tile<TX, RT, VEC>(down, blockIdx.x - ups, blockIdx.y, lds);
+}
+
+// Parts of both gradients added up in order.
 struct JoinArgs {
     const float *part[2];
-    const int32_t *present[2];
+    const int32_t *present;
     float *out[2];
     int64_t each[2];                   // R C
-    int splits[2];
-    int adapters;
+    int splits, adapters;
 };
 __global__ __launch_bounds__(256) void k_adapter_join(JoinArgs a)
 {
@@ -606,8 +741,8 @@ __global__ __launch_bounds__(256) void k_adapter_join(JoinArgs a)
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i - lane < each; i += (int64_t)gridDim.x * 256) {
         const int64_t at = min(i, each - 1);
         float s = 0.0f;
-        for (int p0 = 0; p0 < a.splits[which]; p0 += 64) {
-            uint64_t parts = __ballot(p0 + lane < a.splits[which] && a.present[which][(p0 + lane) * a.adapters + adapter]);
+        for (int p0 = 0; p0 < a.splits; p0 += 64) {
+            uint64_t parts = __ballot(p0 + lane < a.splits && a.present[(p0 + lane) * a.adapters + adapter]);
             while (parts) {                              // four loads at a time
                 float v[4];
 #pragma unroll
@@ -638,23 +773,27 @@ constexpr int64_t kTokenRows = 16;     // up to so many rows each is done by its
 int rank_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }
 int rank_blocks(int R) { return (R + 16 * rank_tiles(R) - 1) / (16 * rank_tiles(R)); }
 
-// Parts of the first product's reduction: workgroups for the whole chip, with two steps for each wavefront at least.
+// Parts of the first product's reduction: workgroups for the whole chip, each with a batch of steps for its wavefronts at least.
 int first_splits(int64_t T, int64_t K, int R)
 {
     if (T <= kTokenRows) return 1;
     const int64_t wgs = (T + kRows - 1) / kRows * rank_blocks(R);
-    return (int)std::max<int64_t>(1, std::min<int64_t>((640 + wgs - 1) / wgs, (K + 511) / 512));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(1024 / wgs, (K + 511) / 512));
 }
-int64_t first_chunk(int64_t K, int splits) { return ((K + splits - 1) / splits + 63) / 64 * 64; }
+int64_t first_chunk(int64_t K, int splits) { return ((K + splits - 1) / splits + 255) / 256 * 256; }
 
-// Parts of the rows for an outer product.
-int64_t outer_span(int64_t T, int64_t C, int R)
+// Parts of the rows for the outer products: a workgroup or two to each CU.
+int64_t outer_span(int64_t T, int64_t K, int64_t N, int R)
 {
-    const int64_t wgs = (C + 127) / 128 * rank_blocks(R), most = rank_tiles(R) == 4 ? 256 : 640;
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((most + wgs - 1) / wgs, (T + 63) / 64));
+    const int64_t wgs = ((K + 127) / 128 + (N + 127) / 128) * rank_blocks(R), most = rank_tiles(R) == 4 ? 256 : 512;
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(most / wgs, (T + 63) / 64));
     return ((T + splits - 1) / splits + 63) / 64 * 64;
 }
-int outer_splits(int64_t T, int64_t C, int R) { return (int)((T + outer_span(T, C, R) - 1) / outer_span(T, C, R)); }
+int outer_splits(int64_t T, int64_t K, int64_t N, int R)
+{
+    const int64_t span = outer_span(T, K, N, R);
+    return (int)((T + span - 1) / span);
+}
 
 struct Carver {                        // offsets of a workspace's parts, 256-byte aligned
     char *base;
@@ -668,19 +807,21 @@ struct Carver {                        // offsets of a workspace's parts, 256-by
 };
 
 struct BackwardSpace {
-    float *dh, *parts, *down, *up;
-    int32_t *has_down, *has_up;
+    float *dh, *parts, *down, *up;     // down, up: parts of the gradients; NULL where there is one part
+    int32_t *present;
+    int splits;
     size_t bytes;
     BackwardSpace(void *workspace, int64_t T, int64_t K, int64_t N, int R, int adapters)
     {
         Carver c = {(char *)workspace};
-        const int splits = first_splits(T, N, R), sd = outer_splits(T, K, R), su = outer_splits(T, N, R);
+        const int first = first_splits(T, N, R);
+        splits = outer_splits(T, K, N, R);
         dh = c.take<float>(T * R);
-        parts = splits > 1 ? c.take<float>(splits * T * R) : dh;
-        down = sd > 1 ? c.take<float>((int64_t)sd * adapters * R * K) : nullptr;
-        up = su > 1 ? c.take<float>((int64_t)su * adapters * R * N) : nullptr;
-        has_down = c.take<int32_t>((int64_t)sd * adapters);
-        has_up = c.take<int32_t>((int64_t)su * adapters);
+        parts = first > 1 ? c.take<float>(first * T * R) : dh;
+        const int64_t all = splits > 1 ? (int64_t)splits * adapters : 0;
+        down = c.take<float>(all * R * K);
+        up = c.take<float>(all * R * N);
+        present = c.take<int32_t>(all);
         bytes = c.at;
     }
 };
@@ -714,6 +855,8 @@ void first(const FirstArgs &a, int x_type, int w_type, bool vec, hipStream_t str
     else x_type == PWLQ_I8 ? first_as<int8_t, f16>(a, vec, stream) : first_as<f16, f16>(a, vec, stream);
 }
 
+constexpr int64_t kSecondWgs = 512;    // that walk at once
+
 template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipStream_t stream)
 {
     if (a.rows <= kTokenRows && a.splits == 1) {
@@ -724,57 +867,45 @@ template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipSt
     }
     const int64_t tiles = (a.rows + kSecondRows - 1) / kSecondRows, columns = (a.C + 127) / 128;
     const int waves = tiles * columns < 2048 ? 1 : 4;
-    a.column_tiles = (int)((columns + waves - 1) / waves);
+    a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, waves == 1 ? columns : (kSecondWgs + tiles - 1) / tiles);
     const size_t lds = sizeof(float) * kSecondRows * second_pitch(a.R);
-    const unsigned grid = (unsigned)(tiles * a.column_tiles);
+    const unsigned grid = (unsigned)(tiles * a.walks);
     if (vec) k_adapter_second<TW, TB, true><<<grid, 64 * waves, lds, stream>>>(a);
     else k_adapter_second<TW, TB, false><<<grid, 64 * waves, lds, stream>>>(a);
 }
 
-void second(const SecondArgs &a, int w_type, int base_type, bool vec, hipStream_t stream)
+void second(SecondArgs a, int w_type, int base_type, bool vec, hipStream_t stream)
 {
+    a.has_base = a.base != nullptr;
+    if (!a.base) {
+        a.base = a.w;
+        a.base_stride = 0;
+        base_type = w_type;
+    }
     if (w_type == PWLQ_F32) second_as<float, float>(a, vec, stream);
     else if (w_type == PWLQ_BF16) base_type == PWLQ_F32 ? second_as<bf16, float>(a, vec, stream) : second_as<bf16, bf16>(a, vec, stream);
     else base_type == PWLQ_F32 ? second_as<f16, float>(a, vec, stream) : second_as<f16, f16>(a, vec, stream);
 }
 
-template <typename TX> void outer_as(const OuterArgs &a, bool vec, hipStream_t stream)
+template <typename TX, typename TY> void outer_as(const OuterArgs &up, const OuterArgs &down, int splits, bool vec, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.column_tiles * rank_blocks(a.R)), a.adapters, a.splits);
+    const dim3 grid((unsigned)(up.column_tiles * up.rank_blocks + down.column_tiles * down.rank_blocks), splits);
 #define PWLQ_OUTER(RT)                                                                          \
     do {                                                                                        \
-        if (vec) k_adapter_outer<TX, RT, true><<<grid, 256, 0, stream>>>(a);                    \
-        else k_adapter_outer<TX, RT, false><<<grid, 256, 0, stream>>>(a);                       \
+        if (vec) k_adapter_outer<TX, TY, RT, true><<<grid, 256, 0, stream>>>(up, down);         \
+        else k_adapter_outer<TX, TY, RT, false><<<grid, 256, 0, stream>>>(up, down);            \
     } while (0)
-    if (rank_tiles(a.R) == 1) PWLQ_OUTER(1);
-    else if (rank_tiles(a.R) == 2) PWLQ_OUTER(2);
+    if (rank_tiles(up.R) == 1) PWLQ_OUTER(1);
+    else if (rank_tiles(up.R) == 2) PWLQ_OUTER(2);
     else PWLQ_OUTER(4);
 #undef PWLQ_OUTER
 }
 
-void outer(const pwlq_rows &x, int64_t T, int64_t C, int R, int adapters, const float *h, const int32_t *ids, float *out, float *parts,
-           int32_t *present, hipStream_t stream)
+void outer(const OuterArgs &up, const OuterArgs &down, int splits, int x_type, int w_type, bool vec, hipStream_t stream)
 {
-    OuterArgs a = {};
-    a.h = h;
-    a.x = x.data;
-    a.stride = x.stride;
-    a.rows = T;
-    a.C = C;
-    a.span = outer_span(T, C, R);
-    a.splits = outer_splits(T, C, R);
-    a.step = x.step;
-    a.ids = ids;
-    a.R = R;
-    a.adapters = adapters;
-    a.column_tiles = (int)((C + 127) / 128);
-    a.out = a.splits > 1 ? parts : out;
-    a.present = a.splits > 1 ? present : nullptr;
-    const bool vec = C % 8 == 0 && vectors(x, T) && aligned16(a.out);
-    if (x.type == PWLQ_F32) outer_as<float>(a, vec, stream);
-    else if (x.type == PWLQ_BF16) outer_as<bf16>(a, vec, stream);
-    else if (x.type == PWLQ_F16) outer_as<f16>(a, vec, stream);
-    else outer_as<int8_t>(a, vec, stream);
+    if (w_type == PWLQ_F32) x_type == PWLQ_I8 ? outer_as<int8_t, float>(up, down, splits, vec, stream) : outer_as<float, float>(up, down, splits, vec, stream);
+    else if (w_type == PWLQ_BF16) x_type == PWLQ_I8 ? outer_as<int8_t, bf16>(up, down, splits, vec, stream) : outer_as<bf16, bf16>(up, down, splits, vec, stream);
+    else x_type == PWLQ_I8 ? outer_as<int8_t, f16>(up, down, splits, vec, stream) : outer_as<f16, f16>(up, down, splits, vec, stream);
 }
 
 bool whole_vectors(int64_t C, const void *w) { return C % 8 == 0 && aligned16(w); }
@@ -866,7 +997,7 @@ void adapter_forward(const pwlq_adapter_args &a, void *workspace, hipStream_t st
     s.splits = parts;
     s.adapters = a.adapters;
     s.out_type = a.out.type;
-    second(s, a.weight_type, a.base.data ? a.base.type : PWLQ_F32, whole_vectors(a.N, a.up) && vectors(a.base, a.T) && vectors(a.out, a.T), stream);
+    second(s, a.weight_type, a.base.type, whole_vectors(a.N, a.up) && vectors(a.base, a.T) && vectors(a.out, a.T), stream);
 }
 
 size_t adapter_backward_workspace(int64_t T, int64_t K, int64_t N, int R, int adapters)
@@ -910,29 +1041,47 @@ void adapter_backward(const pwlq_adapter_backward_args &a, void *workspace, hipS
     s.splits = parts;
     s.adapters = a.adapters;
     s.out_type = a.dx.type;
-    second(s, a.weight_type, a.dx_base.data ? a.dx_base.type : PWLQ_F32,
+    second(s, a.weight_type, a.dx_base.type,
            whole_vectors(a.K, a.down) && vectors(a.dx_base, a.T) && vectors(a.dx, a.T), stream);
-    outer(a.x, a.T, a.K, a.R, a.adapters, space.dh, a.ids, a.d_down, space.down, space.has_down, stream);
-    outer(a.dy, a.T, a.N, a.R, a.adapters, a.h, a.ids, a.d_up, space.up, space.has_up, stream);
+    OuterArgs up = {}, down = {};
+    up.rows = down.rows = a.T;
+    up.span = down.span = outer_span(a.T, a.K, a.N, a.R);
+    up.ids = down.ids = a.ids;
+    up.R = down.R = a.R;
+    up.adapters = down.adapters = a.adapters;
+    up.rank_blocks = down.rank_blocks = rank_blocks(a.R);
+    up.h = a.h;
+    up.x = a.dy.data;
+    up.stride = a.dy.stride;
+    up.C = a.N;
+    up.column_tiles = (int)((a.N + 127) / 128);
+    down.h = space.dh;
+    down.x = a.x.data;
+    down.stride = a.x.stride;
+    down.step = a.x.step;
+    down.C = a.K;
+    down.column_tiles = (int)((a.K + 127) / 128);
+    const bool join = space.splits > 1;
+    up.out = join ? space.up : a.d_up;
+    down.out = join ? space.down : a.d_down;
+    up.present = down.present = join ? space.present : nullptr;
+    up.flags = true;
+    outer(up, down, space.splits, a.x.type, a.weight_type,
+          whole_vectors(a.N, up.out) && whole_vectors(a.K, down.out) && vectors(a.x, a.T) && vectors(a.dy, a.T), stream);
+    if (!join) return;
     JoinArgs j = {};
-    int n = 0;
-    auto join = [&](const float *part, const int32_t *present, float *out, int64_t C) {
-        const int splits = outer_splits(a.T, C, a.R);
-        if (splits == 1) return;
-        j.part[n] = part;
-        j.present[n] = present;
-        j.out[n] = out;
-        j.each[n] = a.R * C;
-        j.splits[n++] = splits;
-    };
-    join(space.down, space.has_down, a.d_down, a.K);
-    join(space.up, space.has_up, a.d_up, a.N);
+    j.part[0] = space.down;
+    j.part[1] = space.up;
+    j.present = space.present;
+    j.out[0] = a.d_down;
+    j.out[1] = a.d_up;
+    j.each[0] = a.R * a.K;
+    j.each[1] = a.R * a.N;
+    j.splits = space.splits;
     j.adapters = a.adapters;
-    if (n) {
-        const int64_t most = std::max(j.each[0], j.each[1]);
-        const dim3 grid((unsigned)std::min<int64_t>((most + 255) / 256, 1 << 16), a.adapters, n);
-        k_adapter_join<<<grid, 256, 0, stream>>>(j);
-    }
+    const int64_t most = std::max(j.each[0], j.each[1]);
+    const dim3 grid((unsigned)std::min<int64_t>((most + 255) / 256, 1 << 16), a.adapters, 2);
+    k_adapter_join<<<grid, 256, 0, stream>>>(j);
 }
 
 } // namespace pwlq_block
