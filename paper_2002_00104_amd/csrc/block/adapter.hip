@@ -19,10 +19,6 @@ namespace {
 
 constexpr int kRows = 32;              // rows of a tile of the first product: two of the matrix instructions'
 
-// Nothing is moved across: the loads above it are issued before what uses them.  The compiler would otherwise put each beside its use,
-// which saves registers and waits for memory once per load.
-__device__ inline void loads_first() { __builtin_amdgcn_sched_barrier(0); }
-
 __device__ inline int64_t clamp_row(int64_t row, int64_t rows) { return row < rows ? row : rows - 1; }
 
 // The adapters of a tile's rows, one after the other, and the rows that each has.

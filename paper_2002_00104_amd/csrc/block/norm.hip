@@ -7,6 +7,8 @@
 //   dv   = alpha gate dx,                           d_gate = sum over its rows of alpha v dx
 //   df   = a (post dv - fh mean(post dv fh)),       d_post = sum over rows of dv fh
 // All of it is bound by memory: a workgroup holds a row in registers and reads each of its values once.
+#include <algorithm>
+
 #include "launch.h"
 #include "rows.h"
 
@@ -15,55 +17,71 @@
 namespace pwlq_block {
 namespace {
 
+// Wavefronts that walk the rows at once, as many as are resident: sixteen to a CU, and for the backward pass, which keeps more
+// of a row and the columns' sums in registers, eight.
+constexpr int64_t kForwardWaves = 256 * 16, kBackwardWaves = 256 * 8;
+
 inline int threads_for(int64_t cols, int E) { return (int)((cols + 64 * E - 1) / (64 * E) * 64); }
 
-template <typename TF, typename TX, int E, bool VEC>
-__global__ __launch_bounds__(1024) void k_norm_block(pwlq_norm_args a)
+template <typename TF, typename TX, int E, bool VEC, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_norm_block(pwlq_norm_args a)
 {
     __shared__ float slots[2][2][16];
     __shared__ uint32_t top[2][16];
     const int threads = blockDim.x, thread = threadIdx.x, D = (int)a.D;
     const float inv = 1.0f / (float)D;
     const int64_t per_gate = a.gate ? a.T / a.gate_rows : 1;
+    Row<float, E, VEC> pre, post;
+    Row<TF, E, VEC> f, gate;
+    Row<TX, E, VEC> x;
+    pre.load(a.pre_weight, D, threads, thread);
+    if (a.post_weight) post.load(a.post_weight, D, threads, thread);
+    auto load = [&](int64_t row) {
+        x.load((const TX *)a.x.data + row * a.x.stride, D, threads, thread);
+        if (a.f.data) f.load((const TF *)a.f.data + row * a.f.stride, D, threads, thread);
+        if (a.gate) gate.load((const TF *)a.gate + row / per_gate * a.D, D, threads, thread);
+    };
+    load(blockIdx.x);
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1) {
-        float x[E], w[E];
-        load_row<TX, E, VEC>((const TX *)a.x.data + row * a.x.stride, D, threads, thread, x);
+        float v[E], g[E], w[E];
+        x.get(v);
+        if (a.f.data) f.get(g);
+        if (a.gate) gate.get(w);
+        load(min(row + gridDim.x, a.T - 1));           // the next row, while this one is worked on
+        loads_first();
         if (a.f.data) {
-            float f[E];
-            load_row<TF, E, VEC>((const TF *)a.f.data + row * a.f.stride, D, threads, thread, f);
             float scale = a.alpha;
             if (a.post_weight) {
-                load_row<float, E, VEC>(a.post_weight, D, threads, thread, w);
-                float s = 0.0f;
+                float s = 0.0f, p[E];
 #pragma unroll
-                for (int i = 0; i < E; ++i) s += f[i] * f[i];
+                for (int i = 0; i < E; ++i) s += g[i] * g[i];
                 scale *= 1.0f / sqrtf(block_sum(s, slots[turn][0], threads) * inv + a.eps);
+                post.get(p);
 #pragma unroll
-                for (int i = 0; i < E; ++i) f[i] *= w[i];
+                for (int i = 0; i < E; ++i) g[i] *= p[i];
             }
             if (a.gate) {
-                load_row<TF, E, VEC>((const TF *)a.gate + row / per_gate * a.D, D, threads, thread, w);
 #pragma unroll
-                for (int i = 0; i < E; ++i) f[i] *= w[i];
+                for (int i = 0; i < E; ++i) g[i] *= w[i];
             }
 #pragma unroll
-            for (int i = 0; i < E; ++i) x[i] += scale * f[i];
-            store_row<TX, E, VEC>((TX *)a.x_out.data + row * a.x_out.stride, D, threads, thread, x);
+            for (int i = 0; i < E; ++i) v[i] += scale * g[i];
+            store_row<TX, E, VEC>((TX *)a.x_out.data + row * a.x_out.stride, D, threads, thread, v);
         }
-        load_row<float, E, VEC>(a.pre_weight, D, threads, thread, w);
         float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) s += x[i] * x[i];
+        for (int i = 0; i < E; ++i) s += v[i] * v[i];
         const float b = 1.0f / sqrtf(block_sum(s, slots[turn][1], threads) * inv + a.eps);
+        pre.get(w);
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = x[i] * b * w[i];
+        for (int i = 0; i < E; ++i) v[i] = v[i] * b * w[i];
         if (a.u.type == PWLQ_I8) {
-            const Step q = step_of(block_max(largest(x), top[turn], threads));
-            store_codes<E, VEC>((int8_t *)a.u.data + row * a.u.stride, D, threads, thread, x, q.factor);
+            const Step q = step_of(block_max(largest(v), top[turn], threads));
+            store_codes<E, VEC>((int8_t *)a.u.data + row * a.u.stride, D, threads, thread, v, q.factor);
             if (thread == 0) a.u.step[row] = q.step;
         } else {
-            store_row<TF, E, VEC>((TF *)a.u.data + row * a.u.stride, D, threads, thread, x);
+            store_row<TF, E, VEC>((TF *)a.u.data + row * a.u.stride, D, threads, thread, v);
         }
     }
 }
@@ -82,114 +100,143 @@ __device__ inline float *gate_sums(const pwlq_norm_backward_args &a, const NormP
     return (g * per >= first && (g + 1) * per <= last ? a.d_gate + g * a.D : part.gate + ((int64_t)blockIdx.x + g) * a.D);
 }
 
-template <typename TF, typename TX, bool KEPT, int E, bool VEC>
-__global__ __launch_bounds__(1024) void k_norm_backward(pwlq_norm_backward_args a, NormPartials part)
+// What vector instructions there are per element bounds this as much as memory, so a row's factors are joined before they meet
+// its elements: steps of 8 bits with the norms' factors, alpha and the gate with the post weight.  Both the gate's and the post
+// weight's gradients are column factors times sum dx fh over the rows of one gate row, the only sum kept for them.
+template <typename TF, typename TX, bool KEPT, int E, bool VEC, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_args a, NormPartials part)
 {
     typedef typename std::conditional<KEPT, int8_t, TF>::type SF;
     typedef typename std::conditional<KEPT, int8_t, TX>::type SX;
-    __shared__ float slots[2][4][16];
+    __shared__ float2 slots[2][2][16];
     const int threads = blockDim.x, thread = threadIdx.x, D = (int)a.D;
     const float inv = 1.0f / (float)D;
-    const int64_t per_gate = a.gate ? a.T / a.gate_rows : 1;
+    const int64_t per_gate = a.gate ? a.T / a.gate_rows : a.T;
     const int64_t first = (int64_t)blockIdx.x * part.span, last = min(first + part.span, a.T);
-    float sum_pre[E], sum_post[E], sum_gate[E], gate[E];
+    float pre[E], back[E], sum_pre[E], sum_post[E], sum_f[E];      // back: alpha gate post
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        sum_pre[i] = sum_post[i] = sum_gate[i] = 0.0f;
-        gate[i] = 1.0f;
+    for (int i = 0; i < E; ++i) sum_pre[i] = sum_post[i] = sum_f[i] = 0.0f;
+    Row<TF, E, VEC> du_row;
+    Row<TX, E, VEC> dx_row;
+    Row<SX, E, VEC> x_row;
+    Row<SF, E, VEC> f_row;
+    float x_step = 1.0f, f_step = 1.0f;
+    auto load = [&](int64_t row) {
+        x_row.load((const SX *)a.x_out.data + row * a.x_out.stride, D, threads, thread);
+        if (a.du.data) du_row.load((const TF *)a.du.data + row * a.du.stride, D, threads, thread);
+        if (a.dx_out.data) dx_row.load((const TX *)a.dx_out.data + row * a.dx_out.stride, D, threads, thread);
+        if (a.f.data) f_row.load((const SF *)a.f.data + row * a.f.stride, D, threads, thread);
+        if (KEPT) x_step = a.x_out.step[row];
+        if (KEPT && a.f.data) f_step = a.f.step[row];
+    };
+    // alpha gate into g, post into p
+    auto factors = [&](int64_t gate_row, float (&g)[E], float (&p)[E]) {
+        Row<float, E, VEC> post;
+        Row<TF, E, VEC> gate;
+        if (a.post_weight) post.load(a.post_weight, D, threads, thread);
+        if (a.gate) gate.load((const TF *)a.gate + gate_row * a.D, D, threads, thread);
+#pragma unroll
+        for (int i = 0; i < E; ++i) g[i] = p[i] = 1.0f;
+        if (a.post_weight) post.get(p);
+        if (a.gate) gate.get(g);
+#pragma unroll
+        for (int i = 0; i < E; ++i) g[i] *= a.alpha;
+    };
+    // the sums of a gate row's end
+    auto settle = [&](int64_t gate_row) {
+        float g[E], p[E];
+        factors(gate_row, g, p);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            sum_post[i] += g[i] * sum_f[i];
+            sum_f[i] *= a.alpha * p[i];
+        }
+        if (a.gate) store_row<float, E, VEC>(gate_sums(a, part, gate_row, per_gate, first, last), D, threads, thread, sum_f);
+#pragma unroll
+        for (int i = 0; i < E; ++i) sum_f[i] = 0.0f;
+    };
+    {
+        Row<float, E, VEC> weight;
+        weight.load(a.pre_weight, D, threads, thread);
+        weight.get(pre);
     }
+    load(first);
     int64_t at_gate = -1;
     int turn = 0;
     for (int64_t row = first; row < last; ++row, turn ^= 1) {
-        float dx[E], x[E], f[E], du[E], w[E];
-        load_row<SX, E, VEC>((const SX *)a.x_out.data + row * a.x_out.stride, D, threads, thread, x);
-        if (a.du.data) load_row<TF, E, VEC>((const TF *)a.du.data + row * a.du.stride, D, threads, thread, du);
-        if (a.dx_out.data) load_row<TX, E, VEC>((const TX *)a.dx_out.data + row * a.dx_out.stride, D, threads, thread, dx);
-        if (a.f.data) load_row<SF, E, VEC>((const SF *)a.f.data + row * a.f.stride, D, threads, thread, f);
-        if (a.gate && row / per_gate != at_gate) {
-            if (at_gate >= 0) {
-                store_row<float, E, VEC>(gate_sums(a, part, at_gate, per_gate, first, last), D, threads, thread, sum_gate);
-#pragma unroll
-                for (int i = 0; i < E; ++i) sum_gate[i] = 0.0f;
-            }
-            at_gate = row / per_gate;
-            load_row<TF, E, VEC>((const TF *)a.gate + at_gate * a.D, D, threads, thread, gate);
-        }
-        if (!a.dx_out.data) {
+        float dx[E], x[E], f[E], du[E];
+        x_row.get(x);
+        if (a.f.data) f_row.get(f);
+        if (a.du.data) du_row.get(du);
+        if (a.dx_out.data) dx_row.get(dx);
+        else {
 #pragma unroll
             for (int i = 0; i < E; ++i) dx[i] = 0.0f;
         }
-        if (a.du.data) {
-            if constexpr (KEPT) {
-                const float step = a.x_out.step[row];
+        const float xs = x_step, fs = f_step;
+        if (a.f.data && row / per_gate != at_gate) {
+            if (at_gate >= 0) settle(at_gate);
+            at_gate = row / per_gate;
+            float p[E];
+            factors(at_gate, back, p);
 #pragma unroll
-                for (int i = 0; i < E; ++i) x[i] *= step;
-            }
-            load_row<float, E, VEC>(a.pre_weight, D, threads, thread, w);
+            for (int i = 0; i < E; ++i) back[i] *= p[i];
+        }
+        load(min(row + 1, last - 1));                  // the next row, while this one is worked on
+        loads_first();
+        if (a.du.data) {
             float s = 0.0f, t = 0.0f;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 s += x[i] * x[i];
-                t += x[i] * (w[i] * du[i]);
+                t += x[i] * (pre[i] * du[i]);
             }
-            s = block_sum(s, slots[turn][0], threads);
-            t = block_sum(t, slots[turn][1], threads);
-            const float b = 1.0f / sqrtf(s * inv + a.eps), mean = t * inv * b * b;
+            block_sum2(s, t, slots[turn][0], threads);
+            const float b = 1.0f / sqrtf(s * xs * xs * inv + a.eps), xb = xs * b, mean = t * xb * inv * b * xb;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                dx[i] += b * (w[i] * du[i] - x[i] * mean);
-                sum_pre[i] += du[i] * (x[i] * b);
+                dx[i] = dx[i] + b * (pre[i] * du[i]) - mean * x[i];
+                sum_pre[i] += du[i] * (x[i] * xb);
             }
         }
         store_row<TX, E, VEC>((TX *)a.dx.data + row * a.dx.stride, D, threads, thread, dx);
         if (!a.f.data) continue;
-        if constexpr (KEPT) {
-            const float step = a.f.step[row];
-#pragma unroll
-            for (int i = 0; i < E; ++i) f[i] *= step;
-        }
-        // dx becomes dv / gate, then dv
-#pragma unroll
-        for (int i = 0; i < E; ++i) dx[i] *= a.alpha;
         if (a.post_weight) {
-            load_row<float, E, VEC>(a.post_weight, D, threads, thread, w);
             float s = 0.0f, t = 0.0f;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 s += f[i] * f[i];
-                t += f[i] * (w[i] * (gate[i] * dx[i]));
+                t += f[i] * (back[i] * dx[i]);
             }
-            s = block_sum(s, slots[turn][2], threads);
-            t = block_sum(t, slots[turn][3], threads);
-            const float c = 1.0f / sqrtf(s * inv + a.eps), mean = t * inv * c * c;
+            block_sum2(s, t, slots[turn][1], threads);
+            const float c = 1.0f / sqrtf(s * fs * fs * inv + a.eps), fc = fs * c, mean = t * fc * inv * c * fc;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const float dv = gate[i] * dx[i], fh = f[i] * c;
-                sum_gate[i] += dx[i] * (fh * w[i]);
-                sum_post[i] += dv * fh;
-                dx[i] = c * (w[i] * dv - f[i] * mean);
+                sum_f[i] += dx[i] * (f[i] * fc);
+                dx[i] = c * (back[i] * dx[i]) - mean * f[i];
             }
         } else {
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                sum_gate[i] += dx[i] * f[i];
-                dx[i] *= gate[i];
+                sum_f[i] += dx[i] * (f[i] * fs);
+                dx[i] *= back[i];
             }
         }
         store_row<TF, E, VEC>((TF *)a.df.data + row * a.df.stride, D, threads, thread, dx);
     }
+    if (at_gate >= 0) settle(at_gate);
     store_row<float, E, VEC>(part.pre + (int64_t)blockIdx.x * a.D, D, threads, thread, sum_pre);
     if (part.post) store_row<float, E, VEC>(part.post + (int64_t)blockIdx.x * a.D, D, threads, thread, sum_post);
-    if (at_gate >= 0) store_row<float, E, VEC>(gate_sums(a, part, at_gate, per_gate, first, last), D, threads, thread, sum_gate);
 }
 
-// Sums of the partial rows: of all workgroups for the norms' weights, of those that meet it for a gate row.
+// Sums of the partial rows, in order: of all workgroups for the norms' weights, of those that meet it for a gate row.  Sixteen
+// wavefronts take a row each in turn, four loads under way.
 constexpr int kSumWaves = 16;
 __global__ __launch_bounds__(64 * kSumWaves) void k_column_sums(pwlq_norm_backward_args a, NormPartials part, int workgroups)
 {
     __shared__ float sums[kSumWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+    const int64_t col = min((int64_t)blockIdx.x * 64 + lane, a.D - 1);
     // outputs: d_pre, d_post, the rows of d_gate
     for (int64_t out = blockIdx.y; out < 2 + (a.d_gate ? a.gate_rows : 0); out += gridDim.y) {
         const float *from = out == 0 ? part.pre : part.post;
@@ -205,12 +252,18 @@ __global__ __launch_bounds__(64 * kSumWaves) void k_column_sums(pwlq_norm_backwa
         }
         if (!to) continue;
         float s = 0.0f;
-        if (col < a.D)
-            for (int64_t w = first + wave; w < last; w += kSumWaves) s += from[w * a.D + col];
+        for (int64_t w = first + wave; w < last; w += 8 * kSumWaves) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = from[min(w + j * kSumWaves, last - 1) * a.D + col];
+            loads_first();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += w + j * kSumWaves < last ? v[j] : 0.0f;
+        }
         __syncthreads();
         sums[wave][lane] = s;
         __syncthreads();
-        if (wave == 0 && col < a.D) {
+        if (wave == 0 && blockIdx.x * 64 + lane < a.D) {
 #pragma unroll
             for (int i = 1; i < kSumWaves; ++i) s += sums[i][lane];
             to[col] = s;
@@ -226,33 +279,40 @@ __global__ void k_zero(float *a, int64_t na, float *b, int64_t nb, float *c, int
     for (int64_t j = i; j < nc; j += step) c[j] = 0.0f;
 }
 
-// Workgroups of the backward pass, each with sums of its own.
-constexpr int64_t kBackwardWgs = 512;
-int64_t backward_span(int64_t T) { return (T + kBackwardWgs - 1) / kBackwardWgs; }
+// Elements of a thread, by the row's length, and the registers a kernel may have by its most threads.  The forward pass takes 8 up
+// to 4096 columns and 16 beyond; the backward pass 8 up to 2048, 16 beyond (at 4096 16 of 256 threads 45.6 us, 8 of 512
+// 55.5: fewer wavefronts meet at each of its two barriers a row).
+int forward_elements(int64_t D) { return D <= 4096 ? 8 : 16; }
+int backward_elements(int64_t D) { return D <= 2048 ? 8 : 16; }
+
+int64_t backward_span(int64_t T, int64_t D)
+{
+    const int64_t wgs = kBackwardWaves / (threads_for(D, backward_elements(D)) / 64);
+    return (T + wgs - 1) / wgs;
+}
 
 template <typename TF, typename TX> void norm_as(const pwlq_norm_args &a, bool vec, hipStream_t stream)
 {
-    const unsigned grid = row_grid(a.T);
-#define PWLQ_NORM(E)                                                                                    \
-    do {                                                                                                \
-        if (vec) k_norm_block<TF, TX, E, true><<<grid, threads_for(a.D, E), 0, stream>>>(a);            \
-        else k_norm_block<TF, TX, E, false><<<grid, threads_for(a.D, E), 0, stream>>>(a);               \
-    } while (0)
-    if (a.D <= 8192) PWLQ_NORM(8);
-    else PWLQ_NORM(16);
+    const int64_t wgs = kForwardWaves / (threads_for(a.D, forward_elements(a.D)) / 64);
+    const unsigned grid = (unsigned)std::min(a.T, wgs);
+#define PWLQ_NORM(E, THREADS)                                                                                   \
+    (vec ? k_norm_block<TF, TX, E, true, THREADS><<<grid, threads_for(a.D, E), 0, stream>>>(a)                  \
+         : k_norm_block<TF, TX, E, false, THREADS><<<grid, threads_for(a.D, E), 0, stream>>>(a))
+    if (a.D <= 4096) PWLQ_NORM(8, 512);
+    else if (a.D <= 8192) PWLQ_NORM(16, 512);
+    else PWLQ_NORM(16, 1024);
 #undef PWLQ_NORM
 }
 
 template <typename TF, typename TX, bool KEPT>
 void backward_as(const pwlq_norm_backward_args &a, const NormPartials &part, unsigned grid, bool vec, hipStream_t stream)
 {
-#define PWLQ_NORM(E)                                                                                            \
-    do {                                                                                                        \
-        if (vec) k_norm_backward<TF, TX, KEPT, E, true><<<grid, threads_for(a.D, E), 0, stream>>>(a, part);     \
-        else k_norm_backward<TF, TX, KEPT, E, false><<<grid, threads_for(a.D, E), 0, stream>>>(a, part);        \
-    } while (0)
-    if (a.D <= 8192) PWLQ_NORM(8);
-    else PWLQ_NORM(16);
+#define PWLQ_NORM(E, THREADS)                                                                                            \
+    (vec ? k_norm_backward<TF, TX, KEPT, E, true, THREADS><<<grid, threads_for(a.D, E), 0, stream>>>(a, part)            \
+         : k_norm_backward<TF, TX, KEPT, E, false, THREADS><<<grid, threads_for(a.D, E), 0, stream>>>(a, part))
+    if (a.D <= 2048) PWLQ_NORM(8, 256);
+    else if (a.D <= 8192) PWLQ_NORM(16, 512);
+    else PWLQ_NORM(16, 1024);
 #undef PWLQ_NORM
 }
 
@@ -274,7 +334,7 @@ void norm_block(const pwlq_norm_args &a, hipStream_t stream)
 size_t norm_backward_workspace(int64_t T, int64_t D, int64_t gate_rows)
 {
     if (!T) return 0;
-    const int64_t wgs = (T + backward_span(T) - 1) / backward_span(T);
+    const int64_t wgs = (T + backward_span(T, D) - 1) / backward_span(T, D);
     return (size_t)(3 * wgs + gate_rows) * (size_t)D * sizeof(float);
 }
 
@@ -285,7 +345,7 @@ void norm_backward(const pwlq_norm_backward_args &a, void *workspace, hipStream_
         k_zero<<<256, 256, 0, stream>>>(a.d_pre, a.d_pre ? a.D : 0, a.d_post, a.d_post ? a.D : 0, a.d_gate, n);
         return;
     }
-    const int64_t span = backward_span(a.T), wgs = (a.T + span - 1) / span;
+    const int64_t span = backward_span(a.T, a.D), wgs = (a.T + span - 1) / span;
     NormPartials part = {(float *)workspace, a.d_post ? (float *)workspace + wgs * a.D : nullptr,
                          (float *)workspace + 2 * wgs * a.D, span};
     const bool vec = a.D % 8 == 0 && vectors(a.du, a.T) && vectors(a.dx_out, a.T) && vectors(a.x_out, a.T) &&

@@ -19,8 +19,10 @@ __global__ __launch_bounds__(1024) void k_pack_rows(const T *x, int64_t stride, 
     const int threads = blockDim.x, thread = threadIdx.x;
     int turn = 0;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x, turn ^= 1) {
+        Row<T, E, VEC> r;
         float v[E];
-        load_row<T, E, VEC>(x + row * stride, cols, threads, thread, v);
+        r.load(x + row * stride, cols, threads, thread);
+        r.get(v);
         const Step s = step_of(block_max(largest(v), slots[turn], threads));
         store_codes<E, VEC>(codes + row * cols, cols, threads, thread, v, s.factor);
         if (thread == 0) step[row] = s.step;
@@ -32,8 +34,10 @@ __global__ __launch_bounds__(1024) void k_unpack_rows(const int8_t *codes, const
 {
     const int threads = blockDim.x, thread = threadIdx.x;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        Row<int8_t, E, VEC> r;
         float v[E];
-        load_row<int8_t, E, VEC>(codes + row * cols, cols, threads, thread, v);
+        r.load(codes + row * cols, cols, threads, thread);
+        r.get(v);
         const float s = step[row];
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] *= s;

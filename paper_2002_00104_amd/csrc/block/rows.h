@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
 
 namespace pwlq_block {
 
@@ -38,93 +39,139 @@ __device__ inline float widen(bf16 v) { return (float)v; }
 __device__ inline float widen(f16 v) { return (float)v; }
 __device__ inline float widen(int8_t v) { return (float)v; }
 
-template <typename T> __device__ inline v8f load8(const T *p) { return widen(*(const typename Vec8<T>::type *)p); }
 template <typename T> __device__ inline void store8(T *p, v8f v)
 {
     *(typename Vec8<T>::type *)p = __builtin_convertvector(v, typename Vec8<T>::type);
 }
 
-// Eight codes in two words; a code is a whole number within +-127 held in binary32.
-__device__ inline v2u codes8(v8f q)
+// A row as a buffer of its own length: reads beyond its end give 0 and writes there do nothing, by the hardware's bounds
+// check, so threads past the end need no branch and no select.  `row` is the same for the whole wavefront.
+__device__ inline __amdgpu_buffer_rsrc_t row_buffer(const void *row, int bytes)
 {
-    v2u r = {0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i / 4] |= ((uint32_t)(int)q[i] & 0xffu) << (8 * (i & 3));
-    return r;
+    return __builtin_amdgcn_make_buffer_rsrc((void *)row, 0, bytes, 0x00027000);
+}
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+template <typename T> __device__ inline typename Vec8<T>::type buffer_load8(__amdgpu_buffer_rsrc_t b, int offset)
+{
+    union { v4u w[sizeof(T) == 4 ? 2 : 1]; v2u half; typename Vec8<T>::type v; } u;
+    if constexpr (sizeof(T) == 1) u.half = __builtin_amdgcn_raw_buffer_load_b64(b, offset, 0, 0);
+    else u.w[0] = __builtin_amdgcn_raw_buffer_load_b128(b, offset, 0, 0);
+    if constexpr (sizeof(T) == 4) u.w[1] = __builtin_amdgcn_raw_buffer_load_b128(b, offset + 16, 0, 0);
+    return u.v;
+}
+template <typename T> __device__ inline void buffer_store8(__amdgpu_buffer_rsrc_t b, int offset, typename Vec8<T>::type v)
+{
+    union { v4u w[sizeof(T) == 4 ? 2 : 1]; v2u half; typename Vec8<T>::type v; } u;
+    u.v = v;
+    if constexpr (sizeof(T) == 1) __builtin_amdgcn_raw_buffer_store_b64(u.half, b, offset, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b128(u.w[0], b, offset, 0, 0);
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(u.w[1], b, offset + 16, 0, 0);
+}
+template <typename T> __device__ inline T buffer_load1(__amdgpu_buffer_rsrc_t b, int offset)
+{
+    union { uint32_t w; uint16_t h; uint8_t c; T v; } u;
+    if constexpr (sizeof(T) == 1) u.c = __builtin_amdgcn_raw_buffer_load_b8(b, offset, 0, 0);
+    else if constexpr (sizeof(T) == 2) u.h = __builtin_amdgcn_raw_buffer_load_b16(b, offset, 0, 0);
+    else u.w = __builtin_amdgcn_raw_buffer_load_b32(b, offset, 0, 0);
+    return u.v;
+}
+template <typename T> __device__ inline void buffer_store1(__amdgpu_buffer_rsrc_t b, int offset, T v)
+{
+    union { uint32_t w; uint16_t h; uint8_t c; T v; } u;
+    u.v = v;
+    if constexpr (sizeof(T) == 1) __builtin_amdgcn_raw_buffer_store_b8(u.c, b, offset, 0, 0);
+    else if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(u.h, b, offset, 0, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(u.w, b, offset, 0, 0);
 }
 
-// Column of a thread's element i.  VEC: vectors of eight columns, as many vectors apart as there are threads; else
-// single columns that far apart.  Both coalesce, the second for any length and alignment.
-template <bool VEC> __device__ inline int column(int i, int threads, int thread)
-{
-    return VEC ? ((i >> 3) * threads + thread) * 8 + (i & 7) : i * threads + thread;
-}
+// Columns of one row as they are in memory: thread `thread` of `threads` takes E.  VEC: vectors of eight columns, as many
+// vectors apart as there are threads; else single columns that far apart.  Both coalesce, the second for any length and
+// alignment.  load() only reads, so several rows can be under way; get() widens.
+template <typename T, int E, bool VEC> struct Row {
+    typename std::conditional<VEC, typename Vec8<T>::type, T>::type raw[VEC ? E / 8 : E];
 
-// Columns of one row: thread `thread` of `threads` takes E.  Those past the row's end are 0.
-template <typename T, int E, bool VEC>
-__device__ inline void load_row(const T *row, int cols, int threads, int thread, float (&v)[E])
-{
-    if constexpr (VEC) {
-        typename Vec8<T>::type raw[E / 8];
+    __device__ void load(const T *row, int cols, int threads, int thread)
+    {
+        const __amdgpu_buffer_rsrc_t b = row_buffer(row, cols * (int)sizeof(T));
+        if constexpr (VEC) {
 #pragma unroll
-        for (int j = 0; j < E / 8; ++j) {
-            const int c = (j * threads + thread) * 8;
-            raw[j] = c < cols ? *(const typename Vec8<T>::type *)(row + c) : typename Vec8<T>::type(0);
+            for (int j = 0; j < E / 8; ++j) raw[j] = buffer_load8<T>(b, (j * threads + thread) * 8 * (int)sizeof(T));
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) raw[i] = buffer_load1<T>(b, (i * threads + thread) * (int)sizeof(T));
         }
-#pragma unroll
-        for (int j = 0; j < E / 8; ++j) {
-            const v8f w = widen(raw[j]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[8 * j + i] = w[i];
-        }
-    } else {
-        T raw[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const int c = i * threads + thread;
-            raw[i] = c < cols ? row[c] : T(0);
-        }
-#pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = widen(raw[i]);
     }
-}
+    __device__ void get(float (&v)[E]) const
+    {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int j = 0; j < E / 8; ++j) {
+                const v8f w = widen(raw[j]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * j + i] = w[i];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = widen(raw[i]);
+        }
+    }
+};
+
+// Nothing is moved across: the loads above it are issued before what uses them.  The compiler would otherwise put each beside its use,
+// which saves registers and waits for memory once per load.
+__device__ inline void loads_first() { __builtin_amdgcn_sched_barrier(0); }
 
 template <typename T, int E, bool VEC>
 __device__ inline void store_row(T *row, int cols, int threads, int thread, const float (&v)[E])
 {
+    const __amdgpu_buffer_rsrc_t b = row_buffer(row, cols * (int)sizeof(T));
     if constexpr (VEC) {
 #pragma unroll
         for (int j = 0; j < E / 8; ++j) {
-            const int c = (j * threads + thread) * 8;
             v8f w;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = v[8 * j + i];
-            if (c < cols) store8(row + c, w);
+            buffer_store8<T>(b, (j * threads + thread) * 8 * (int)sizeof(T), __builtin_convertvector(w, typename Vec8<T>::type));
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const int c = i * threads + thread;
-            if (c < cols) row[c] = (T)v[i];
-        }
+        for (int i = 0; i < E; ++i) buffer_store1<T>(b, (i * threads + thread) * (int)sizeof(T), (T)v[i]);
     }
 }
 
-// Sum, or maximum of unsigned words, over a workgroup of whole wavefronts.  `slots`: LDS of this reduction alone, a word
-// per wavefront (at most 16), not written again before the workgroup's next barrier.  Every thread gets the same result: the
-// order of the sum is fixed.
+// Sum, or maximum of unsigned words, over a wavefront: a scan along each row of sixteen lanes, then along the rows, all by
+// data-parallel moves; the last lane has the result.  0 is neutral for both.
+template <int CONTROL, int ROWS> __device__ inline uint32_t moved(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, ROWS, 0xf, true);
+}
 __device__ inline float wave_sum(float v)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+#define PWLQ_STEP(CONTROL, ROWS) v += __uint_as_float(moved<CONTROL, ROWS>(__float_as_uint(v)))
+    PWLQ_STEP(0x111, 0xf);             // one lane up
+    PWLQ_STEP(0x112, 0xf);
+    PWLQ_STEP(0x114, 0xf);
+    PWLQ_STEP(0x118, 0xf);
+    PWLQ_STEP(0x142, 0xa);             // a row's last lane to the next row
+    PWLQ_STEP(0x143, 0xc);             // lane 31 to the upper half
+#undef PWLQ_STEP
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
 }
 __device__ inline uint32_t wave_max(uint32_t v)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
-    return v;
+#define PWLQ_STEP(CONTROL, ROWS) v = max(v, moved<CONTROL, ROWS>(v))
+    PWLQ_STEP(0x111, 0xf);
+    PWLQ_STEP(0x112, 0xf);
+    PWLQ_STEP(0x114, 0xf);
+    PWLQ_STEP(0x118, 0xf);
+    PWLQ_STEP(0x142, 0xa);
+    PWLQ_STEP(0x143, 0xc);
+#undef PWLQ_STEP
+    return __builtin_amdgcn_readlane(v, 63);
 }
+
+// The same over a workgroup of whole wavefronts, at most 16.  `slots`: LDS of this reduction alone, a word per wavefront (two for
+// two sums), not written again before the workgroup's next barrier.  Every thread gets the same result, and the order is fixed.
 __device__ inline float block_sum(float v, float *slots, int threads)
 {
     v = wave_sum(v);
@@ -134,6 +181,19 @@ __device__ inline float block_sum(float v, float *slots, int threads)
     float s = 0.0f;
     for (int w = 0; w < threads / 64; ++w) s += slots[w];
     return s;
+}
+__device__ inline void block_sum2(float &v, float &u, float2 *slots, int threads)
+{
+    v = wave_sum(v);
+    u = wave_sum(u);
+    if (threads == 64) return;
+    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = make_float2(v, u);
+    __syncthreads();
+    v = u = 0.0f;
+    for (int w = 0; w < threads / 64; ++w) {
+        v += slots[w].x;
+        u += slots[w].y;
+    }
 }
 __device__ inline uint32_t block_max(uint32_t v, uint32_t *slots, int threads)
 {
@@ -161,35 +221,39 @@ __device__ inline Step step_of(uint32_t bits)
     }
     return s;
 }
-// With factor 0 the code is 0 whatever the element is: rows that hold a NaN or an infinity.
-__device__ inline float code_of(float x, float factor) { return factor == 0.0f ? 0.0f : __builtin_rintf(x * factor); }
-
 template <int E> __device__ inline uint32_t largest(const float (&v)[E])
 {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    for (int i = 0; i < E; i += 2) m = max(max(m, __float_as_uint(v[i]) & 0x7fffffffu), __float_as_uint(v[i + 1]) & 0x7fffffffu);
     return m;
 }
 
+// rne(x factor) in the low byte: added to 1.5 2^23 the product's fraction is rounded away.  |x factor| is at most 127.
+__device__ inline uint32_t code_byte(float x, float factor) { return __float_as_uint(x * factor + 12582912.0f); }
+__device__ inline uint32_t four_codes(const float *x, float factor)
+{
+    const uint32_t a = __builtin_amdgcn_perm(code_byte(x[1], factor), code_byte(x[0], factor), 0x0c0c0400u);
+    const uint32_t b = __builtin_amdgcn_perm(code_byte(x[3], factor), code_byte(x[2], factor), 0x0c0c0400u);
+    return __builtin_amdgcn_perm(b, a, 0x05040100u);
+}
+
+// Codes of a row.  With factor 0 (a row of next to nothing, or one that holds a NaN or an infinity) all are 0, whatever v is.
 template <int E, bool VEC>
 __device__ inline void store_codes(int8_t *row, int cols, int threads, int thread, const float (&v)[E], float factor)
 {
+    const __amdgpu_buffer_rsrc_t b = row_buffer(row, cols);
+    const bool none = factor == 0.0f;
     if constexpr (VEC) {
 #pragma unroll
         for (int j = 0; j < E / 8; ++j) {
-            const int c = (j * threads + thread) * 8;
-            v8f q;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = code_of(v[8 * j + i], factor);
-            if (c < cols) *(v2u *)(row + c) = codes8(q);
+            v2u q = {0u, 0u};
+            if (!none) q = v2u{four_codes(v + 8 * j, factor), four_codes(v + 8 * j + 4, factor)};
+            buffer_store8<int8_t>(b, (j * threads + thread) * 8, q);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const int c = i * threads + thread;
-            if (c < cols) row[c] = (int8_t)(int)code_of(v[i], factor);
-        }
+        for (int i = 0; i < E; ++i) buffer_store1<int8_t>(b, i * threads + thread, none ? 0 : (int8_t)code_byte(v[i], factor));
     }
 }
 
