@@ -353,22 +353,39 @@ __global__ __launch_bounds__(256) void k_adapter_second(SecondArgs a)
     WV w[4];
     load_ranks(adapter, 0, 128 * tile + 8 * l, w);
 
-    for (int row = threadIdx.x >> 4; row < kSecondRows; row += blockDim.x >> 4)
-        for (int r = l; r < pitch - 1; r += 16) {
-            const int64_t at = clamp_row(row0 + row, a.rows) * a.R + min(r, a.R - 1);
-            float s = 0.0f;
-            for (int p = 0; p < a.splits; p += 4) {
-                float v[4];
+    // H into LDS, its parts added up in order: four elements of a thread and four parts under way.  Sixteen ranks of a row are
+    // neighbours, then the rows, then the next sixteen ranks.
+    for (int i = threadIdx.x; i - (int)threadIdx.x < kSecondRows * (pitch - 1); i += 4 * blockDim.x) {
+        int row[4], r[4];
+        int64_t at[4];
+        float sum[4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = a.h[min(p + j, a.splits - 1) * a.rows * a.R + at];
-                loads_first();
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s += p + j < a.splits ? v[j] : 0.0f;
-            }
-            if (r >= a.R) s = 0.0f;
-            else if (walk == 0 && a.h_out && row0 + row < a.rows) a.h_out[at] = s;
-            hs[row * pitch + r] = s;
+        for (int j = 0; j < 4; ++j) {
+            const int e = i + j * blockDim.x;
+            row[j] = (e >> 4) % kSecondRows;
+            r[j] = e / (16 * kSecondRows) * 16 + (e & 15);
+            at[j] = clamp_row(row0 + row[j], a.rows) * a.R + min(r[j], a.R - 1);
+            sum[j] = 0.0f;
         }
+        for (int p = 0; p < a.splits; p += 4) {
+            float v[4][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[k][j] = a.h[min(p + k, a.splits - 1) * a.rows * a.R + at[j]];
+            loads_first();
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] += p + k < a.splits ? v[k][j] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (r[j] >= pitch - 1) continue;
+            if (r[j] < a.R && walk == 0 && a.h_out && row0 + row[j] < a.rows) a.h_out[at[j]] = sum[j];
+            hs[row[j] * pitch + r[j]] = r[j] < a.R ? sum[j] : 0.0f;
+        }
+    }
     __syncthreads();
     for (; tile < tiles; tile += stride) {
         const int64_t col = 128 * tile + 8 * l;
@@ -423,50 +440,6 @@ __global__ __launch_bounds__(256) void k_adapter_second(SecondArgs a)
 // --------------------------------------------------------------------------
 // both products for few rows
 // --------------------------------------------------------------------------
-// One rank of one row.
-template <typename TX, typename TW, bool VEC>
-__global__ __launch_bounds__(256) void k_adapter_first_token(FirstArgs a)
-{
-    __shared__ float slots[16];
-    const int64_t row = blockIdx.y;
-    const int r = blockIdx.x, id = a.ids[row];
-    float s = 0.0f;
-    if (id >= 0 && id < a.adapters) {
-        const TX *x = (const TX *)a.x + row * a.stride;
-        const TW *w = (const TW *)a.w + ((int64_t)id * a.R + r) * a.K;
-        v8f t = v8f(0);
-#pragma unroll 2
-        for (int64_t k = 8 * threadIdx.x; k < a.K; k += 8 * 256) t += widen(piece<TX, VEC>(x, k, a.K)) * widen(piece<TW, VEC>(w, k, a.K));
-        s = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
-        s = block_sum(s, slots, 256) * (a.step ? a.scale[id] * a.step[row] : a.scale[id]);
-    }
-    if (threadIdx.x == 0) a.out[row * a.R + r] = s;
-}
-
-// 512 columns of one row; the four wavefronts share the ranks.
-template <typename TW, typename TB, bool VEC>
-__global__ __launch_bounds__(256) void k_adapter_second_token(SecondArgs a)
-{
-    __shared__ v8f sums[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = blockIdx.y, col = (int64_t)blockIdx.x * 512 + 8 * lane;
-    const int id = a.ids[row];
-    v8f y = v8f(0), base = v8f(0);
-    if (a.has_base && wave == 0) base = widen(piece<TB, VEC>((const TB *)a.base + row * a.base_stride, col, a.C));
-    if (id >= 0 && id < a.adapters) {
-        const TW *w = (const TW *)a.w + (int64_t)id * a.R * a.C;
-#pragma unroll 4
-        for (int r = wave; r < a.R; r += 4) y += a.h[row * a.R + r] * widen(piece<TW, VEC>(w + (int64_t)r * a.C, col, a.C));
-    }
-    sums[wave][lane] = y;
-    __syncthreads();
-    if (wave) return;
-    y = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-    y += a.base_step ? base * a.base_step[row] : base;
-    if (a.out_type == PWLQ_F32) store_columns<float>(a.out, row * a.out_stride, col, a.C, y, VEC);
-    else store_columns<TW>(a.out, row * a.out_stride, col, a.C, y, VEC);
-}
-
 // Both products of one row in one launch, for 512 columns: the row's H is computed by each of its workgroups anew, which costs
 // reading down again from L2 but no second launch and no wait for it.  The sixteen wavefronts share the ranks of both products.
 struct TokenArgs {
@@ -575,15 +548,14 @@ template <int RT> struct OuterLds {
 
 template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const OuterArgs &a, int tile, int split, OuterLds<RT> &lds)
 {
-    constexpr int kUnits = RT == 4 ? 1 : 2;            // of sixteen rows, under way at once
     typedef typename Vec8<TX>::type XV;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
     const int64_t col = (int64_t)(tile % a.column_tiles) * 128 + 8 * l;
     const int r0 = tile / a.column_tiles * 16 * RT;
     const int64_t t0 = split * a.span, t1 = min(t0 + a.span, a.rows);
     struct Rows {
-        XV x[kUnits][4];
-        float h[kUnits][4][RT], step[kUnits][4];
+        XV x[4];
+        float h[4][RT], step[4];
     };
     float *const part = a.out + (int64_t)split * a.adapters * a.R * a.C;
     int32_t *const present = a.present && a.flags && tile == 0 ? a.present + (int64_t)split * a.adapters : nullptr;
@@ -616,43 +588,38 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
             __syncthreads();
             auto load = [&](int first, Rows &v) {
 #pragma unroll
-                for (int u = 0; u < kUnits; ++u)
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t row = t + lds.list[min(first + element_of<TX>(q, i), count - 1)];
+                    v.x[i] = columns8<TX, VEC>((const TX *)a.x + row * a.stride, col, a.C);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int64_t row = t + lds.list[min(first + 16 * u + element_of<TX>(q, i), count - 1)];
-                        v.x[u][i] = columns8<TX, VEC>((const TX *)a.x + row * a.stride, col, a.C);
-#pragma unroll
-                        for (int n = 0; n < RT; ++n) v.h[u][i][n] = a.h[row * a.R + min(r0 + 16 * n + l, a.R - 1)];
-                        if constexpr (sizeof(TX) == 1) v.step[u][i] = a.step[row];
-                    }
+                    for (int n = 0; n < RT; ++n) v.h[i][n] = a.h[row * a.R + min(r0 + 16 * n + l, a.R - 1)];
+                    if constexpr (sizeof(TX) == 1) v.step[i] = a.step[row];
+                }
             };
-            int first = 16 * kUnits * wave;
+            int first = 16 * wave;
             if (first >= count) continue;
             Rows now, after;
             load(first, now);
-            for (; first < count; first += 64 * kUnits, now = after) {
-                load(first + 64 * kUnits, after);          // beyond the list: its last row, not used
+            for (; first < count; first += 64, now = after) {
+                load(first + 64, after);                   // beyond the list: its last row, not used
                 loads_first();
+                bool own[4];
 #pragma unroll
-                for (int u = 0; u < kUnits; ++u) {
-                    bool own[4];
+                for (int i = 0; i < 4; ++i) {
+                    own[i] = first + element_of<TX>(q, i) < count;
+                    now.x[i] = own[i] ? now.x[i] : XV(0);
+                }
+#pragma unroll
+                for (int n = 0; n < RT; ++n) {
+                    float h[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        own[i] = first + 16 * u + element_of<TX>(q, i) < count;
-                        now.x[u][i] = own[i] ? now.x[u][i] : XV(0);
+                        h[i] = now.h[i][n];
+                        if constexpr (sizeof(TX) == 1) h[i] *= now.step[i];
+                        h[i] = own[i] ? h[i] : 0.0f;
                     }
-#pragma unroll
-                    for (int n = 0; n < RT; ++n) {
-                        float h[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            h[i] = now.h[u][i][n];
-                            if constexpr (sizeof(TX) == 1) h[i] *= now.step[u][i];
-                            h[i] = own[i] ? h[i] : 0.0f;
-                        }
-                        if constexpr (in_thirds<TX>) product16<TX>(thirds(h), now.x[u], acc[n]);
-                        else product16<TX>(h, now.x[u], acc[n]);
-                    }
+                    if constexpr (in_thirds<TX>) product16<TX>(thirds(h), now.x, acc[n]);
+                    else product16<TX>(h, now.x, acc[n]);
                 }
             }
         }
@@ -713,7 +680,7 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
 
 // Both gradients in one launch: the second fills the chip while the first one's last workgroups end.
 template <typename TX, typename TY, int RT, bool VEC>
-__global__ __launch_bounds__(256) void k_adapter_outer(OuterArgs up, OuterArgs down)
+__global__ __launch_bounds__(256, 3) void k_adapter_outer(OuterArgs up, OuterArgs down)
 {
     __shared__ OuterLds<RT> lds;
     const int ups = up.column_tiles * up.rank_blocks;
@@ -772,17 +739,18 @@ int rank_blocks(int R) { return (R + 16 * rank_tiles(R) - 1) / (16 * rank_tiles(
 // Parts of the first product's reduction: workgroups for the whole chip, each with a batch of steps for its wavefronts at least.
 int first_splits(int64_t T, int64_t K, int R)
 {
-    if (T <= kTokenRows) return 1;
+    if (!T) return 1;
     const int64_t wgs = (T + kRows - 1) / kRows * rank_blocks(R);
     return (int)std::max<int64_t>(1, std::min<int64_t>(1024 / wgs, (K + 511) / 512));
 }
 int64_t first_chunk(int64_t K, int splits) { return ((K + splits - 1) / splits + 255) / 256 * 256; }
 
-// Parts of the rows for the outer products: a workgroup or two to each CU.
+// Parts of the rows for the outer products: three workgroups to each CU.
+int outer_blocks(int R) { return R <= 16 ? 1 : (R + 31) / 32; }
 int64_t outer_span(int64_t T, int64_t K, int64_t N, int R)
 {
-    const int64_t wgs = ((K + 127) / 128 + (N + 127) / 128) * rank_blocks(R), most = rank_tiles(R) == 4 ? 256 : 512;
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(most / wgs, (T + 63) / 64));
+    const int64_t wgs = ((K + 127) / 128 + (N + 127) / 128) * outer_blocks(R);
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(768 / wgs, (T + 63) / 64));
     return ((T + splits - 1) / splits + 63) / 64 * 64;
 }
 int outer_splits(int64_t T, int64_t K, int64_t N, int R)
@@ -824,12 +792,6 @@ struct BackwardSpace {
 
 template <typename TX, typename TW> void first_as(FirstArgs a, bool vec, hipStream_t stream)
 {
-    if (a.rows <= kTokenRows) {
-        const dim3 grid(a.R, (unsigned)a.rows);
-        if (vec) k_adapter_first_token<TX, TW, true><<<grid, 256, 0, stream>>>(a);
-        else k_adapter_first_token<TX, TW, false><<<grid, 256, 0, stream>>>(a);
-        return;
-    }
     const int64_t tiles = (a.rows + kRows - 1) / kRows, splits = (a.K + a.chunk - 1) / a.chunk;
     a.slots = (int)std::min<int64_t>(std::min(a.adapters, kRows), std::max<int64_t>(1, 2048 / (tiles * splits * rank_blocks(a.R))));
     const dim3 grid((unsigned)(tiles * a.slots), rank_blocks(a.R), (unsigned)splits);
@@ -855,12 +817,6 @@ constexpr int64_t kSecondWgs = 512;    // that walk at once
 
 template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipStream_t stream)
 {
-    if (a.rows <= kTokenRows && a.splits == 1) {
-        const dim3 grid((unsigned)((a.C + 511) / 512), (unsigned)a.rows);
-        if (vec) k_adapter_second_token<TW, TB, true><<<grid, 256, 0, stream>>>(a);
-        else k_adapter_second_token<TW, TB, false><<<grid, 256, 0, stream>>>(a);
-        return;
-    }
     const int64_t tiles = (a.rows + kSecondRows - 1) / kSecondRows, columns = (a.C + 127) / 128;
     const int waves = tiles * columns < 2048 ? 1 : 4;
     a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, waves == 1 ? columns : (kSecondWgs + tiles - 1) / tiles);
@@ -891,9 +847,8 @@ template <typename TX, typename TY> void outer_as(const OuterArgs &up, const Out
         if (vec) k_adapter_outer<TX, TY, RT, true><<<grid, 256, 0, stream>>>(up, down);         \
         else k_adapter_outer<TX, TY, RT, false><<<grid, 256, 0, stream>>>(up, down);            \
     } while (0)
-    if (rank_tiles(up.R) == 1) PWLQ_OUTER(1);
-    else if (rank_tiles(up.R) == 2) PWLQ_OUTER(2);
-    else PWLQ_OUTER(4);
+    if (up.R <= 16) PWLQ_OUTER(1);
+    else PWLQ_OUTER(2);
 #undef PWLQ_OUTER
 }
 
@@ -907,10 +862,7 @@ void outer(const OuterArgs &up, const OuterArgs &down, int splits, int x_type, i
 bool whole_vectors(int64_t C, const void *w) { return C % 8 == 0 && aligned16(w); }
 
 // Whether few rows go through one launch.
-bool by_token(const pwlq_adapter_args &a)
-{
-    return a.T <= kTokenRows && a.R <= kTokenRanks;
-}
+bool by_token(int64_t T, int R) { return T <= kTokenRows && R <= kTokenRanks; }
 
 template <typename TX, typename TW> void token_as(const TokenArgs &a, int64_t rows, bool vec, hipStream_t stream)
 {
@@ -951,13 +903,14 @@ void token(const pwlq_adapter_args &a, hipStream_t stream)
 
 size_t adapter_workspace(int64_t T, int64_t K, int R)
 {
+    if (by_token(T, R)) return 0;
     const int splits = first_splits(T, K, R);
     return splits > 1 ? (size_t)splits * (size_t)T * (size_t)R * sizeof(float) : 0;
 }
 
 void adapter_forward(const pwlq_adapter_args &a, void *workspace, hipStream_t stream)
 {
-    if (by_token(a)) {
+    if (by_token(a.T, a.R)) {
         token(a, stream);
         return;
     }
@@ -1045,7 +998,7 @@ void adapter_backward(const pwlq_adapter_backward_args &a, void *workspace, hipS
     up.ids = down.ids = a.ids;
     up.R = down.R = a.R;
     up.adapters = down.adapters = a.adapters;
-    up.rank_blocks = down.rank_blocks = rank_blocks(a.R);
+    up.rank_blocks = down.rank_blocks = outer_blocks(a.R);
     up.h = a.h;
     up.x = a.dy.data;
     up.stride = a.dy.stride;
