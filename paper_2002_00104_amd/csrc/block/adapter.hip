@@ -256,28 +256,54 @@ __device__ inline void as_words(v2u v, uint32_t (&w)[4])
     for (int j = 0; j < 4; ++j) w[j] = upper_halves(__float_as_uint(f[2 * j + 1]), __float_as_uint(f[2 * j]));
 }
 
-// y[j] += sum over the sixteen elements of h times column j of x; `h`: H of the lane's row and elements.
-template <typename T> __device__ inline void product16(const Thirds &h, const typename Vec8<T>::type (&x)[4], v4f (&y)[8])
-{
+// H of a lane's row and elements, and the columns of x, as the instructions take them.
+template <typename T, bool THIRDS = in_thirds<T>> struct H16 {
+    Thirds t;
+    __device__ H16(const float (&h)[4]) : t(thirds(h)) {}
+};
+template <typename T> struct H16<T, false> {
+    float v[4];
+    __device__ H16(const float (&h)[4])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = h[i];
+    }
+};
+template <typename T, bool THIRDS = in_thirds<T>> struct Columns {
     uint32_t w[4][4];
+    __device__ Columns(const typename Vec8<T>::type (&x)[4])
+    {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) as_words(x[i], w[i]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const v4s c = j & 1 ? words(upper_halves(w[1][j / 2], w[0][j / 2]), upper_halves(w[3][j / 2], w[2][j / 2]))
-                            : words(lower_halves(w[1][j / 2], w[0][j / 2]), lower_halves(w[3][j / 2], w[2][j / 2]));
-#pragma unroll
-        for (int p = 2; p >= 0; --p) y[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(words(h.w[p][0], h.w[p][1]), c, y[j], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) as_words(x[i], w[i]);
     }
-}
-template <typename T> __device__ inline void product16(const float (&h)[4], const typename Vec8<T>::type (&x)[4], v4f (&y)[8])
+};
+template <typename T> struct Columns<T, false> {
+    typename Vec8<T>::type v[4];
+    __device__ Columns(const typename Vec8<T>::type (&x)[4])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = x[i];
+    }
+};
+// y[j] += sum over the sixteen elements of h times column j0 + j.
+template <typename T, int N> __device__ inline void product16(const H16<T, true> &h, const Columns<T, true> &x, int j0, v4f (&y)[N])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const v8f c = widen(x[i]);
+    for (int p = 2; p >= 0; --p)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[i], c[j], y[j], 0, 0, 0);
-    }
+        for (int j = 0; j < N; ++j) {
+            const int d = (j0 + j) / 2;
+            const v4s c = j & 1 ? words(upper_halves(x.w[1][d], x.w[0][d]), upper_halves(x.w[3][d], x.w[2][d]))
+                                : words(lower_halves(x.w[1][d], x.w[0][d]), lower_halves(x.w[3][d], x.w[2][d]));
+            y[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(words(h.t.w[p][0], h.t.w[p][1]), c, y[j], 0, 0, 0);
+        }
+}
+template <typename T, int N> __device__ inline void product16(const H16<T, false> &h, const Columns<T, false> &x, int j0, v4f (&y)[N])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) y[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(h.v[i], widen(x.v[i][j0 + j]), y[j], 0, 0, 0);
 }
 
 // --------------------------------------------------------------------------
@@ -296,53 +322,73 @@ struct SecondArgs {
 };
 
 // A wavefront does 16 rows by 128 columns.  The ranks come sixteen at a time, their products added to the row's sum where the
-// row has the adapter.  A workgroup walks along its
-// rows, H in LDS; the next tile's base and W are on their way while one is computed and stored.
+// row has the adapter.  A workgroup walks along its rows, H in LDS; the next tile's base and W are on their way while one is
+// computed and stored.  Rows and adapters are buffers of their own length: ranks beyond R read as 0, rows beyond the last are not
+// written, and an address is one register of a lane's.
 constexpr int kSecondRows = 16;
 __host__ __device__ inline int second_pitch(int R) { return (R + 15) / 16 * 16 + 1; }
 
-template <typename T> __device__ inline void store_columns(void *data, int64_t at, int64_t col, int64_t cols, v8f v, bool vec)
+// Eight columns at once or one by one; those beyond the last belong to no output, whatever is read there.
+template <typename T, bool VEC> __device__ inline typename Vec8<T>::type buffer_columns(__amdgpu_buffer_rsrc_t b, int offset)
 {
-    T *p = (T *)data + at + col;
-    if (vec) {
-        if (col < cols) store8(p, v);
+    if constexpr (VEC) return buffer_load8<T>(b, offset);
+    else {
+        union { typename Vec8<T>::type v; T e[8]; } u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u.e[i] = buffer_load1<T>(b, offset + i * (int)sizeof(T));
+        return u.v;
+    }
+}
+template <typename T, bool VEC> __device__ inline void store_tile(__amdgpu_buffer_rsrc_t b, int offset, int columns, v8f v)
+{
+    if constexpr (VEC) {
+        if (columns > 0) buffer_store8<T>(b, offset, __builtin_convertvector(v, typename Vec8<T>::type));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (col + i < cols) p[i] = (T)v[i];
+            if (i < columns) buffer_store1<T>(b, offset + i * (int)sizeof(T), (T)v[i]);
     }
 }
 
 template <typename TW, typename TB, bool VEC>
-__global__ __launch_bounds__(256) void k_adapter_second(SecondArgs a)
+__global__ __launch_bounds__(256, sizeof(TB) == 2 && VEC ? 3 : 2) void k_adapter_second(SecondArgs a)
 {
     typedef typename Vec8<TW>::type WV;
     typedef typename Vec8<TB>::type BV;
     extern __shared__ float hs[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x / 64, l = lane & 15, q = lane >> 4;
     const int64_t row0 = (int64_t)(blockIdx.x / a.walks) * kSecondRows;
-    const int walk = blockIdx.x % a.walks, pitch = second_pitch(a.R);
-    int64_t tile = walk * waves + wave;                // of 128 columns
-    const int64_t tiles = (a.C + 127) / 128, stride = (int64_t)a.walks * waves;
+    const int walk = blockIdx.x % a.walks, pitch = second_pitch(a.R), C = (int)a.C;
+    const int tiles = (C + 127) / 128, stride = a.walks * waves;
+    int tile = walk * waves + wave;                    // of 128 columns
 
-    // what a tile needs from memory: base, and the first adapter's first ranks (0 beyond R)
-    auto load_base = [&](int64_t col, BV (&v)[4]) {
+    const uint32_t rows = (uint32_t)min((int64_t)kSecondRows, a.rows - row0);
+    const int base_pitch = (int)a.base_stride * (int)sizeof(TB), out_size = a.out_type == PWLQ_F32 ? 4 : (int)sizeof(TW);
+    const int out_pitch = (int)a.out_stride * out_size;
+    const __amdgpu_buffer_rsrc_t base_rows = row_buffer((const TB *)a.base + row0 * a.base_stride, (rows - 1) * base_pitch + C * sizeof(TB));
+    const __amdgpu_buffer_rsrc_t out_rows =
+        row_buffer((char *)a.out + row0 * a.out_stride * out_size, (rows - 1) * out_pitch + C * out_size);
+
+    // what a tile needs from memory: base, and the first adapter's first ranks
+    BV base[4];
+    WV w[4];
+    auto load_base = [&](int tile) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            v[i] = columns8<TB, VEC>((const TB *)a.base + clamp_row(row0 + 4 * q + i, a.rows) * a.base_stride, col, a.C);
+            base[i] = buffer_columns<TB, VEC>(base_rows, (4 * q + i) * base_pitch + (128 * tile + 8 * l) * (int)sizeof(TB));
     };
-    auto load_ranks = [&](int adapter, int r0, int64_t col, WV (&v)[4]) {
+    auto load_ranks = [&](int adapter, int r0, int tile) {
+        const __amdgpu_buffer_rsrc_t b = row_buffer((const TW *)a.w + (int64_t)adapter * a.R * C, (uint32_t)a.R * C * sizeof(TW));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            v[i] = columns8<TW, VEC>((const TW *)a.w + ((int64_t)adapter * a.R + min(r0 + element_of<TW>(q, i), a.R - 1)) * a.C, col, a.C);
+            w[i] = buffer_columns<TW, VEC>(b, (int)((uint32_t)((r0 + element_of<TW>(q, i)) * (uint32_t)C + 128 * tile + 8 * l) * (uint32_t)sizeof(TW)));
     };
     const int id = Adapters::load(a.ids, row0, a.rows);
     float factor[4];                                   // without factors any number that can be read
     const float *from = a.base_step ? a.base_step : a.h;
 #pragma unroll
     for (int i = 0; i < 4; ++i) factor[i] = from[a.base_step ? clamp_row(row0 + 4 * q + i, a.rows) : 0];
-    BV base[4];
-    load_base(128 * tile + 8 * l, base);
+    load_base(tile);
     loads_first();
     const Adapters all(id, row0, a.rows, a.adapters, kSecondRows);
     Adapters of = all;
@@ -350,8 +396,7 @@ __global__ __launch_bounds__(256) void k_adapter_second(SecondArgs a)
     uint64_t mine = 0;
     of.next(adapter, mine);
     const int first_adapter = adapter;
-    WV w[4];
-    load_ranks(adapter, 0, 128 * tile + 8 * l, w);
+    load_ranks(adapter, 0, tile);
 
     // H into LDS, its parts added up in order: four elements of a thread and four parts under way.  Sixteen ranks of a row are
     // neighbours, then the rows, then the next sixteen ranks.
@@ -388,11 +433,11 @@ __global__ __launch_bounds__(256) void k_adapter_second(SecondArgs a)
     }
     __syncthreads();
     for (; tile < tiles; tile += stride) {
-        const int64_t col = 128 * tile + 8 * l;
         v8f acc[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i] = a.has_base ? widen(base[i]) * (a.base_step ? factor[i] : 1.0f) : v8f(0);
-        load_base(col + 128 * stride, base);               // of the next tile (of the last columns after the last one)
+        const int after = tile + stride < tiles ? tile + stride : tile;
+        load_base(after);
         of = all;
         bool more = of.next(adapter, mine);
         int r0 = 0;
@@ -401,38 +446,41 @@ __global__ __launch_bounds__(256) void k_adapter_second(SecondArgs a)
             float h[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int r = r0 + element_of<TW>(q, i);
-                now[i] = r < a.R ? w[i] : WV(0);
-                h[i] = hs[l * pitch + r];
+                now[i] = w[i];
+                h[i] = hs[l * pitch + r0 + element_of<TW>(q, i)];
             }
-            const uint64_t rows = mine;
+            const uint64_t own_rows = mine;
             r0 += 16;
             if (r0 >= a.R) {
                 r0 = 0;
                 more = of.next(adapter, mine);
             }
-            load_ranks(more ? adapter : first_adapter, r0, more ? col : col + 128 * stride, w);
+            load_ranks(more ? adapter : first_adapter, r0, more ? tile : after);
             loads_first();
-            v4f y[8];
+            const H16<TW> h16(h);
+            const Columns<TW> columns(now);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = v4f(0);
-            if constexpr (in_thirds<TW>) product16<TW>(thirds(h), now, y);
-            else product16<TW>(h, now, y);
+            for (int j0 = 0; j0 < 8; j0 += 4) {        // four columns' sums at a time
+                v4f y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool own = (rows >> (4 * q + i)) & 1;
+                for (int j = 0; j < 4; ++j) y[j] = v4f(0);
+                product16(h16, columns, j0, y);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[i][j] += own ? y[j][i] : 0.0f;
+                for (int i = 0; i < 4; ++i) {
+                    const bool own = (own_rows >> (4 * q + i)) & 1;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[i][j0 + j] += own ? y[j][i] : 0.0f;
+                }
+                loads_first();
             }
         }
+        const int offset = 4 * q * out_pitch + (128 * tile + 8 * l) * out_size, left = C - (128 * tile + 8 * l);
         if (a.out_type == PWLQ_F32) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (row0 + 4 * q + i < a.rows) store_columns<float>(a.out, (row0 + 4 * q + i) * a.out_stride, col, a.C, acc[i], VEC);
+            for (int i = 0; i < 4; ++i) store_tile<float, VEC>(out_rows, offset + i * out_pitch, left, acc[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (row0 + 4 * q + i < a.rows) store_columns<TW>(a.out, (row0 + 4 * q + i) * a.out_stride, col, a.C, acc[i], VEC);
+            for (int i = 0; i < 4; ++i) store_tile<TW, VEC>(out_rows, offset + i * out_pitch, left, acc[i]);
         }
     }
 }
@@ -609,6 +657,7 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
                     own[i] = first + element_of<TX>(q, i) < count;
                     now.x[i] = own[i] ? now.x[i] : XV(0);
                 }
+                const Columns<TX> columns(now.x);
 #pragma unroll
                 for (int n = 0; n < RT; ++n) {
                     float h[4];
@@ -618,8 +667,7 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
                         if constexpr (sizeof(TX) == 1) h[i] *= now.step[i];
                         h[i] = own[i] ? h[i] : 0.0f;
                     }
-                    if constexpr (in_thirds<TX>) product16<TX>(thirds(h), now.x, acc[n]);
-                    else product16<TX>(h, now.x, acc[n]);
+                    product16(H16<TX>(h), columns, 0, acc[n]);
                 }
             }
         }
@@ -669,7 +717,14 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
                         v8f v;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) v[j] = acc[n][j][i];
-                        if (r < a.R) store_columns<float>(out, (int64_t)r * a.C, col, a.C, v, VEC);
+                        if (r >= a.R) continue;
+                        if constexpr (VEC) {
+                            if (col < a.C) *(v8f *)(out + (int64_t)r * a.C + col) = v;
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (col + j < a.C) out[(int64_t)r * a.C + col + j] = v[j];
+                        }
                     }
                 }
             }
@@ -813,13 +868,12 @@ void first(const FirstArgs &a, int x_type, int w_type, bool vec, hipStream_t str
     else x_type == PWLQ_I8 ? first_as<int8_t, f16>(a, vec, stream) : first_as<f16, f16>(a, vec, stream);
 }
 
-constexpr int64_t kSecondWgs = 512;    // that walk at once
 
 template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipStream_t stream)
 {
     const int64_t tiles = (a.rows + kSecondRows - 1) / kSecondRows, columns = (a.C + 127) / 128;
     const int waves = tiles * columns < 2048 ? 1 : 4;
-    a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, waves == 1 ? columns : (kSecondWgs + tiles - 1) / tiles);
+    a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, waves == 1 ? columns : ((sizeof(TB) == 2 ? 768 : 512) + tiles - 1) / tiles);
     const size_t lds = sizeof(float) * kSecondRows * second_pitch(a.R);
     const unsigned grid = (unsigned)(tiles * a.walks);
     if (vec) k_adapter_second<TW, TB, true><<<grid, 64 * waves, lds, stream>>>(a);

@@ -7,6 +7,7 @@ namespace {
 
 constexpr int64_t kMostRows = 1LL << 26;       // grids of all launches stay below 2^32 threads a dimension
 
+constexpr int64_t kMostStride = 1LL << 24;     // sixteen rows of binary32 stay below 2 GiB
 bool float_type(int type) { return type == PWLQ_F32 || type == PWLQ_BF16 || type == PWLQ_F16; }
 
 // Rows of `cols` columns that have to be there: type (codes only where `codes`), step, stride, alignment to their own elements.
@@ -54,6 +55,9 @@ int check_adapter(int64_t T, int64_t K, int64_t N, int R, int adapters, int type
     if (adapters < 1 || adapters > 65535) return fail(PWLQ_EINVAL, "adapters=%d outside [1,65535]", adapters);
     if (!float_type(type)) return fail(PWLQ_EINVAL, "weight_type=%d is none of the float types", type);
     if ((T + 15) / 16 * ((N > K ? N : K) / 128 + 4) * 64 > 0xffffffffLL) return fail(PWLQ_EINVAL, "grid too large");
+    // rows and adapters are addressed within tiles by 32 bits
+    const int64_t most = (1LL << 31) / pwlq_block::type_size(type);
+    if (R * K >= most || R * N >= most) return fail(PWLQ_EINVAL, "an adapter of 2 GiB or more");
     if (!down || !up || !scale || (T && !ids)) return fail(PWLQ_ENULL, "an input pointer is NULL");
     if (((uintptr_t)down | (uintptr_t)up) % (uintptr_t)pwlq_block::type_size(type) != 0)
         return fail(PWLQ_EINVAL, "down or up is not aligned to its elements");
@@ -63,6 +67,7 @@ int check_adapter(int64_t T, int64_t K, int64_t N, int R, int adapters, int type
 int check_columns(const char *name, const pwlq_rows &r, int64_t cols, int weight_type, bool codes = false, bool row_factors = false)
 {
     if (int rc = check_rows(name, r, cols, codes, row_factors)) return rc;
+    if (r.stride > kMostStride) return fail(PWLQ_EINVAL, "%s: a stride of %lld, over %lld", name, (long long)r.stride, (long long)kMostStride);
     if (r.type != weight_type && r.type != (codes ? PWLQ_I8 : PWLQ_F32))
         return fail(PWLQ_EINVAL, "%s has type %d beside weights of type %d", name, r.type, weight_type);
     return PWLQ_OK;

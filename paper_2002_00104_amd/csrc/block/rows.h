@@ -44,13 +44,14 @@ template <typename T> __device__ inline void store8(T *p, v8f v)
     *(typename Vec8<T>::type *)p = __builtin_convertvector(v, typename Vec8<T>::type);
 }
 
-// A row as a buffer of its own length: reads beyond its end give 0 and writes there do nothing, by the hardware's bounds
-// check, so threads past the end need no branch and no select.  `row` is the same for the whole wavefront.
-__device__ inline __amdgpu_buffer_rsrc_t row_buffer(const void *row, int bytes)
+// A row, or neighbouring rows, as a buffer of their own length: reads beyond its end give 0 and writes there do nothing, by the
+// hardware's bounds check, so threads past the end need no branch and no select.  `row` is the same for the whole wavefront.
+__device__ inline __amdgpu_buffer_rsrc_t row_buffer(const void *row, uint32_t bytes)
 {
-    return __builtin_amdgcn_make_buffer_rsrc((void *)row, 0, bytes, 0x00027000);
+    return __builtin_amdgcn_make_buffer_rsrc((void *)row, 0, (int)bytes, 0x00027000);
 }
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+// Offsets in bytes.
 template <typename T> __device__ inline typename Vec8<T>::type buffer_load8(__amdgpu_buffer_rsrc_t b, int offset)
 {
     union { v4u w[sizeof(T) == 4 ? 2 : 1]; v2u half; typename Vec8<T>::type v; } u;
