@@ -646,10 +646,13 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
             };
             int first = 16 * wave;
             if (first >= count) continue;
-            Rows now, after;
+            // one step ahead with sixteen ranks, whose workgroups are four to a CU, two steps ahead with 32 (two to a CU);
+            // beyond the list its last row is read and not used
+            Rows now, after, later;
             load(first, now);
-            for (; first < count; first += 64, now = after) {
-                load(first + 64, after);                   // beyond the list: its last row, not used
+            if (RT > 1) load(first + 64, after);
+            for (; first < count; first += 64) {
+                load(first + 64 * RT, RT > 1 ? later : after);
                 loads_first();
                 bool own[4];
 #pragma unroll
@@ -669,6 +672,8 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
                     }
                     product16(H16<TX>(h), columns, 0, acc[n]);
                 }
+                now = after;
+                if (RT > 1) after = later;
             }
         }
 #pragma unroll
@@ -735,7 +740,7 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
 
 // Both gradients in one launch: the second fills the chip while the first one's last workgroups end.
 template <typename TX, typename TY, int RT, bool VEC>
-__global__ __launch_bounds__(256, 3) void k_adapter_outer(OuterArgs up, OuterArgs down)
+__global__ __launch_bounds__(256, RT == 1 && VEC && sizeof(TY) == 2 ? 4 : 2) void k_adapter_outer(OuterArgs up, OuterArgs down)
 {
     __shared__ OuterLds<RT> lds;
     const int ups = up.column_tiles * up.rank_blocks;
@@ -800,12 +805,12 @@ int first_splits(int64_t T, int64_t K, int R)
 }
 int64_t first_chunk(int64_t K, int splits) { return ((K + splits - 1) / splits + 255) / 256 * 256; }
 
-// Parts of the rows for the outer products: three workgroups to each CU.
+// Parts of the rows for the outer products: as many workgroups as are resident.
 int outer_blocks(int R) { return R <= 16 ? 1 : (R + 31) / 32; }
 int64_t outer_span(int64_t T, int64_t K, int64_t N, int R)
 {
     const int64_t wgs = ((K + 127) / 128 + (N + 127) / 128) * outer_blocks(R);
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(768 / wgs, (T + 63) / 64));
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((R <= 16 ? 1024 : 512) / wgs, (T + 63) / 64));
     return ((T + splits - 1) / splits + 63) / 64 * 64;
 }
 int outer_splits(int64_t T, int64_t K, int64_t N, int R)
