@@ -62,33 +62,31 @@ __device__ inline v4f multiply(v8f x, v8f w, v4f acc)
     return acc;
 }
 
-// Eight elements from column `col` on, without a branch, so that several loads can be under way: columns beyond the last are
-// read from it.
+// Eight elements from column `col` on.  A vector that would reach past the row's end is the row's last eight instead, shifted by
+// beyond(): in place of a branch, so that several loads can be under way, and nothing past the end is read.  Rows shorter than a
+// vector go element by element (VEC false).
+__device__ inline int64_t start_of(int64_t col, int64_t cols) { return min(col, cols - 8); }
+__device__ inline int beyond(int64_t col, int64_t cols) { return (int)min(col - start_of(col, cols), (int64_t)8); }
 template <typename T, bool VEC> __device__ inline typename Vec8<T>::type columns8(const T *row, int64_t col, int64_t cols)
 {
-    typedef typename Vec8<T>::type V;
-    if constexpr (VEC) return *(const V *)(row + min(col, cols - 8));
+    if constexpr (VEC) return load8(row + start_of(col, cols));
     else {
-        union { V v; T e[8]; } u;
+        union { typename Vec8<T>::type v; T e[8]; } u;
 #pragma unroll
         for (int i = 0; i < 8; ++i) u.e[i] = row[min(col + i, cols - 1)];
         return u.v;
     }
 }
-// Of those eight, the ones before `end`, and 0 for the others: elements of a reduction.
-template <typename T, bool VEC> __device__ inline typename Vec8<T>::type before(typename Vec8<T>::type v, int64_t col, int64_t end)
+// Of such a vector the elements of a reduction: those from `col` on and before `end` (which ends the row or a run of vectors), 0
+// for the others, each element once in all.
+template <typename T, bool VEC> __device__ inline typename Vec8<T>::type only(typename Vec8<T>::type v, int64_t col, int64_t end, int64_t cols)
 {
-    typedef typename Vec8<T>::type V;
-    if constexpr (VEC) return col < end ? v : V(0);
-    union { V v; T e[8]; } u;
+    union { typename Vec8<T>::type v; T e[8]; } u;
     u.v = v;
+    const int skip = VEC ? (col < end ? beyond(col, cols) : 8) : 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u.e[i] = col + i < end ? u.e[i] : T(0);
+    for (int i = 0; i < 8; ++i) u.e[i] = VEC ? (i >= skip ? u.e[i] : T(0)) : (col + i < end ? u.e[i] : T(0));
     return u.v;
-}
-template <typename T, bool VEC> __device__ inline typename Vec8<T>::type piece(const T *row, int64_t col, int64_t cols)
-{
-    return before<T, VEC>(columns8<T, VEC>(row, col, cols), col, cols);
 }
 
 struct FirstArgs {
@@ -153,9 +151,9 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
                 for (int half = 0; half < 2; ++half) {
                     const int64_t c = k + 256 * b + half_at<TX>(q, half);
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) x[b][half][m] = whole ? *(const XV *)(xr[m] + c) : columns8<TX, VEC>(xr[m], c, a.K);
+                    for (int m = 0; m < 2; ++m) x[b][half][m] = whole ? load8(xr[m] + c) : columns8<TX, VEC>(xr[m], c, a.K);
 #pragma unroll
-                    for (int n = 0; n < RT; ++n) w[b][half][n] = whole ? *(const WV *)(wr[n] + c) : columns8<TW, VEC>(wr[n], c, a.K);
+                    for (int n = 0; n < RT; ++n) w[b][half][n] = whole ? load8(wr[n] + c) : columns8<TW, VEC>(wr[n], c, a.K);
                 }
             loads_first();
             if constexpr (!whole) {
@@ -165,9 +163,9 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
                     for (int half = 0; half < 2; ++half) {
                         const int64_t c = k + 256 * b + half_at<TX>(q, half);
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) x[b][half][m] = before<TX, VEC>(x[b][half][m], c, k1);
+                        for (int m = 0; m < 2; ++m) x[b][half][m] = only<TX, VEC>(x[b][half][m], c, k1, a.K);
 #pragma unroll
-                        for (int n = 0; n < RT; ++n) w[b][half][n] = before<TW, VEC>(w[b][half][n], c, k1);
+                        for (int n = 0; n < RT; ++n) w[b][half][n] = only<TW, VEC>(w[b][half][n], c, k1, a.K);
                     }
             }
 #pragma unroll
@@ -328,7 +326,7 @@ struct SecondArgs {
 constexpr int kSecondRows = 16;
 __host__ __device__ inline int second_pitch(int R) { return (R + 15) / 16 * 16 + 1; }
 
-// Eight columns at once or one by one; those beyond the last belong to no output, whatever is read there.
+// Eight columns at once or one by one, from a byte offset on.
 template <typename T, bool VEC> __device__ inline typename Vec8<T>::type buffer_columns(__amdgpu_buffer_rsrc_t b, int offset)
 {
     if constexpr (VEC) return buffer_load8<T>(b, offset);
@@ -339,14 +337,14 @@ template <typename T, bool VEC> __device__ inline typename Vec8<T>::type buffer_
         return u.v;
     }
 }
-template <typename T, bool VEC> __device__ inline void store_tile(__amdgpu_buffer_rsrc_t b, int offset, int columns, v8f v)
+// Of eight columns those from the first `skip` on, and at most `columns`.
+template <typename T, bool VEC> __device__ inline void store_tile(__amdgpu_buffer_rsrc_t b, int offset, int skip, int columns, v8f v)
 {
-    if constexpr (VEC) {
-        if (columns > 0) buffer_store8<T>(b, offset, __builtin_convertvector(v, typename Vec8<T>::type));
-    } else {
+    if (VEC && skip == 0) buffer_store8<T>(b, offset, __builtin_convertvector(v, typename Vec8<T>::type));
+    else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i < columns) buffer_store1<T>(b, offset + i * (int)sizeof(T), (T)v[i]);
+            if (i >= skip && i < columns) buffer_store1<T>(b, offset + i * (int)sizeof(T), (T)v[i]);
     }
 }
 
@@ -369,19 +367,21 @@ __global__ __launch_bounds__(256, sizeof(TB) == 2 && VEC ? 3 : 2) void k_adapter
     const __amdgpu_buffer_rsrc_t out_rows =
         row_buffer((char *)a.out + row0 * a.out_stride * out_size, (rows - 1) * out_pitch + C * out_size);
 
+    // a lane's first column in a tile; the last vector of a row that is no whole number of them starts further left
+    auto column = [&](int tile) { return VEC ? (int)start_of(128 * tile + 8 * l, C) : 128 * tile + 8 * l; };
     // what a tile needs from memory: base, and the first adapter's first ranks
     BV base[4];
     WV w[4];
     auto load_base = [&](int tile) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            base[i] = buffer_columns<TB, VEC>(base_rows, (4 * q + i) * base_pitch + (128 * tile + 8 * l) * (int)sizeof(TB));
+            base[i] = buffer_columns<TB, VEC>(base_rows, (4 * q + i) * base_pitch + column(tile) * (int)sizeof(TB));
     };
     auto load_ranks = [&](int adapter, int r0, int tile) {
         const __amdgpu_buffer_rsrc_t b = row_buffer((const TW *)a.w + (int64_t)adapter * a.R * C, (uint32_t)a.R * C * sizeof(TW));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            w[i] = buffer_columns<TW, VEC>(b, (int)((uint32_t)((r0 + element_of<TW>(q, i)) * (uint32_t)C + 128 * tile + 8 * l) * (uint32_t)sizeof(TW)));
+            w[i] = buffer_columns<TW, VEC>(b, (int)((uint32_t)((r0 + element_of<TW>(q, i)) * (uint32_t)C + column(tile)) * (uint32_t)sizeof(TW)));
     };
     const int id = Adapters::load(a.ids, row0, a.rows);
     float factor[4];                                   // without factors any number that can be read
@@ -474,13 +474,14 @@ __global__ __launch_bounds__(256, sizeof(TB) == 2 && VEC ? 3 : 2) void k_adapter
                 loads_first();
             }
         }
-        const int offset = 4 * q * out_pitch + (128 * tile + 8 * l) * out_size, left = C - (128 * tile + 8 * l);
+        const int offset = 4 * q * out_pitch + column(tile) * out_size, left = C - column(tile);
+        const int skip = VEC ? beyond(128 * tile + 8 * l, C) : 0;
         if (a.out_type == PWLQ_F32) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) store_tile<float, VEC>(out_rows, offset + i * out_pitch, left, acc[i]);
+            for (int i = 0; i < 4; ++i) store_tile<float, VEC>(out_rows, offset + i * out_pitch, skip, left, acc[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) store_tile<TW, VEC>(out_rows, offset + i * out_pitch, left, acc[i]);
+            for (int i = 0; i < 4; ++i) store_tile<TW, VEC>(out_rows, offset + i * out_pitch, skip, left, acc[i]);
         }
     }
 }
@@ -520,7 +521,7 @@ __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
     v8f y = v8f(0);
     if (id >= 0 && id < a.adapters) {
         const TW *up = (const TW *)a.up + (int64_t)id * a.R * a.C;
-        const WV ahead = piece<TW, VEC>(up + (int64_t)min(wave, a.R - 1) * a.C, col, a.C);
+        const WV ahead = columns8<TW, VEC>(up + (int64_t)min(wave, a.R - 1) * a.C, col, a.C);
         const TX *x = (const TX *)a.x + row * a.x_stride;
         const float scale = a.x_step ? a.scale[id] * a.x_step[row] : a.scale[id];
         for (int r = wave; r < a.R; r += kTokenWaves) {
@@ -528,25 +529,31 @@ __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
             v8f t = v8f(0);
             int64_t k = 0;
             if constexpr (VEC) {
-                // vectors beyond the row are read from its last one and count nothing
                 for (; k < a.K; k += 512 * kAhead) {
                     XV xv[kAhead];
                     WV wv[kAhead];
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) {
-                        const int64_t c = min(k + 512 * i + 8 * lane, a.K - 8);
-                        xv[i] = *(const XV *)(x + c);
-                        wv[i] = *(const WV *)(w + c);
+                        const int64_t c = start_of(k + 512 * i + 8 * lane, a.K);
+                        xv[i] = load8(x + c);
+                        wv[i] = load8(w + c);
                     }
                     loads_first();
+                    if (k + 512 * kAhead <= a.K) {
 #pragma unroll
-                    for (int i = 0; i < kAhead; ++i) {
-                        const v8f p = widen(xv[i]) * widen(wv[i]);
-                        t += k + 512 * i + 8 * lane < a.K ? p : v8f(0);
+                        for (int i = 0; i < kAhead; ++i) t += widen(xv[i]) * widen(wv[i]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kAhead; ++i) {
+                            const v8f p = widen(xv[i]) * widen(wv[i]);
+                            const int skip = beyond(k + 512 * i + 8 * lane, a.K);      // 8 past the row's end
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) t[j] += j >= skip ? p[j] : 0.0f;
+                        }
                     }
                 }
             } else {
-                for (k = 8 * lane; k < a.K; k += 512) t += widen(piece<TX, VEC>(x, k, a.K)) * widen(piece<TW, VEC>(w, k, a.K));
+                for (k = lane; k < a.K; k += 64) t[0] += widen(x[k]) * widen(w[k]);
             }
             const float s = wave_sum(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
             if (lane == 0) hs[r] = s * scale;
@@ -554,11 +561,17 @@ __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
         __syncthreads();
         if (blockIdx.x == 0 && threadIdx.x < a.R) a.h[row * a.R + threadIdx.x] = hs[threadIdx.x];
         if (wave < a.R) y = hs[wave] * widen(ahead);
-        for (int r = wave + kTokenWaves; r < a.R; r += kTokenWaves) y += hs[r] * widen(piece<TW, VEC>(up + (int64_t)r * a.C, col, a.C));
+        for (int r = wave + kTokenWaves; r < a.R; r += kTokenWaves) y += hs[r] * widen(columns8<TW, VEC>(up + (int64_t)r * a.C, col, a.C));
     } else if (blockIdx.x == 0 && threadIdx.x < a.R) {
         a.h[row * a.R + threadIdx.x] = 0.0f;
     }
-    sums[wave][lane] = y;
+    const int skip = VEC ? beyond(col, a.C) : 0;       // columns that belong to the lane before
+    if (skip == 0) sums[wave][lane] = y;
+    else {
+#pragma unroll
+        for (int j = 1; j < 8; ++j)
+            if (j >= skip) ((float *)&sums[wave][lane])[j - skip] = y[j];
+    }
     __syncthreads();
     if (threadIdx.x >= kTokenColumns || col0 + threadIdx.x >= a.C) return;
     float s = 0.0f;
@@ -578,7 +591,7 @@ struct OuterArgs {
     int64_t stride, rows, C, span;     // span: rows of a workgroup
     const float *step;
     const int32_t *ids;
-    int R, adapters, column_tiles, rank_blocks;
+    int R, adapters, column_tiles, rank_blocks, slots;
     float *out;                        // [splits, adapters, R, C]
     int32_t *present;                  // [splits, adapters]: whether the part has rows of the adapter; NULL where there is one part
     bool flags;                        // whether this product writes them: both have the same rows
@@ -594,7 +607,8 @@ template <int RT> struct OuterLds {
     int list[kListed];
 };
 
-template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const OuterArgs &a, int tile, int split, OuterLds<RT> &lds)
+// `slot`: of a.slots (a power of two) workgroups that share the adapters of these rows, by their lowest bits.
+template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const OuterArgs &a, int tile, int split, int slot, OuterLds<RT> &lds)
 {
     typedef typename Vec8<TX>::type XV;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
@@ -608,9 +622,9 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
     float *const part = a.out + (int64_t)split * a.adapters * a.R * a.C;
     int32_t *const present = a.present && a.flags && tile == 0 ? a.present + (int64_t)split * a.adapters : nullptr;
     if (present)
-        for (int i = threadIdx.x; i < a.adapters; i += 256) present[i] = 0;
+        for (int i = slot + threadIdx.x * a.slots; i < a.adapters; i += 256 * a.slots) present[i] = 0;
     v4f acc[RT][8];
-    for (int adapter = -1, next;; adapter = next) {
+    for (int adapter = slot - a.slots, next;; adapter = next) {
         next = a.adapters;
 #pragma unroll
         for (int n = 0; n < RT; ++n)
@@ -623,7 +637,7 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
             loads_first();
 #pragma unroll
             for (int g = 0; g < kListed / 64; ++g)
-                if (id[g] > adapter) next = min(next, id[g]);
+                if (id[g] > adapter && (id[g] & (a.slots - 1)) == slot) next = min(next, id[g]);
             if (adapter < 0) continue;
             int count = 0;
             __syncthreads();
@@ -681,14 +695,14 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
         next = __builtin_amdgcn_readfirstlane(next);
         // adapters without rows here: nothing in a part, zeros where there are no parts
         if (!a.present)
-            for (int none = adapter + 1; none < next; ++none)
+            for (int none = adapter + a.slots; none < next; none += a.slots)
                 for (int i = threadIdx.x; i < 16 * RT * 128; i += 256) {
                     const int r = r0 + i / 128;
                     const int64_t c = (int64_t)(tile % a.column_tiles) * 128 + i % 128;
                     if (r < a.R && c < a.C) part[((int64_t)none * a.R + r) * a.C + c] = 0.0f;
                 }
         if (adapter >= 0) {
-            if (present && (int)threadIdx.x == adapter % 256) present[adapter] = 1;
+            if (present && (int)threadIdx.x == adapter / a.slots % 256) present[adapter] = 1;
             if (wave >= 2) {
 #pragma unroll
                 for (int n = 0; n < RT; ++n)
@@ -724,7 +738,7 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
                         for (int j = 0; j < 8; ++j) v[j] = acc[n][j][i];
                         if (r >= a.R) continue;
                         if constexpr (VEC) {
-                            if (col < a.C) *(v8f *)(out + (int64_t)r * a.C + col) = v;
+                            if (col < a.C) store8(out + (int64_t)r * a.C + start_of(col, a.C), v);     // columns of two vectors: the same sums twice
                         } else {
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
@@ -744,8 +758,8 @@ __global__ __launch_bounds__(256, RT == 1 && VEC && sizeof(TY) == 2 ? 4 : 2) voi
 {
     __shared__ OuterLds<RT> lds;
     const int ups = up.column_tiles * up.rank_blocks;
-    if ((int)blockIdx.x < ups) outer_tile<TY, RT, VEC>(up, blockIdx.x, blockIdx.y, lds);
-    else outer_tile<TX, RT, VEC>(down, blockIdx.x - ups, blockIdx.y, lds);
+    if ((int)blockIdx.x < ups) outer_tile<TY, RT, VEC>(up, blockIdx.x, blockIdx.y, blockIdx.z, lds);
+    else outer_tile<TX, RT, VEC>(down, blockIdx.x - ups, blockIdx.y, blockIdx.z, lds);
 }
 
 // Parts of both gradients added up in order.
@@ -819,6 +833,15 @@ int outer_splits(int64_t T, int64_t K, int64_t N, int R)
     return (int)((T + span - 1) / span);
 }
 
+// Where that leaves CUs idle the adapters are done beside each other.
+int outer_slots(int64_t T, int64_t K, int64_t N, int R, int adapters)
+{
+    const int64_t wgs = ((K + 127) / 128 + (N + 127) / 128) * outer_blocks(R) * outer_splits(T, K, N, R);
+    int slots = 1;
+    while (2 * slots <= adapters && 2 * slots * wgs <= 1024) slots *= 2;
+    return slots;
+}
+
 struct Carver {                        // offsets of a workspace's parts, 256-byte aligned
     char *base;
     size_t at = 0;
@@ -877,8 +900,9 @@ void first(const FirstArgs &a, int x_type, int w_type, bool vec, hipStream_t str
 template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipStream_t stream)
 {
     const int64_t tiles = (a.rows + kSecondRows - 1) / kSecondRows, columns = (a.C + 127) / 128;
-    const int waves = tiles * columns < 2048 ? 1 : 4;
-    a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, waves == 1 ? columns : ((sizeof(TB) == 2 ? 768 : 512) + tiles - 1) / tiles);
+    const int waves = (int)std::min<int64_t>(columns, 4);
+    // as many workgroups as are resident walk at once
+    a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, ((sizeof(TB) == 2 ? 768 : 512) + tiles - 1) / tiles);
     const size_t lds = sizeof(float) * kSecondRows * second_pitch(a.R);
     const unsigned grid = (unsigned)(tiles * a.walks);
     if (vec) k_adapter_second<TW, TB, true><<<grid, 64 * waves, lds, stream>>>(a);
@@ -900,7 +924,7 @@ void second(SecondArgs a, int w_type, int base_type, bool vec, hipStream_t strea
 
 template <typename TX, typename TY> void outer_as(const OuterArgs &up, const OuterArgs &down, int splits, bool vec, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(up.column_tiles * up.rank_blocks + down.column_tiles * down.rank_blocks), splits);
+    const dim3 grid((unsigned)(up.column_tiles * up.rank_blocks + down.column_tiles * down.rank_blocks), splits, up.slots);
 #define PWLQ_OUTER(RT)                                                                          \
     do {                                                                                        \
         if (vec) k_adapter_outer<TX, TY, RT, true><<<grid, 256, 0, stream>>>(up, down);         \
@@ -917,8 +941,6 @@ void outer(const OuterArgs &up, const OuterArgs &down, int splits, int x_type, i
     else if (w_type == PWLQ_BF16) x_type == PWLQ_I8 ? outer_as<int8_t, bf16>(up, down, splits, vec, stream) : outer_as<bf16, bf16>(up, down, splits, vec, stream);
     else x_type == PWLQ_I8 ? outer_as<int8_t, f16>(up, down, splits, vec, stream) : outer_as<f16, f16>(up, down, splits, vec, stream);
 }
-
-bool whole_vectors(int64_t C, const void *w) { return C % 8 == 0 && aligned16(w); }
 
 // Whether few rows go through one launch.
 bool by_token(int64_t T, int R) { return T <= kTokenRows && R <= kTokenRanks; }
@@ -952,7 +974,7 @@ void token(const pwlq_adapter_args &a, hipStream_t stream)
     t.adapters = a.adapters;
     t.base_type = a.base.type;
     t.out_type = a.out.type;
-    const bool vec = whole_vectors(a.K, a.down) && whole_vectors(a.N, a.up) && vectors(a.x, a.T), packed = a.x.type == PWLQ_I8;
+    const bool vec = a.K >= 8 && a.N >= 8, packed = a.x.type == PWLQ_I8;
     if (a.weight_type == PWLQ_F32) packed ? token_as<int8_t, float>(t, a.T, vec, stream) : token_as<float, float>(t, a.T, vec, stream);
     else if (a.weight_type == PWLQ_BF16) packed ? token_as<int8_t, bf16>(t, a.T, vec, stream) : token_as<bf16, bf16>(t, a.T, vec, stream);
     else packed ? token_as<int8_t, f16>(t, a.T, vec, stream) : token_as<f16, f16>(t, a.T, vec, stream);
@@ -988,7 +1010,7 @@ void adapter_forward(const pwlq_adapter_args &a, void *workspace, hipStream_t st
     f.adapters = a.adapters;
     const int parts = (int)((a.K + f.chunk - 1) / f.chunk);
     f.out = parts > 1 ? (float *)workspace : a.h;
-    first(f, a.x.type, a.weight_type, whole_vectors(a.K, a.down) && vectors(a.x, a.T), stream);
+    first(f, a.x.type, a.weight_type, a.K >= 8, stream);
     SecondArgs s = {};
     s.h = f.out;
     s.h_out = parts > 1 ? a.h : nullptr;
@@ -1005,7 +1027,7 @@ void adapter_forward(const pwlq_adapter_args &a, void *workspace, hipStream_t st
     s.splits = parts;
     s.adapters = a.adapters;
     s.out_type = a.out.type;
-    second(s, a.weight_type, a.base.type, whole_vectors(a.N, a.up) && vectors(a.base, a.T) && vectors(a.out, a.T), stream);
+    second(s, a.weight_type, a.base.type, a.N >= 8, stream);
 }
 
 size_t adapter_backward_workspace(int64_t T, int64_t K, int64_t N, int R, int adapters)
@@ -1033,7 +1055,7 @@ void adapter_backward(const pwlq_adapter_backward_args &a, void *workspace, hipS
     f.adapters = a.adapters;
     const int parts = (int)((a.N + f.chunk - 1) / f.chunk);
     f.out = parts > 1 ? space.parts : space.dh;
-    first(f, a.dy.type, a.weight_type, whole_vectors(a.N, a.up) && vectors(a.dy, a.T), stream);
+    first(f, a.dy.type, a.weight_type, a.N >= 8, stream);
     SecondArgs s = {};
     s.h = f.out;
     s.h_out = parts > 1 ? space.dh : nullptr;
@@ -1050,7 +1072,7 @@ void adapter_backward(const pwlq_adapter_backward_args &a, void *workspace, hipS
     s.adapters = a.adapters;
     s.out_type = a.dx.type;
     second(s, a.weight_type, a.dx_base.type,
-           whole_vectors(a.K, a.down) && vectors(a.dx_base, a.T) && vectors(a.dx, a.T), stream);
+           a.K >= 8, stream);
     OuterArgs up = {}, down = {};
     up.rows = down.rows = a.T;
     up.span = down.span = outer_span(a.T, a.K, a.N, a.R);
@@ -1058,6 +1080,7 @@ void adapter_backward(const pwlq_adapter_backward_args &a, void *workspace, hipS
     up.R = down.R = a.R;
     up.adapters = down.adapters = a.adapters;
     up.rank_blocks = down.rank_blocks = outer_blocks(a.R);
+    up.slots = down.slots = outer_slots(a.T, a.K, a.N, a.R, a.adapters);
     up.h = a.h;
     up.x = a.dy.data;
     up.stride = a.dy.stride;
@@ -1075,7 +1098,7 @@ void adapter_backward(const pwlq_adapter_backward_args &a, void *workspace, hipS
     up.present = down.present = join ? space.present : nullptr;
     up.flags = true;
     outer(up, down, space.splits, a.x.type, a.weight_type,
-          whole_vectors(a.N, up.out) && whole_vectors(a.K, down.out) && vectors(a.x, a.T) && vectors(a.dy, a.T), stream);
+          a.K >= 8 && a.N >= 8, stream);
     if (!join) return;
     JoinArgs j = {};
     j.part[0] = space.down;

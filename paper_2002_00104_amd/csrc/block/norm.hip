@@ -86,18 +86,22 @@ __global__ __launch_bounds__(THREADS) void k_norm_block(pwlq_norm_args a)
     }
 }
 
-// Partial sums of the parameters' gradients: workgroup w walks the rows [w span, (w + 1) span) and keeps a sum per column
-// in registers; the next launch adds the workgroups' sums in order, so a gradient does not depend on timing.  A
-// gate of several rows changes inside the walk.  A gate row whose rows all lie in it is written to d_gate; else the sums
-// of workgroup w for gate row g are partial row w + g, one of its own for each pair, since from a pair to the next one of the two grows.
+// Partial sums of the parameters' gradients: walk w takes the rows [w span, (w + 1) span) and keeps a sum per column in
+// registers; the next launch adds the walks' sums in order, so a gradient does not depend on timing.  Rows of up to 512 columns
+// take a wavefront each, and the four walks of a workgroup first add theirs up in LDS.  A gate of several rows changes inside a
+// walk.  A gate row whose rows all lie in it is written to d_gate; else the sums of walk w for gate row g are partial row w + g,
+// one of its own for each pair, since from a pair to the next one of the two grows.
 struct NormPartials {
-    float *pre, *post, *gate;      // [workgroups, D], [workgroups, D], [workgroups + gate_rows, D]
+    float *pre, *post, *gate;      // [workgroups, D], [workgroups, D], [workgroups * walks + gate_rows, D]
     int64_t span;
+    int walks;                     // of a workgroup
 };
+constexpr int kWalks = 4, kWalkColumns = 512;
 
-__device__ inline float *gate_sums(const pwlq_norm_backward_args &a, const NormPartials &part, int64_t g, int64_t per, int64_t first, int64_t last)
+__device__ inline float *gate_sums(const pwlq_norm_backward_args &a, const NormPartials &part, int64_t walk, int64_t g, int64_t per,
+                                   int64_t first, int64_t last)
 {
-    return (g * per >= first && (g + 1) * per <= last ? a.d_gate + g * a.D : part.gate + ((int64_t)blockIdx.x + g) * a.D);
+    return (g * per >= first && (g + 1) * per <= last ? a.d_gate + g * a.D : part.gate + (walk + g) * a.D);
 }
 
 // What vector instructions there are per element bounds this as much as memory, so a row's factors are joined before they meet
@@ -109,10 +113,12 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
     typedef typename std::conditional<KEPT, int8_t, TF>::type SF;
     typedef typename std::conditional<KEPT, int8_t, TX>::type SX;
     __shared__ float2 slots[2][2][16];
-    const int threads = blockDim.x, thread = threadIdx.x, D = (int)a.D;
+    // a walk's threads: the whole workgroup, or one of its wavefronts
+    const int threads = part.walks == 1 ? blockDim.x : 64, thread = part.walks == 1 ? threadIdx.x : threadIdx.x & 63, D = (int)a.D;
+    const int64_t walk = (int64_t)blockIdx.x * part.walks + (part.walks == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
     const float inv = 1.0f / (float)D;
     const int64_t per_gate = a.gate ? a.T / a.gate_rows : a.T;
-    const int64_t first = (int64_t)blockIdx.x * part.span, last = min(first + part.span, a.T);
+    const int64_t first = walk * part.span, last = min(first + part.span, a.T);
     float pre[E], back[E], sum_pre[E], sum_post[E], sum_f[E];      // back: alpha gate post
 #pragma unroll
     for (int i = 0; i < E; ++i) sum_pre[i] = sum_post[i] = sum_f[i] = 0.0f;
@@ -151,7 +157,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
             sum_post[i] += g[i] * sum_f[i];
             sum_f[i] *= a.alpha * p[i];
         }
-        if (a.gate) store_row<float, E, VEC>(gate_sums(a, part, gate_row, per_gate, first, last), D, threads, thread, sum_f);
+        if (a.gate) store_row<float, E, VEC>(gate_sums(a, part, walk, gate_row, per_gate, first, last), D, threads, thread, sum_f);
 #pragma unroll
         for (int i = 0; i < E; ++i) sum_f[i] = 0.0f;
     };
@@ -160,7 +166,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
         weight.load(a.pre_weight, D, threads, thread);
         weight.get(pre);
     }
-    load(first);
+    if (first < last) load(first);
     int64_t at_gate = -1;
     int turn = 0;
     for (int64_t row = first; row < last; ++row, turn ^= 1) {
@@ -225,6 +231,28 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
         store_row<TF, E, VEC>((TF *)a.df.data + row * a.df.stride, D, threads, thread, dx);
     }
     if (at_gate >= 0) settle(at_gate);
+    if constexpr (E == 8) {
+        if (part.walks > 1) {                          // the other walks' sums, in order
+            __shared__ float sums[kWalks - 1][2][kWalkColumns];
+            const int wave = threadIdx.x >> 6;
+            if (wave) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    sums[wave - 1][0][64 * i + thread] = sum_pre[i];
+                    sums[wave - 1][1][64 * i + thread] = sum_post[i];
+                }
+            }
+            __syncthreads();
+            if (wave) return;
+#pragma unroll
+            for (int w = 0; w < kWalks - 1; ++w)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    sum_pre[i] += sums[w][0][64 * i + thread];
+                    sum_post[i] += sums[w][1][64 * i + thread];
+                }
+        }
+    }
     store_row<float, E, VEC>(part.pre + (int64_t)blockIdx.x * a.D, D, threads, thread, sum_pre);
     if (part.post) store_row<float, E, VEC>(part.post + (int64_t)blockIdx.x * a.D, D, threads, thread, sum_post);
 }
@@ -285,10 +313,17 @@ __global__ void k_zero(float *a, int64_t na, float *b, int64_t nb, float *c, int
 int forward_elements(int64_t D) { return D <= 4096 ? 8 : 16; }
 int backward_elements(int64_t D) { return D <= 2048 ? 8 : 16; }
 
+int backward_walks(int64_t D) { return D <= kWalkColumns ? kWalks : 1; }
+// Rows of a walk: two at least, since what a walk leaves behind is read again.
 int64_t backward_span(int64_t T, int64_t D)
 {
-    const int64_t wgs = kBackwardWaves / (threads_for(D, backward_elements(D)) / 64);
-    return (T + wgs - 1) / wgs;
+    const int64_t walks = kBackwardWaves / (threads_for(D, backward_elements(D)) / 64);
+    return std::max<int64_t>((T + walks - 1) / walks, 2);
+}
+int64_t backward_wgs(int64_t T, int64_t D)
+{
+    const int64_t rows = backward_span(T, D) * backward_walks(D);
+    return (T + rows - 1) / rows;
 }
 
 template <typename TF, typename TX> void norm_as(const pwlq_norm_args &a, bool vec, hipStream_t stream)
@@ -307,9 +342,10 @@ template <typename TF, typename TX> void norm_as(const pwlq_norm_args &a, bool v
 template <typename TF, typename TX, bool KEPT>
 void backward_as(const pwlq_norm_backward_args &a, const NormPartials &part, unsigned grid, bool vec, hipStream_t stream)
 {
+    const int threads = part.walks * threads_for(a.D, backward_elements(a.D));
 #define PWLQ_NORM(E, THREADS)                                                                                            \
-    (vec ? k_norm_backward<TF, TX, KEPT, E, true, THREADS><<<grid, threads_for(a.D, E), 0, stream>>>(a, part)            \
-         : k_norm_backward<TF, TX, KEPT, E, false, THREADS><<<grid, threads_for(a.D, E), 0, stream>>>(a, part))
+    (vec ? k_norm_backward<TF, TX, KEPT, E, true, THREADS><<<grid, threads, 0, stream>>>(a, part)            \
+         : k_norm_backward<TF, TX, KEPT, E, false, THREADS><<<grid, threads, 0, stream>>>(a, part))
     if (a.D <= 2048) PWLQ_NORM(8, 256);
     else if (a.D <= 8192) PWLQ_NORM(16, 512);
     else PWLQ_NORM(16, 1024);
@@ -334,8 +370,7 @@ void norm_block(const pwlq_norm_args &a, hipStream_t stream)
 size_t norm_backward_workspace(int64_t T, int64_t D, int64_t gate_rows)
 {
     if (!T) return 0;
-    const int64_t wgs = (T + backward_span(T, D) - 1) / backward_span(T, D);
-    return (size_t)(3 * wgs + gate_rows) * (size_t)D * sizeof(float);
+    return (size_t)(backward_wgs(T, D) * (2 + backward_walks(D)) + gate_rows) * (size_t)D * sizeof(float);
 }
 
 void norm_backward(const pwlq_norm_backward_args &a, void *workspace, hipStream_t stream)
@@ -345,9 +380,9 @@ void norm_backward(const pwlq_norm_backward_args &a, void *workspace, hipStream_
         k_zero<<<256, 256, 0, stream>>>(a.d_pre, a.d_pre ? a.D : 0, a.d_post, a.d_post ? a.D : 0, a.d_gate, n);
         return;
     }
-    const int64_t span = backward_span(a.T, a.D), wgs = (a.T + span - 1) / span;
+    const int64_t wgs = backward_wgs(a.T, a.D);
     NormPartials part = {(float *)workspace, a.d_post ? (float *)workspace + wgs * a.D : nullptr,
-                         (float *)workspace + 2 * wgs * a.D, span};
+                         (float *)workspace + 2 * wgs * a.D, backward_span(a.T, a.D), backward_walks(a.D)};
     const bool vec = a.D % 8 == 0 && vectors(a.du, a.T) && vectors(a.dx_out, a.T) && vectors(a.x_out, a.T) &&
                      vectors(a.f, a.T) && vectors(a.dx, a.T) && vectors(a.df, a.T) && aligned16(a.post_weight) &&
                      aligned16(a.pre_weight) && aligned16(a.gate) && aligned16(a.d_gate);

@@ -24,6 +24,16 @@ template <> struct Vec8<bf16> { typedef v8bf type; };
 template <> struct Vec8<f16> { typedef v8h type; };
 template <> struct Vec8<int8_t> { typedef v2u type; };
 
+// The same vectors anywhere in memory: loads and stores need the alignment of an element only (unaligned access mode), so rows
+// of any length and stride move in vectors.
+template <typename T> struct Loose8;
+template <> struct Loose8<float> { typedef float type __attribute__((ext_vector_type(8), aligned(4))); };
+template <> struct Loose8<bf16> { typedef bf16 type __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct Loose8<f16> { typedef f16 type __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct Loose8<int8_t> { typedef uint32_t type __attribute__((ext_vector_type(2), aligned(1))); };
+template <typename T> __device__ inline typename Vec8<T>::type load8(const T *p) { return *(const typename Loose8<T>::type *)p; }
+template <typename T> __device__ inline void store8(T *p, typename Vec8<T>::type v) { *(typename Loose8<T>::type *)p = v; }
+
 __device__ inline v8f widen(v8f v) { return v; }
 __device__ inline v8f widen(v8bf v) { return __builtin_convertvector(v, v8f); }
 __device__ inline v8f widen(v8h v) { return __builtin_convertvector(v, v8f); }
