@@ -136,6 +136,7 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
         const TW *wr[RT];
 #pragma unroll
         for (int n = 0; n < RT; ++n) wr[n] = (const TW *)a.w + ((int64_t)adapter * a.R + min(r0 + 16 * n + l, a.R - 1)) * a.K;
+        const float scale = a.scale[adapter];
         v4f acc[2][RT];
 #pragma unroll
         for (int m = 0; m < 2; ++m)
@@ -191,7 +192,6 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sums[wave][16 * m + 4 * q + i][16 * n + l] = acc[m][n][i];
         __syncthreads();
-        const float scale = a.scale[adapter];
         for (int i = threadIdx.x; i < kRows * 16 * RT; i += 256) {
             const int row = i / (16 * RT), col = i % (16 * RT);
             if (!((mine >> row) & 1) || r0 + col >= a.R) continue;
@@ -489,6 +489,18 @@ __global__ __launch_bounds__(256, sizeof(TB) == 2 && VEC ? 3 : 2) void k_adapter
 // --------------------------------------------------------------------------
 // both products for few rows
 // --------------------------------------------------------------------------
+// Eight columns in their places: those of a shifted vector that belong to the lane before are left out.
+template <bool VEC> __device__ inline void put_columns(v8f &place, v8f y, int64_t col, int64_t cols)
+{
+    const int skip = VEC ? beyond(col, cols) : 0;
+    if (skip == 0) place = y;
+    else {
+#pragma unroll
+        for (int j = 1; j < 8; ++j)
+            if (j >= skip) ((float *)&place)[j - skip] = y[j];
+    }
+}
+
 // Both products of one row in one launch, for 512 columns: the row's H is computed by each of its workgroups anew, which costs
 // reading down again from L2 but no second launch and no wait for it.  The sixteen wavefronts share the ranks of both products.
 struct TokenArgs {
@@ -527,33 +539,27 @@ __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
         for (int r = wave; r < a.R; r += kTokenWaves) {
             const TW *w = (const TW *)a.down + ((int64_t)id * a.R + r) * a.K;
             v8f t = v8f(0);
-            int64_t k = 0;
             if constexpr (VEC) {
-                for (; k < a.K; k += 512 * kAhead) {
+                const int64_t whole = a.K / 8;         // vectors; those beyond are read from the last one and count nothing
+                for (int64_t k = 0; k < whole; k += 64 * kAhead) {
                     XV xv[kAhead];
                     WV wv[kAhead];
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) {
-                        const int64_t c = start_of(k + 512 * i + 8 * lane, a.K);
+                        const int64_t c = 8 * min(k + 64 * i + lane, whole - 1);
                         xv[i] = load8(x + c);
                         wv[i] = load8(w + c);
                     }
                     loads_first();
-                    if (k + 512 * kAhead <= a.K) {
 #pragma unroll
-                        for (int i = 0; i < kAhead; ++i) t += widen(xv[i]) * widen(wv[i]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < kAhead; ++i) {
-                            const v8f p = widen(xv[i]) * widen(wv[i]);
-                            const int skip = beyond(k + 512 * i + 8 * lane, a.K);      // 8 past the row's end
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) t[j] += j >= skip ? p[j] : 0.0f;
-                        }
+                    for (int i = 0; i < kAhead; ++i) {
+                        const v8f p = widen(xv[i]) * widen(wv[i]);
+                        t += k + 64 * i + lane < whole ? p : v8f(0);
                     }
                 }
+                if (8 * whole + lane < a.K) t[0] += widen(x[8 * whole + lane]) * widen(w[8 * whole + lane]);
             } else {
-                for (k = lane; k < a.K; k += 64) t[0] += widen(x[k]) * widen(w[k]);
+                for (int64_t k = lane; k < a.K; k += 64) t[0] += widen(x[k]) * widen(w[k]);
             }
             const float s = wave_sum(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
             if (lane == 0) hs[r] = s * scale;
@@ -565,13 +571,7 @@ __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
     } else if (blockIdx.x == 0 && threadIdx.x < a.R) {
         a.h[row * a.R + threadIdx.x] = 0.0f;
     }
-    const int skip = VEC ? beyond(col, a.C) : 0;       // columns that belong to the lane before
-    if (skip == 0) sums[wave][lane] = y;
-    else {
-#pragma unroll
-        for (int j = 1; j < 8; ++j)
-            if (j >= skip) ((float *)&sums[wave][lane])[j - skip] = y[j];
-    }
+    put_columns<VEC>(sums[wave][lane], y, col, a.C);
     __syncthreads();
     if (threadIdx.x >= kTokenColumns || col0 + threadIdx.x >= a.C) return;
     float s = 0.0f;
@@ -580,6 +580,61 @@ __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
     const int64_t at = row * a.out_stride + col0 + threadIdx.x;
     if (a.out_type == PWLQ_F32) ((float *)a.out)[at] = base + s;
     else ((TW *)a.out)[at] = (TW)(base + s);
+}
+
+// The second product of a few rows, each by itself: 512 columns of a row, the four wavefronts share the ranks.  Tiles of sixteen
+// rows would do their adapters one after the other.
+template <typename TW, bool VEC>
+__global__ __launch_bounds__(256) void k_adapter_second_row(SecondArgs a, int base_type)
+{
+    __shared__ float hs[256];
+    __shared__ v8f sums[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = blockIdx.y, col0 = (int64_t)blockIdx.x * 512, col = col0 + 8 * lane;
+    const int id = a.ids[row];
+    const bool any = id >= 0 && id < a.adapters;
+    float base[2];
+    if (a.has_base) {
+        const float factor = a.base_step ? a.base_step[row] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t at = row * a.base_stride + min(col0 + threadIdx.x + 256 * i, a.C - 1);
+            base[i] = (base_type == PWLQ_F32 ? ((const float *)a.base)[at] : widen(((const TW *)a.base)[at])) * factor;
+        }
+    } else {
+        base[0] = base[1] = 0.0f;
+    }
+    if ((int)threadIdx.x < a.R) {
+        float s = 0.0f;
+        for (int p = 0; p < a.splits; ++p) s += a.h[(p * a.rows + row) * a.R + threadIdx.x];
+        hs[threadIdx.x] = s;
+        if (blockIdx.x == 0 && a.h_out) a.h_out[row * a.R + threadIdx.x] = s;
+    }
+    __syncthreads();
+    v8f y = v8f(0);
+    if (any) {
+        const TW *w = (const TW *)a.w + (int64_t)id * a.R * a.C;
+        for (int r = wave; r < a.R; r += 16) {             // four ranks under way
+            typename Vec8<TW>::type v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = columns8<TW, VEC>(w + (int64_t)min(r + 4 * j, a.R - 1) * a.C, col, a.C);
+            loads_first();
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (r + 4 * j < a.R) y += hs[r + 4 * j] * widen(v[j]);
+        }
+    }
+    put_columns<VEC>(sums[wave][lane], y, col, a.C);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = threadIdx.x + 256 * i;
+        if (col0 + c >= a.C) return;
+        const float s = (((const float *)sums[0])[c] + ((const float *)sums[1])[c]) + (((const float *)sums[2])[c] + ((const float *)sums[3])[c]);
+        const int64_t at = row * a.out_stride + col0 + c;
+        if (a.out_type == PWLQ_F32) ((float *)a.out)[at] = base[i] + s;
+        else ((TW *)a.out)[at] = (TW)(base[i] + s);
+    }
 }
 
 // --------------------------------------------------------------------------
@@ -626,6 +681,7 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
     v4f acc[RT][8];
     for (int adapter = slot - a.slots, next;; adapter = next) {
         next = a.adapters;
+        bool alone = true;                             // the first wavefront has all rows
 #pragma unroll
         for (int n = 0; n < RT; ++n)
 #pragma unroll
@@ -648,6 +704,7 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
                 count += __builtin_popcountll(mine);
             }
             __syncthreads();
+            alone &= count <= 16;
             auto load = [&](int first, Rows &v) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -703,33 +760,36 @@ template <typename TX, int RT, bool VEC> __device__ inline void outer_tile(const
                 }
         if (adapter >= 0) {
             if (present && (int)threadIdx.x == adapter / a.slots % 256) present[adapter] = 1;
-            if (wave >= 2) {
+            if (!alone) {
+                if (wave >= 2) {
 #pragma unroll
-                for (int n = 0; n < RT; ++n)
+                    for (int n = 0; n < RT; ++n)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) lds.sums[wave - 2][8 * n + j][lane] = acc[n][j];
+                        for (int j = 0; j < 8; ++j) lds.sums[wave - 2][8 * n + j][lane] = acc[n][j];
+                }
+                __syncthreads();
+                if (wave < 2) {
+#pragma unroll
+                    for (int n = 0; n < RT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) acc[n][j] += lds.sums[wave][8 * n + j][lane];
+                }
+                __syncthreads();
+                if (wave == 1) {
+#pragma unroll
+                    for (int n = 0; n < RT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) lds.sums[0][8 * n + j][lane] = acc[n][j];
+                }
+                __syncthreads();
             }
-            __syncthreads();
-            if (wave < 2) {
-#pragma unroll
-                for (int n = 0; n < RT; ++n)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[n][j] += lds.sums[wave][8 * n + j][lane];
-            }
-            __syncthreads();
-            if (wave == 1) {
-#pragma unroll
-                for (int n = 0; n < RT; ++n)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) lds.sums[0][8 * n + j][lane] = acc[n][j];
-            }
-            __syncthreads();
             if (wave == 0) {
                 float *out = part + (int64_t)adapter * a.R * a.C;
 #pragma unroll
                 for (int n = 0; n < RT; ++n) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[n][j] += lds.sums[0][8 * n + j][lane];
+                    for (int j = 0; j < 8; ++j)
+                        if (!alone) acc[n][j] += lds.sums[0][8 * n + j][lane];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = r0 + 16 * n + 4 * q + i;
@@ -897,8 +957,17 @@ void first(const FirstArgs &a, int x_type, int w_type, bool vec, hipStream_t str
 }
 
 
+constexpr int64_t kSingleRows = 64;    // up to so many rows the second product does each by itself
+
 template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipStream_t stream)
 {
+    if (a.rows <= kSingleRows) {
+        const dim3 grid((unsigned)((a.C + 511) / 512), (unsigned)a.rows);
+        const int base_type = std::is_same<TB, float>::value ? PWLQ_F32 : -1;
+        if (vec) k_adapter_second_row<TW, true><<<grid, 256, 0, stream>>>(a, base_type);
+        else k_adapter_second_row<TW, false><<<grid, 256, 0, stream>>>(a, base_type);
+        return;
+    }
     const int64_t tiles = (a.rows + kSecondRows - 1) / kSecondRows, columns = (a.C + 127) / 128;
     const int waves = (int)std::min<int64_t>(columns, 4);
     // as many workgroups as are resident walk at once

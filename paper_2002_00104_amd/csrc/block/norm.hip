@@ -136,14 +136,16 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
         if (KEPT && a.f.data) f_step = a.f.step[row];
     };
     // alpha gate into g, post into p
-    auto factors = [&](int64_t gate_row, float (&g)[E], float (&p)[E]) {
-        Row<float, E, VEC> post;
-        Row<TF, E, VEC> gate;
-        if (a.post_weight) post.load(a.post_weight, D, threads, thread);
-        if (a.gate) gate.load((const TF *)a.gate + gate_row * a.D, D, threads, thread);
+    constexpr bool kHold = E == 8;                     // post stays in registers where there is room
+    Row<float, E, VEC> post;
+    Row<TF, E, VEC> gate;
+    auto factors = [&](float (&g)[E], float (&p)[E]) {
 #pragma unroll
         for (int i = 0; i < E; ++i) g[i] = p[i] = 1.0f;
-        if (a.post_weight) post.get(p);
+        if (a.post_weight) {
+            if (!kHold) post.load(a.post_weight, D, threads, thread);
+            post.get(p);
+        }
         if (a.gate) gate.get(g);
 #pragma unroll
         for (int i = 0; i < E; ++i) g[i] *= a.alpha;
@@ -151,7 +153,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
     // the sums of a gate row's end
     auto settle = [&](int64_t gate_row) {
         float g[E], p[E];
-        factors(gate_row, g, p);
+        factors(g, p);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             sum_post[i] += g[i] * sum_f[i];
@@ -161,12 +163,13 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
 #pragma unroll
         for (int i = 0; i < E; ++i) sum_f[i] = 0.0f;
     };
-    {
-        Row<float, E, VEC> weight;
-        weight.load(a.pre_weight, D, threads, thread);
-        weight.get(pre);
-    }
+    Row<float, E, VEC> weight;
+    weight.load(a.pre_weight, D, threads, thread);
+    if (kHold && a.post_weight) post.load(a.post_weight, D, threads, thread);
+    if (a.gate && first < last) gate.load((const TF *)a.gate + first / per_gate * a.D, D, threads, thread);
     if (first < last) load(first);
+    loads_first();
+    weight.get(pre);
     int64_t at_gate = -1;
     int turn = 0;
     for (int64_t row = first; row < last; ++row, turn ^= 1) {
@@ -181,10 +184,13 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
         }
         const float xs = x_step, fs = f_step;
         if (a.f.data && row / per_gate != at_gate) {
-            if (at_gate >= 0) settle(at_gate);
+            if (at_gate >= 0) {
+                settle(at_gate);
+                if (a.gate) gate.load((const TF *)a.gate + row / per_gate * a.D, D, threads, thread);
+            }
             at_gate = row / per_gate;
             float p[E];
-            factors(at_gate, back, p);
+            factors(back, p);
 #pragma unroll
             for (int i = 0; i < E; ++i) back[i] *= p[i];
         }
@@ -260,13 +266,13 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
 // Sums of the partial rows, in order: of all workgroups for the norms' weights, of those that meet it for a gate row.  Sixteen
 // wavefronts take a row each in turn, four loads under way.
 constexpr int kSumWaves = 16;
-__global__ __launch_bounds__(64 * kSumWaves) void k_column_sums(pwlq_norm_backward_args a, NormPartials part, int workgroups)
+__global__ __launch_bounds__(64 * kSumWaves) void k_column_sums(pwlq_norm_backward_args a, NormPartials part, int workgroups, int64_t outs)
 {
     __shared__ float sums[kSumWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t col = min((int64_t)blockIdx.x * 64 + lane, a.D - 1);
     // outputs: d_pre, d_post, the rows of d_gate
-    for (int64_t out = blockIdx.y; out < 2 + (a.d_gate ? a.gate_rows : 0); out += gridDim.y) {
+    for (int64_t out = blockIdx.y; out < outs; out += gridDim.y) {
         const float *from = out == 0 ? part.pre : part.post;
         float *to = out == 0 ? a.d_pre : a.d_post;
         int64_t first = 0, last = workgroups;
@@ -397,9 +403,11 @@ void norm_backward(const pwlq_norm_backward_args &a, void *workspace, hipStream_
     else if (tx == PWLQ_F16) PWLQ_AS(f16, f16);
     else PWLQ_AS(f16, float);
 #undef PWLQ_AS
-    const int64_t outs = 2 + (a.d_gate ? a.gate_rows : 0);
+    // gate rows that lie within walks are written already
+    const bool straddled = a.d_gate && part.span % (a.T / a.gate_rows) != 0;
+    const int64_t outs = 2 + (straddled ? a.gate_rows : 0);
     const dim3 grid((unsigned)((a.D + 63) / 64), (unsigned)(outs < 4096 ? outs : 4096));
-    k_column_sums<<<grid, 64 * kSumWaves, 0, stream>>>(a, part, (int)wgs);
+    k_column_sums<<<grid, 64 * kSumWaves, 0, stream>>>(a, part, (int)wgs, outs);
 }
 
 } // namespace pwlq_block
