@@ -127,7 +127,7 @@ int pwlq_norm_block_backward(const pwlq_norm_backward_args *args, void *workspac
  * Rows without an adapter, and rows of another adapter, are not touched by an
  * adapter's infinities or NaN (its own rows get NaN where the product of such a
  * value may have been an infinity).  1 <= R <= 256, 1 <= adapters <= 65535, an
- * adapter below 2 GiB, strides up to 2^24.
+ * adapter below 2 GiB, strides up to 2^20.
  * Workspace: device, 256-byte aligned, pwlq_adapter_workspace_bytes(T, K, R).
  */
 typedef struct {

@@ -43,6 +43,69 @@ struct Adapters {
     }
 };
 
+// SPAN neighbouring rows in tiles of at most ROWS rows of one adapter: the span's adapters in turn, the rows of each in order.
+// Rows of one request are next to each other, so with a span of one tile most tiles have one adapter, and one of several is done
+// once for each.  Where requests may alternate (a batch that decodes), a span of 256 rows collects full tiles of rows that need the
+// same weights.  Rows without an adapter are adapter -1.
+constexpr int kCollected = 256;
+template <int ROWS, int SPAN> struct Tiles {
+    static constexpr int kNone = 0x7fffffff, kGroups = SPAN < 64 ? 1 : SPAN / 64;
+    int id[kGroups];                   // of the rows 64 g + lane; kNone beyond the last row
+    uint64_t mine[kGroups];            // the rows of `adapter`
+    int adapter, count, first, end;    // `count` of them, in the tiles [first, end)
+
+    __device__ void load(const int32_t *ids, int64_t row0, int64_t rows)
+    {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) id[g] = ids[clamp_row(row0 + 64 * g + (threadIdx.x & 63), rows)];
+    }
+    // `after`: adapters up to it are left out
+    __device__ void start(int64_t row0, int64_t rows, int adapters, int after)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+            id[g] = 64 * g + lane >= SPAN || row0 + 64 * g + lane >= rows ? kNone : id[g] >= 0 && id[g] < adapters ? id[g] : -1;
+        adapter = after;
+        count = first = end = 0;
+    }
+    // Goes on to the adapter that has the tile; false: there are fewer tiles.
+    __device__ bool seek(int tile)
+    {
+        while (tile >= end) {
+            uint32_t left = 0;         // kNone less the next adapter
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+                if (id[g] > adapter) left = max(left, (uint32_t)kNone - (uint32_t)id[g]);
+            left = wave_max(left);
+            if (left == 0) return false;
+            adapter = (int)((uint32_t)kNone - left);
+            count = 0;
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                mine[g] = __ballot(id[g] == adapter);
+                count += __builtin_popcountll(mine[g]);
+            }
+            first = end;
+            end += (count + ROWS - 1) / ROWS;
+        }
+        return true;
+    }
+    __device__ int size(int tile) const { return min(ROWS, count - (tile - first) * ROWS); }
+    // The tile's rows into `list`, by the wavefronts together.
+    __device__ void rows(int tile, int *list, int waves) const
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        int before = -(tile - first) * ROWS;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const int at = before + __builtin_popcountll(mine[g] & ((1ull << lane) - 1));
+            if (g % waves == wave && ((mine[g] >> lane) & 1) && at >= 0 && at < ROWS) list[at] = 64 * g + lane;
+            before += __builtin_popcountll(mine[g]);
+        }
+    }
+};
+
 // --------------------------------------------------------------------------
 // first product
 // --------------------------------------------------------------------------
@@ -94,7 +157,7 @@ struct FirstArgs {
     int64_t stride, rows, K, chunk;    // chunk: reduction elements of a workgroup, a multiple of 64
     const float *step, *scale;
     const int32_t *ids;
-    int R, adapters, slots;
+    int R, adapters, turns;            // turns: workgroups that share a span's tiles
     float *out;                        // [splits, rows, R]: a sum for each part of the reduction
 };
 
@@ -104,36 +167,39 @@ template <typename TX> __device__ inline int half_at(int q, int half) { return s
 // A tile of 32 rows by 16 RT ranks, and a part of the reduction.  The four wavefronts take its steps of 64 elements in turn
 // and add up in LDS.  Several steps' loads are issued before the first one's products: a wavefront waits for memory
 // once per batch.
-template <typename TX, typename TW, int RT, bool VEC>
+template <typename TX, typename TW, int RT, int SPAN, bool VEC>
 __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
 {
     constexpr int kBatch = sizeof(TW) == 2 || RT == 1 ? 2 : 1;
     typedef typename Vec8<TX>::type XV;
     typedef typename Vec8<TW>::type WV;
     __shared__ float sums[4][kRows][16 * RT];
+    __shared__ int list[kRows];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, q = lane >> 4;
-    const unsigned tiles = gridDim.x / a.slots;        // slots outermost: most tiles have work in the first alone, and the chip's
-    const int64_t row0 = (int64_t)(blockIdx.x % tiles) * kRows;    // eight dies take workgroups in turn
-    const int slot = blockIdx.x / tiles, r0 = blockIdx.y * 16 * RT;
+    const unsigned spans = gridDim.x / a.turns;        // turns outermost: the later ones may have no tile, and the chip's eight dies
+    const int64_t row0 = (int64_t)(blockIdx.x % spans) * SPAN;     // take workgroups in turn
+    const int turn = blockIdx.x / spans, r0 = blockIdx.y * 16 * RT;
     const int64_t k0 = (int64_t)blockIdx.z * a.chunk, k1 = min(k0 + a.chunk, a.K);
-    float *out = a.out + (int64_t)blockIdx.z * a.rows * a.R;
-    const TX *xr[2];
-#pragma unroll
-    for (int m = 0; m < 2; ++m) xr[m] = (const TX *)a.x + clamp_row(row0 + 16 * m + l, a.rows) * a.stride;
+    float *out = a.out + (int64_t)blockIdx.z * a.rows * a.R + row0 * a.R;
 
-    Adapters of(Adapters::load(a.ids, row0, a.rows), row0, a.rows, a.adapters, kRows);
-    if (slot == 0) {                                   // rows without an adapter
-        const uint64_t none = ~of.left;
-        for (int i = threadIdx.x; i < kRows * 16 * RT; i += 256) {
-            const int row = i / (16 * RT), r = r0 + i % (16 * RT);
-            if (((none >> row) & 1) && row0 + row < a.rows && r < a.R) out[(row0 + row) * a.R + r] = 0.0f;
-        }
+    Tiles<kRows, SPAN> of;
+    of.load(a.ids, row0, a.rows);
+    of.start(row0, a.rows, a.adapters, -1);
+    if (turn == 0) {                                   // rows without an adapter
+#pragma unroll
+        for (int g = 0; g < of.kGroups; ++g)
+            if (g == wave && of.id[g] == -1)
+                for (int r = r0; r < min(r0 + 16 * RT, a.R); ++r) out[(64 * g + lane) * a.R + r] = 0.0f;
     }
-    int adapter;
-    uint64_t mine;
-    for (int turn = 0; of.next(adapter, mine); ++turn) {
-        if (turn % a.slots != slot) continue;
+    for (int tile = turn; of.seek(tile); tile += a.turns) {
+        const int adapter = of.adapter, size = of.size(tile);
+        __syncthreads();                               // the last tile's list and sums are read
+        of.rows(tile, list, 4);
+        __syncthreads();
+        const TX *xr[2];
         const TW *wr[RT];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) xr[m] = (const TX *)a.x + (row0 + list[min(16 * m + l, size - 1)]) * a.stride;
 #pragma unroll
         for (int n = 0; n < RT; ++n) wr[n] = (const TW *)a.w + ((int64_t)adapter * a.R + min(r0 + 16 * n + l, a.R - 1)) * a.K;
         const float scale = a.scale[adapter];
@@ -184,7 +250,6 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
         if constexpr (VEC)
             for (; k + 256 * (kBatch - 1) + 64 <= k1; k += 256 * kBatch) batch(k, std::true_type());
         for (; k < k1; k += 256 * kBatch) batch(k, std::false_type());
-        __syncthreads();
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -193,10 +258,11 @@ __global__ __launch_bounds__(256) void k_adapter_first(FirstArgs a)
                 for (int i = 0; i < 4; ++i) sums[wave][16 * m + 4 * q + i][16 * n + l] = acc[m][n][i];
         __syncthreads();
         for (int i = threadIdx.x; i < kRows * 16 * RT; i += 256) {
-            const int row = i / (16 * RT), col = i % (16 * RT);
-            if (!((mine >> row) & 1) || r0 + col >= a.R) continue;
-            const float s = (sums[0][row][col] + sums[1][row][col]) + (sums[2][row][col] + sums[3][row][col]);
-            out[(row0 + row) * a.R + r0 + col] = s * (a.step ? scale * a.step[row0 + row] : scale);
+            const int at = i / (16 * RT), col = i % (16 * RT);
+            if (at >= size || r0 + col >= a.R) continue;
+            const int row = list[at];
+            const float s = (sums[0][at][col] + sums[1][at][col]) + (sums[2][at][col] + sums[3][at][col]);
+            out[row * a.R + r0 + col] = s * (a.step ? scale * a.step[row0 + row] : scale);
         }
     }
 }
@@ -316,7 +382,8 @@ struct SecondArgs {
     const float *base_step;
     const int32_t *ids;
     bool has_base;                     // else base is memory that can be read as a row of C elements, its stride 0
-    int R, splits, adapters, out_type, walks;     // walks: workgroups that share the columns of a tile of rows
+    int R, splits, adapters, out_type;
+    int turns, walks;                  // workgroups that share a span's tiles, and the columns of a tile
 };
 
 // A wavefront does 16 rows by 128 columns.  The ranks come sixteen at a time, their products added to the row's sum where the
@@ -345,6 +412,44 @@ template <typename T, bool VEC> __device__ inline void store_tile(__amdgpu_buffe
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i >= skip && i < columns) buffer_store1<T>(b, offset + i * (int)sizeof(T), (T)v[i]);
+    }
+}
+
+// H of a tile into LDS, its parts added up in order: four elements of a thread and four parts under way.  Sixteen ranks of a row are
+// neighbours, then the rows, then the next sixteen ranks.  `row_of` gives the tile's rows, some row beyond the last `n`.
+template <class RowOf> __device__ inline void load_h(const SecondArgs &a, float *hs, int n, bool keep, RowOf row_of)
+{
+    const int pitch = second_pitch(a.R);
+    for (int i = threadIdx.x; i - (int)threadIdx.x < kSecondRows * (pitch - 1); i += 4 * blockDim.x) {
+        int row[4], r[4];
+        int64_t at[4];
+        float sum[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = i + j * blockDim.x;
+            row[j] = (e >> 4) % kSecondRows;
+            r[j] = e / (16 * kSecondRows) * 16 + (e & 15);
+            at[j] = row_of(row[j]) * a.R + min(r[j], a.R - 1);
+            sum[j] = 0.0f;
+        }
+        for (int p = 0; p < a.splits; p += 4) {
+            float v[4][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[k][j] = a.h[min(p + k, a.splits - 1) * a.rows * a.R + at[j]];
+            loads_first();
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] += p + k < a.splits ? v[k][j] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (r[j] >= pitch - 1) continue;
+            if (r[j] < a.R && keep && a.h_out && row[j] < n) a.h_out[at[j]] = sum[j];
+            hs[row[j] * pitch + r[j]] = r[j] < a.R ? sum[j] : 0.0f;
+        }
     }
 }
 
@@ -398,39 +503,7 @@ __global__ __launch_bounds__(256, sizeof(TB) == 2 && VEC ? 3 : 2) void k_adapter
     const int first_adapter = adapter;
     load_ranks(adapter, 0, tile);
 
-    // H into LDS, its parts added up in order: four elements of a thread and four parts under way.  Sixteen ranks of a row are
-    // neighbours, then the rows, then the next sixteen ranks.
-    for (int i = threadIdx.x; i - (int)threadIdx.x < kSecondRows * (pitch - 1); i += 4 * blockDim.x) {
-        int row[4], r[4];
-        int64_t at[4];
-        float sum[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int e = i + j * blockDim.x;
-            row[j] = (e >> 4) % kSecondRows;
-            r[j] = e / (16 * kSecondRows) * 16 + (e & 15);
-            at[j] = clamp_row(row0 + row[j], a.rows) * a.R + min(r[j], a.R - 1);
-            sum[j] = 0.0f;
-        }
-        for (int p = 0; p < a.splits; p += 4) {
-            float v[4][4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[k][j] = a.h[min(p + k, a.splits - 1) * a.rows * a.R + at[j]];
-            loads_first();
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum[j] += p + k < a.splits ? v[k][j] : 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (r[j] >= pitch - 1) continue;
-            if (r[j] < a.R && walk == 0 && a.h_out && row0 + row[j] < a.rows) a.h_out[at[j]] = sum[j];
-            hs[row[j] * pitch + r[j]] = r[j] < a.R ? sum[j] : 0.0f;
-        }
-    }
+    load_h(a, hs, rows, walk == 0, [&](int row) { return clamp_row(row0 + row, a.rows); });
     __syncthreads();
     for (; tile < tiles; tile += stride) {
         v8f acc[4];
@@ -482,6 +555,111 @@ __global__ __launch_bounds__(256, sizeof(TB) == 2 && VEC ? 3 : 2) void k_adapter
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) store_tile<TW, VEC>(out_rows, offset + i * out_pitch, skip, left, acc[i]);
+        }
+    }
+}
+
+// The same for tiles that are collected, a tile's rows of one adapter: what the ranks give is added to the base by the products.
+template <typename TW, typename TB, bool VEC> __global__ __launch_bounds__(256, 2) void k_adapter_second_collected(SecondArgs a)
+{
+    typedef typename Vec8<TW>::type WV;
+    typedef typename Vec8<TB>::type BV;
+    extern __shared__ float hs[];
+    __shared__ int list[kSecondRows];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x / 64, l = lane & 15, q = lane >> 4;
+    const unsigned spans = gridDim.x / (a.turns * a.walks);
+    const unsigned span = blockIdx.x % spans;          // turns outermost: the later ones may have no tile
+    const int walk = blockIdx.x / spans % a.walks, turn = blockIdx.x / (spans * a.walks), pitch = second_pitch(a.R), C = (int)a.C;
+    const int64_t row0 = (int64_t)span * kCollected;
+    const int tiles = (C + 127) / 128, stride = a.walks * waves;      // tiles of 128 columns
+
+    const int rows = (int)min((int64_t)kCollected, a.rows - row0);
+    const int base_pitch = (int)a.base_stride * (int)sizeof(TB), out_size = a.out_type == PWLQ_F32 ? 4 : (int)sizeof(TW);
+    const int out_pitch = (int)a.out_stride * out_size;
+    const __amdgpu_buffer_rsrc_t base_rows = row_buffer((const TB *)a.base + row0 * a.base_stride, (uint32_t)(rows - 1) * base_pitch + C * sizeof(TB));
+    const __amdgpu_buffer_rsrc_t out_rows =
+        row_buffer((char *)a.out + row0 * a.out_stride * out_size, (uint32_t)(rows - 1) * out_pitch + C * out_size);
+    // a lane's first column in a tile; the last vector of a row that is no whole number of them starts further left
+    auto column = [&](int tile) { return VEC ? (int)start_of(128 * tile + 8 * l, C) : 128 * tile + 8 * l; };
+
+    int row[4];                                        // the lane's rows of the tile
+    float factor[4];                                   // without factors any number that can be read
+    BV base[4];
+    WV w[4];
+    auto load_base = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) base[i] = buffer_columns<TB, VEC>(base_rows, row[i] * base_pitch + column(tile) * (int)sizeof(TB));
+    };
+    const float *factors = a.base_step ? a.base_step + row0 : a.h;
+    Tiles<kSecondRows, kCollected> of;
+    of.load(a.ids, row0, a.rows);
+    of.start(row0, a.rows, a.adapters, -2);
+    for (int at = turn; of.seek(at); at += a.turns) {
+        const int adapter = of.adapter, n = of.size(at);
+        int tile = walk * waves + wave;
+        __syncthreads();                               // the last tile's list and H are read
+        of.rows(at, list, waves);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            row[i] = list[min(4 * q + i, n - 1)];
+            factor[i] = factors[a.base_step ? row[i] : 0];
+        }
+        load_base(tile);
+        const __amdgpu_buffer_rsrc_t ranks = row_buffer((const TW *)a.w + (int64_t)max(adapter, 0) * a.R * C, (uint32_t)a.R * C * sizeof(TW));
+        auto load_ranks = [&](int r0, int tile) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = buffer_columns<TW, VEC>(ranks, (int)((uint32_t)((r0 + element_of<TW>(q, i)) * (uint32_t)C + column(tile)) * (uint32_t)sizeof(TW)));
+        };
+        load_ranks(0, tile);
+
+        load_h(a, hs, n, walk == 0, [&](int i) { return row0 + list[min(i, n - 1)]; });
+        __syncthreads();
+        for (; tile < tiles; tile += stride) {
+            v4f acc[2][4];                             // of a column: the lane's four rows; four columns at a time
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const v8f b = a.has_base ? widen(base[i]) * (a.base_step ? factor[i] : 1.0f) : v8f(0);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j / 4][j % 4][i] = b[j];
+            }
+            const int after = tile + stride < tiles ? tile + stride : tile;
+            load_base(after);                          // the next columns'
+            for (int r0 = 0; r0 < a.R && adapter >= 0; r0 += 16) {
+                WV now[4];
+                float h[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    now[i] = w[i];
+                    h[i] = hs[l * pitch + r0 + element_of<TW>(q, i)];
+                }
+                const bool last = r0 + 16 >= a.R;
+                load_ranks(last ? 0 : r0 + 16, last ? after : tile);
+                loads_first();
+                const H16<TW> h16(h);
+                const Columns<TW> columns(now);
+                product16(h16, columns, 0, acc[0]);
+                loads_first();
+                product16(h16, columns, 4, acc[1]);
+                loads_first();
+            }
+            const int left = C - column(tile), skip = VEC ? beyond(128 * tile + 8 * l, C) : 0;
+            const int offset = column(tile) * out_size;
+            v8f v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = acc[j / 4][j % 4][i];
+            if (a.out_type == PWLQ_F32) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (4 * q + i < n) store_tile<float, VEC>(out_rows, row[i] * out_pitch + offset, skip, left, v[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (4 * q + i < n) store_tile<TW, VEC>(out_rows, row[i] * out_pitch + offset, skip, left, v[i]);
+            }
         }
     }
 }
@@ -933,19 +1111,36 @@ struct BackwardSpace {
     }
 };
 
+// Whether rows are collected by adapter from spans of 256: see Tiles.  Collecting takes a longer start (ids, a list, the rows'
+// addresses from it) and pays where a tile of neighbouring rows would be done for many adapters, each with many ranks.  Both products
+// of 4096 x 4096, 16 ranks, in us, not collected -> collected, rows in runs and rows whose adapters alternate: 256 rows of 2 adapters
+// 10.0 -> 11.5 and 10.2 -> 11.5; of 8 adapters 11.4 -> 13.0 and 15.6 -> 13.7; 2048 rows of 8 adapters 21.7 -> 23.4 and 44.9 -> 25.4;
+// 4096 rows of 16 adapters 32.2 -> 31.6 and 106 -> 43 (inputs in the caches; with inputs from memory 4096 rows of 8 adapters in runs
+// 32 -> 38).  93 rows of 8 adapters and 43 ranks, alternating: 29 -> 21.
+bool collected(int64_t rows, int R, int adapters) { return adapters > 1 && rows * adapters * ((R + 15) / 16) >= 2048; }
+
+// Workgroups that share the tiles of a span of `in_span` rows: one for each tile that it has if its rows have one adapter, in a collected
+// span some for the tiles that further adapters begin, and more where `fill` of them are wanted, up to the tiles there can be.
+int turns(int64_t in_span, int tile, int adapters, bool collect, int64_t fill)
+{
+    const int64_t whole = (in_span + tile - 1) / tile, most = whole + std::min<int64_t>(adapters, in_span - 1);
+    return (int)std::min(most, std::max(whole + (collect ? std::min<int64_t>(adapters, whole / 2) : 0), fill));
+}
+
 template <typename TX, typename TW> void first_as(FirstArgs a, bool vec, hipStream_t stream)
 {
-    const int64_t tiles = (a.rows + kRows - 1) / kRows, splits = (a.K + a.chunk - 1) / a.chunk;
-    a.slots = (int)std::min<int64_t>(std::min(a.adapters, kRows), std::max<int64_t>(1, 2048 / (tiles * splits * rank_blocks(a.R))));
-    const dim3 grid((unsigned)(tiles * a.slots), rank_blocks(a.R), (unsigned)splits);
-#define PWLQ_FIRST(RT)                                                                          \
-    do {                                                                                        \
-        if (vec) k_adapter_first<TX, TW, RT, true><<<grid, 256, 0, stream>>>(a);                \
-        else k_adapter_first<TX, TW, RT, false><<<grid, 256, 0, stream>>>(a);                   \
-    } while (0)
-    if (rank_tiles(a.R) == 1) PWLQ_FIRST(1);
-    else if (rank_tiles(a.R) == 2) PWLQ_FIRST(2);
-    else PWLQ_FIRST(4);
+    const bool collect = collected(a.rows, a.R, a.adapters);
+    const int64_t rows = collect ? kCollected : kRows, spans = (a.rows + rows - 1) / rows, splits = (a.K + a.chunk - 1) / a.chunk;
+    a.turns = turns(std::min(a.rows, rows), kRows, a.adapters, collect, 2048 / (spans * splits * rank_blocks(a.R)));
+    const dim3 grid((unsigned)(spans * a.turns), rank_blocks(a.R), (unsigned)splits);
+#define PWLQ_FIRST(RT, SPAN)                                                                    \
+    (vec ? k_adapter_first<TX, TW, RT, SPAN, true><<<grid, 256, 0, stream>>>(a)                 \
+         : k_adapter_first<TX, TW, RT, SPAN, false><<<grid, 256, 0, stream>>>(a))
+#define PWLQ_FIRST_SPAN(SPAN)                                                                   \
+    (rank_tiles(a.R) == 1 ? PWLQ_FIRST(1, SPAN) : rank_tiles(a.R) == 2 ? PWLQ_FIRST(2, SPAN) : PWLQ_FIRST(4, SPAN))
+    if (collect) PWLQ_FIRST_SPAN(kCollected);
+    else PWLQ_FIRST_SPAN(kRows);
+#undef PWLQ_FIRST_SPAN
 #undef PWLQ_FIRST
 }
 
@@ -970,9 +1165,18 @@ template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipSt
     }
     const int64_t tiles = (a.rows + kSecondRows - 1) / kSecondRows, columns = (a.C + 127) / 128;
     const int waves = (int)std::min<int64_t>(columns, 4);
-    // as many workgroups as are resident walk at once
-    a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, ((sizeof(TB) == 2 ? 768 : 512) + tiles - 1) / tiles);
+    const bool collect = collected(a.rows, a.R, a.adapters);
+    // as many workgroups as are resident walk at once; collected ones, of which some have less to do, a few more
+    a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, ((sizeof(TB) == 2 || collect ? 768 : 512) + tiles - 1) / tiles);
     const size_t lds = sizeof(float) * kSecondRows * second_pitch(a.R);
+    if (collect) {
+        const int64_t spans = (a.rows + kCollected - 1) / kCollected;
+        a.turns = turns(std::min<int64_t>(a.rows, kCollected), kSecondRows, a.adapters, true, 512 / (spans * a.walks));
+        const unsigned grid = (unsigned)(spans * a.turns * a.walks);
+        if (vec) k_adapter_second_collected<TW, TB, true><<<grid, 64 * waves, lds, stream>>>(a);
+        else k_adapter_second_collected<TW, TB, false><<<grid, 64 * waves, lds, stream>>>(a);
+        return;
+    }
     const unsigned grid = (unsigned)(tiles * a.walks);
     if (vec) k_adapter_second<TW, TB, true><<<grid, 64 * waves, lds, stream>>>(a);
     else k_adapter_second<TW, TB, false><<<grid, 64 * waves, lds, stream>>>(a);

@@ -7,7 +7,7 @@ namespace {
 
 constexpr int64_t kMostRows = 1LL << 26;       // grids of all launches stay below 2^32 threads a dimension
 
-constexpr int64_t kMostStride = 1LL << 24;     // sixteen rows of binary32 stay below 2 GiB
+constexpr int64_t kMostStride = 1LL << 20;     // 256 rows of binary32 stay below 2 GiB
 bool float_type(int type) { return type == PWLQ_F32 || type == PWLQ_BF16 || type == PWLQ_F16; }
 
 // Rows of `cols` columns that have to be there: type (codes only where `codes`), step, stride, alignment to their own elements.
@@ -49,12 +49,12 @@ int check_gate(const void *gate, int64_t gate_rows, int64_t T)
 int check_adapter(int64_t T, int64_t K, int64_t N, int R, int adapters, int type, const void *down, const void *up, const int32_t *ids,
                   const float *scale)
 {
-    if (int rc = check_sizes(T, K, 1 << 22)) return rc;
-    if (int rc = check_sizes(T, N, 1 << 22)) return rc;
+    if (int rc = check_sizes(T, K, 1 << 20)) return rc;
+    if (int rc = check_sizes(T, N, 1 << 20)) return rc;
     if (R < 1 || R > 256) return fail(PWLQ_EINVAL, "R=%d outside [1,256]", R);
     if (adapters < 1 || adapters > 65535) return fail(PWLQ_EINVAL, "adapters=%d outside [1,65535]", adapters);
     if (!float_type(type)) return fail(PWLQ_EINVAL, "weight_type=%d is none of the float types", type);
-    if ((T + 15) / 16 * ((N > K ? N : K) / 128 + 4) * 64 > 0xffffffffLL) return fail(PWLQ_EINVAL, "grid too large");
+    if ((T + 255) / 256 * 512 * ((N > K ? N : K) / 512 + 4) > 0xffffffffLL / 256) return fail(PWLQ_EINVAL, "grid too large");
     // rows and adapters are addressed within tiles by 32 bits
     const int64_t most = (1LL << 31) / pwlq_block::type_size(type);
     if (R * K >= most || R * N >= most) return fail(PWLQ_EINVAL, "an adapter of 2 GiB or more");
@@ -170,7 +170,7 @@ int pwlq_norm_block_backward(const pwlq_norm_backward_args *a, void *workspace, 
 
 size_t pwlq_adapter_workspace_bytes(int64_t T, int64_t K, int R)
 {
-    if (T < 0 || T > kMostRows || K < 1 || K > 1 << 22 || R < 1 || R > 256) return 0;
+    if (T < 0 || T > kMostRows || K < 1 || K > 1 << 20 || R < 1 || R > 256) return 0;
     return pwlq_block::adapter_workspace(T, K, R);
 }
 
@@ -191,7 +191,7 @@ int pwlq_adapter(const pwlq_adapter_args *a, void *workspace, size_t workspace_b
 
 size_t pwlq_adapter_backward_workspace_bytes(int64_t T, int64_t K, int64_t N, int R, int adapters)
 {
-    if (T < 0 || T > kMostRows || K < 1 || K > 1 << 22 || N < 1 || N > 1 << 22 || R < 1 || R > 256 || adapters < 1 || adapters > 65535)
+    if (T < 0 || T > kMostRows || K < 1 || K > 1 << 20 || N < 1 || N > 1 << 20 || R < 1 || R > 256 || adapters < 1 || adapters > 65535)
         return 0;
     return pwlq_block::adapter_backward_workspace(T, K, N, R, adapters);
 }

@@ -141,8 +141,8 @@ def test_adapters(calls):
         assert call(**{name: None}) == ENULL, name
     assert call(x=rows(1024, I8)) == ENULL and call(out=rows(48, data=None)) == ENULL
     assert call(R=0) == EINVAL and call(R=257) == EINVAL and call(adapters=0) == EINVAL and call(adapters=65536) == EINVAL
-    assert call(K=0) == EINVAL and call(N=0) == EINVAL and call(N=(1 << 22) + 1) == EINVAL and call(T=-1) == EINVAL
-    assert call(T=1 << 26, N=1 << 22) == EINVAL and call(T=1 << 26, K=1 << 22) == EINVAL
+    assert call(K=0) == EINVAL and call(N=0) == EINVAL and call(N=(1 << 20) + 1) == EINVAL and call(T=-1) == EINVAL
+    assert call(T=1 << 26, N=1 << 20) == EINVAL and call(T=1 << 26, K=1 << 20) == EINVAL
     assert call(weight_type=I8) == EINVAL and call(weight_type=F16) == EINVAL and call(down=FAKE + 1) == EINVAL
     assert call(x=rows(1024, F32)) == EINVAL and call(out=rows(48, I8, step=FAKE)) == EINVAL and call(base=rows(48, F16)) == EINVAL
     assert call(x=rows(1024, stride=1020)) == EINVAL and call(x=rows(1024, step=FAKE)) == EINVAL
