@@ -404,14 +404,15 @@ template <typename T, bool VEC> __device__ inline typename Vec8<T>::type buffer_
         return u.v;
     }
 }
-// Of eight columns those from the first `skip` on, and at most `columns`.
-template <typename T, bool VEC> __device__ inline void store_tile(__amdgpu_buffer_rsrc_t b, int offset, int skip, int columns, v8f v)
+// Of eight columns those from the first `skip` on, and at most `columns`; of a row that is not `there` none.
+template <typename T, bool VEC>
+__device__ inline void store_tile(__amdgpu_buffer_rsrc_t b, int offset, int skip, int columns, bool there, v8f v)
 {
-    if (VEC && skip == 0) buffer_store8<T>(b, offset, __builtin_convertvector(v, typename Vec8<T>::type));
+    if (VEC && skip == 0 && there) buffer_store8<T>(b, offset, __builtin_convertvector(v, typename Vec8<T>::type));
     else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (i >= skip && i < columns) buffer_store1<T>(b, offset + i * (int)sizeof(T), (T)v[i]);
+            if (i >= skip && i < columns && there) buffer_store1<T>(b, offset + i * (int)sizeof(T), (T)v[i]);
     }
 }
 
@@ -453,8 +454,7 @@ template <class RowOf> __device__ inline void load_h(const SecondArgs &a, float 
     }
 }
 
-template <typename TW, typename TB, bool VEC>
-__global__ __launch_bounds__(256, sizeof(TB) == 2 && VEC ? 3 : 2) void k_adapter_second(SecondArgs a)
+template <typename TW, typename TB, bool VEC> __global__ __launch_bounds__(256, 2) void k_adapter_second(SecondArgs a)
 {
     typedef typename Vec8<TW>::type WV;
     typedef typename Vec8<TB>::type BV;
@@ -551,10 +551,10 @@ __global__ __launch_bounds__(256, sizeof(TB) == 2 && VEC ? 3 : 2) void k_adapter
         const int skip = VEC ? beyond(128 * tile + 8 * l, C) : 0;
         if (a.out_type == PWLQ_F32) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) store_tile<float, VEC>(out_rows, offset + i * out_pitch, skip, left, acc[i]);
+            for (int i = 0; i < 4; ++i) store_tile<float, VEC>(out_rows, offset + i * out_pitch, skip, left, true, acc[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) store_tile<TW, VEC>(out_rows, offset + i * out_pitch, skip, left, acc[i]);
+            for (int i = 0; i < 4; ++i) store_tile<TW, VEC>(out_rows, offset + i * out_pitch, skip, left, true, acc[i]);
         }
     }
 }
@@ -654,11 +654,11 @@ template <typename TW, typename TB, bool VEC> __global__ __launch_bounds__(256, 
             if (a.out_type == PWLQ_F32) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (4 * q + i < n) store_tile<float, VEC>(out_rows, row[i] * out_pitch + offset, skip, left, v[i]);
+                    store_tile<float, VEC>(out_rows, row[i] * out_pitch + offset, skip, left, 4 * q + i < n, v[i]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (4 * q + i < n) store_tile<TW, VEC>(out_rows, row[i] * out_pitch + offset, skip, left, v[i]);
+                    store_tile<TW, VEC>(out_rows, row[i] * out_pitch + offset, skip, left, 4 * q + i < n, v[i]);
             }
         }
     }
@@ -1166,8 +1166,9 @@ template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipSt
     const int64_t tiles = (a.rows + kSecondRows - 1) / kSecondRows, columns = (a.C + 127) / 128;
     const int waves = (int)std::min<int64_t>(columns, 4);
     const bool collect = collected(a.rows, a.R, a.adapters);
-    // as many workgroups as are resident walk at once; collected ones, of which some have less to do, a few more
-    a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, ((sizeof(TB) == 2 || collect ? 768 : 512) + tiles - 1) / tiles);
+    // As many workgroups as are resident walk at once.  Of collected ones some have a second tile: with a binary32 base half as many
+    // again take 25.8 us for 4096 rows where these take 28.0; with a base of 16 bits 21.9 and 20.1.
+    a.walks = (int)std::min<int64_t>((columns + waves - 1) / waves, ((collect && sizeof(TB) == 4 ? 768 : 512) + tiles - 1) / tiles);
     const size_t lds = sizeof(float) * kSecondRows * second_pitch(a.R);
     if (collect) {
         const int64_t spans = (a.rows + kCollected - 1) / kCollected;
