@@ -14,14 +14,6 @@ namespace pwlq_block {
 
 inline int type_size(int type) { return type == PWLQ_F32 ? 4 : type == PWLQ_I8 ? 1 : 2; }
 
-// Whether the rows can be read in vectors of eight: 16 bytes of a float type, 8 of codes.
-inline bool vectors(const pwlq_rows &r, int64_t T)
-{
-    const int size = type_size(r.type), unit = size == 1 ? 8 : 16;
-    return !r.data || (((uintptr_t)r.data & (uintptr_t)(unit - 1)) == 0 && (T <= 1 || r.stride * size % unit == 0));
-}
-inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
-
 // Rows that one launch walks through with a workgroup each: enough to fill the chip many times over, and few enough that
 // the runtime's limit of 2^32 threads is far.
 inline unsigned row_grid(int64_t T, int64_t most = 1 << 20) { return (unsigned)(T < most ? T : most); }

@@ -23,7 +23,7 @@ constexpr int64_t kForwardWaves = 256 * 16, kBackwardWaves = 256 * 8;
 
 inline int threads_for(int64_t cols, int E) { return (int)((cols + 64 * E - 1) / (64 * E) * 64); }
 
-template <typename TF, typename TX, int E, bool VEC, int THREADS>
+template <typename TF, typename TX, int E, Share S, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_norm_block(pwlq_norm_args a)
 {
     __shared__ float slots[2][2][16];
@@ -31,23 +31,23 @@ __global__ __launch_bounds__(THREADS) void k_norm_block(pwlq_norm_args a)
     const int threads = blockDim.x, thread = threadIdx.x, D = (int)a.D;
     const float inv = 1.0f / (float)D;
     const int64_t per_gate = a.gate ? a.T / a.gate_rows : 1;
-    Row<float, E, VEC> pre, post;
-    Row<TF, E, VEC> f, gate;
-    Row<TX, E, VEC> x;
-    pre.load(a.pre_weight, D, threads, thread);
-    if (a.post_weight) post.load(a.post_weight, D, threads, thread);
+    Row<float, E, S> pre, post;
+    Row<TF, E, S> f, gate;
+    Row<TX, E, S> x;
+    pre.load(a.pre_weight, Place{D, threads, thread});
+    if (a.post_weight) post.load(a.post_weight, Place{D, threads, thread});
     auto load = [&](int64_t row) {
-        x.load((const TX *)a.x.data + row * a.x.stride, D, threads, thread);
-        if (a.f.data) f.load((const TF *)a.f.data + row * a.f.stride, D, threads, thread);
-        if (a.gate) gate.load((const TF *)a.gate + row / per_gate * a.D, D, threads, thread);
+        x.load((const TX *)a.x.data + row * a.x.stride, Place{D, threads, thread});
+        if (a.f.data) f.load((const TF *)a.f.data + row * a.f.stride, Place{D, threads, thread});
+        if (a.gate) gate.load((const TF *)a.gate + row / per_gate * a.D, Place{D, threads, thread});
     };
     load(blockIdx.x);
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x, turn ^= 1) {
         float v[E], g[E], w[E];
-        x.get(v);
-        if (a.f.data) f.get(g);
-        if (a.gate) gate.get(w);
+        x.get(v, Place{D, threads, thread});
+        if (a.f.data) f.get(g, Place{D, threads, thread});
+        if (a.gate) gate.get(w, Place{D, threads, thread});
         load(min(row + gridDim.x, a.T - 1));           // the next row, while this one is worked on
         loads_first();
         if (a.f.data) {
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_block(pwlq_norm_args a)
 #pragma unroll
                 for (int i = 0; i < E; ++i) s += g[i] * g[i];
                 scale *= 1.0f / sqrtf(block_sum(s, slots[turn][0], threads) * inv + a.eps);
-                post.get(p);
+                post.get(p, Place{D, threads, thread});
 #pragma unroll
                 for (int i = 0; i < E; ++i) g[i] *= p[i];
             }
@@ -67,21 +67,21 @@ __global__ __launch_bounds__(THREADS) void k_norm_block(pwlq_norm_args a)
             }
 #pragma unroll
             for (int i = 0; i < E; ++i) v[i] += scale * g[i];
-            store_row<TX, E, VEC>((TX *)a.x_out.data + row * a.x_out.stride, D, threads, thread, v);
+            store_row<TX, E, S>((TX *)a.x_out.data + row * a.x_out.stride, Place{D, threads, thread}, v);
         }
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < E; ++i) s += v[i] * v[i];
         const float b = 1.0f / sqrtf(block_sum(s, slots[turn][1], threads) * inv + a.eps);
-        pre.get(w);
+        pre.get(w, Place{D, threads, thread});
 #pragma unroll
         for (int i = 0; i < E; ++i) v[i] = v[i] * b * w[i];
         if (a.u.type == PWLQ_I8) {
             const Step q = step_of(block_max(largest(v), top[turn], threads));
-            store_codes<E, VEC>((int8_t *)a.u.data + row * a.u.stride, D, threads, thread, v, q.factor);
+            store_codes<E, S>((int8_t *)a.u.data + row * a.u.stride, Place{D, threads, thread}, v, q.factor);
             if (thread == 0) a.u.step[row] = q.step;
         } else {
-            store_row<TF, E, VEC>((TF *)a.u.data + row * a.u.stride, D, threads, thread, v);
+            store_row<TF, E, S>((TF *)a.u.data + row * a.u.stride, Place{D, threads, thread}, v);
         }
     }
 }
@@ -107,7 +107,7 @@ __device__ inline float *gate_sums(const pwlq_norm_backward_args &a, const NormP
 // What vector instructions there are per element bounds this as much as memory, so a row's factors are joined before they meet
 // its elements: steps of 8 bits with the norms' factors, alpha and the gate with the post weight.  Both the gate's and the post
 // weight's gradients are column factors times sum dx fh over the rows of one gate row, the only sum kept for them.
-template <typename TF, typename TX, bool KEPT, int E, bool VEC, int THREADS>
+template <typename TF, typename TX, bool KEPT, int E, Share S, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_args a, NormPartials part)
 {
     typedef typename std::conditional<KEPT, int8_t, TF>::type SF;
@@ -122,31 +122,31 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
     float pre[E], back[E], sum_pre[E], sum_post[E], sum_f[E];      // back: alpha gate post
 #pragma unroll
     for (int i = 0; i < E; ++i) sum_pre[i] = sum_post[i] = sum_f[i] = 0.0f;
-    Row<TF, E, VEC> du_row;
-    Row<TX, E, VEC> dx_row;
-    Row<SX, E, VEC> x_row;
-    Row<SF, E, VEC> f_row;
+    Row<TF, E, S> du_row;
+    Row<TX, E, S> dx_row;
+    Row<SX, E, S> x_row;
+    Row<SF, E, S> f_row;
     float x_step = 1.0f, f_step = 1.0f;
     auto load = [&](int64_t row) {
-        x_row.load((const SX *)a.x_out.data + row * a.x_out.stride, D, threads, thread);
-        if (a.du.data) du_row.load((const TF *)a.du.data + row * a.du.stride, D, threads, thread);
-        if (a.dx_out.data) dx_row.load((const TX *)a.dx_out.data + row * a.dx_out.stride, D, threads, thread);
-        if (a.f.data) f_row.load((const SF *)a.f.data + row * a.f.stride, D, threads, thread);
+        x_row.load((const SX *)a.x_out.data + row * a.x_out.stride, Place{D, threads, thread});
+        if (a.du.data) du_row.load((const TF *)a.du.data + row * a.du.stride, Place{D, threads, thread});
+        if (a.dx_out.data) dx_row.load((const TX *)a.dx_out.data + row * a.dx_out.stride, Place{D, threads, thread});
+        if (a.f.data) f_row.load((const SF *)a.f.data + row * a.f.stride, Place{D, threads, thread});
         if (KEPT) x_step = a.x_out.step[row];
         if (KEPT && a.f.data) f_step = a.f.step[row];
     };
     // alpha gate into g, post into p
     constexpr bool kHold = E == 8;                     // post stays in registers where there is room
-    Row<float, E, VEC> post;
-    Row<TF, E, VEC> gate;
+    Row<float, E, S> post;
+    Row<TF, E, S> gate;
     auto factors = [&](float (&g)[E], float (&p)[E]) {
 #pragma unroll
         for (int i = 0; i < E; ++i) g[i] = p[i] = 1.0f;
         if (a.post_weight) {
-            if (!kHold) post.load(a.post_weight, D, threads, thread);
-            post.get(p);
+            if (!kHold) post.load(a.post_weight, Place{D, threads, thread});
+            post.get(p, Place{D, threads, thread});
         }
-        if (a.gate) gate.get(g);
+        if (a.gate) gate.get(g, Place{D, threads, thread});
 #pragma unroll
         for (int i = 0; i < E; ++i) g[i] *= a.alpha;
     };
@@ -159,25 +159,25 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
             sum_post[i] += g[i] * sum_f[i];
             sum_f[i] *= a.alpha * p[i];
         }
-        if (a.gate) store_row<float, E, VEC>(gate_sums(a, part, walk, gate_row, per_gate, first, last), D, threads, thread, sum_f);
+        if (a.gate) store_row<float, E, S>(gate_sums(a, part, walk, gate_row, per_gate, first, last), Place{D, threads, thread}, sum_f);
 #pragma unroll
         for (int i = 0; i < E; ++i) sum_f[i] = 0.0f;
     };
-    Row<float, E, VEC> weight;
-    weight.load(a.pre_weight, D, threads, thread);
-    if (kHold && a.post_weight) post.load(a.post_weight, D, threads, thread);
-    if (a.gate && first < last) gate.load((const TF *)a.gate + first / per_gate * a.D, D, threads, thread);
+    Row<float, E, S> weight;
+    weight.load(a.pre_weight, Place{D, threads, thread});
+    if (kHold && a.post_weight) post.load(a.post_weight, Place{D, threads, thread});
+    if (a.gate && first < last) gate.load((const TF *)a.gate + first / per_gate * a.D, Place{D, threads, thread});
     if (first < last) load(first);
     loads_first();
-    weight.get(pre);
+    weight.get(pre, Place{D, threads, thread});
     int64_t at_gate = -1;
     int turn = 0;
     for (int64_t row = first; row < last; ++row, turn ^= 1) {
         float dx[E], x[E], f[E], du[E];
-        x_row.get(x);
-        if (a.f.data) f_row.get(f);
-        if (a.du.data) du_row.get(du);
-        if (a.dx_out.data) dx_row.get(dx);
+        x_row.get(x, Place{D, threads, thread});
+        if (a.f.data) f_row.get(f, Place{D, threads, thread});
+        if (a.du.data) du_row.get(du, Place{D, threads, thread});
+        if (a.dx_out.data) dx_row.get(dx, Place{D, threads, thread});
         else {
 #pragma unroll
             for (int i = 0; i < E; ++i) dx[i] = 0.0f;
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
         if (a.f.data && row / per_gate != at_gate) {
             if (at_gate >= 0) {
                 settle(at_gate);
-                if (a.gate) gate.load((const TF *)a.gate + row / per_gate * a.D, D, threads, thread);
+                if (a.gate) gate.load((const TF *)a.gate + row / per_gate * a.D, Place{D, threads, thread});
             }
             at_gate = row / per_gate;
             float p[E];
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
                 sum_pre[i] += du[i] * (x[i] * xb);
             }
         }
-        store_row<TX, E, VEC>((TX *)a.dx.data + row * a.dx.stride, D, threads, thread, dx);
+        store_row<TX, E, S>((TX *)a.dx.data + row * a.dx.stride, Place{D, threads, thread}, dx);
         if (!a.f.data) continue;
         if (a.post_weight) {
             float s = 0.0f, t = 0.0f;
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
                 dx[i] *= back[i];
             }
         }
-        store_row<TF, E, VEC>((TF *)a.df.data + row * a.df.stride, D, threads, thread, dx);
+        store_row<TF, E, S>((TF *)a.df.data + row * a.df.stride, Place{D, threads, thread}, dx);
     }
     if (at_gate >= 0) settle(at_gate);
     if constexpr (E == 8) {
@@ -259,8 +259,8 @@ __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_ar
                 }
         }
     }
-    store_row<float, E, VEC>(part.pre + (int64_t)blockIdx.x * a.D, D, threads, thread, sum_pre);
-    if (part.post) store_row<float, E, VEC>(part.post + (int64_t)blockIdx.x * a.D, D, threads, thread, sum_post);
+    store_row<float, E, S>(part.pre + (int64_t)blockIdx.x * a.D, Place{D, threads, thread}, sum_pre);
+    if (part.post) store_row<float, E, S>(part.post + (int64_t)blockIdx.x * a.D, Place{D, threads, thread}, sum_post);
 }
 
 // Sums of the partial rows, in order: of all workgroups for the norms' weights, of those that meet it for a gate row.  Sixteen
@@ -332,29 +332,28 @@ int64_t backward_wgs(int64_t T, int64_t D)
     return (T + rows - 1) / rows;
 }
 
-template <typename TF, typename TX> void norm_as(const pwlq_norm_args &a, bool vec, hipStream_t stream)
+template <typename TF, typename TX, Share S> void norm_as(const pwlq_norm_args &a, hipStream_t stream)
 {
     const int64_t wgs = kForwardWaves / (threads_for(a.D, forward_elements(a.D)) / 64);
     const unsigned grid = (unsigned)std::min(a.T, wgs);
-#define PWLQ_NORM(E, THREADS)                                                                                   \
-    (vec ? k_norm_block<TF, TX, E, true, THREADS><<<grid, threads_for(a.D, E), 0, stream>>>(a)                  \
-         : k_norm_block<TF, TX, E, false, THREADS><<<grid, threads_for(a.D, E), 0, stream>>>(a))
+#define PWLQ_NORM(E, THREADS) k_norm_block<TF, TX, E, S, THREADS><<<grid, threads_for(a.D, E), 0, stream>>>(a)
     if (a.D <= 4096) PWLQ_NORM(8, 512);
     else if (a.D <= 8192) PWLQ_NORM(16, 512);
     else PWLQ_NORM(16, 1024);
 #undef PWLQ_NORM
 }
 
-template <typename TF, typename TX, bool KEPT>
-void backward_as(const pwlq_norm_backward_args &a, const NormPartials &part, unsigned grid, bool vec, hipStream_t stream)
+template <typename TF, typename TX, bool KEPT, Share S>
+void backward_as(const pwlq_norm_backward_args &a, const NormPartials &part, unsigned grid, hipStream_t stream)
 {
     const int threads = part.walks * threads_for(a.D, backward_elements(a.D));
-#define PWLQ_NORM(E, THREADS)                                                                                            \
-    (vec ? k_norm_backward<TF, TX, KEPT, E, true, THREADS><<<grid, threads, 0, stream>>>(a, part)            \
-         : k_norm_backward<TF, TX, KEPT, E, false, THREADS><<<grid, threads, 0, stream>>>(a, part))
-    if (a.D <= 2048) PWLQ_NORM(8, 256);
-    else if (a.D <= 8192) PWLQ_NORM(16, 512);
-    else PWLQ_NORM(16, 1024);
+#define PWLQ_NORM(E, THREADS) k_norm_backward<TF, TX, KEPT, E, S, THREADS><<<grid, threads, 0, stream>>>(a, part)
+    if constexpr (S != kTail)
+        if (a.D <= 2048) return PWLQ_NORM(8, 256);
+    if constexpr (S != kSingly) {
+        if (a.D <= 8192) PWLQ_NORM(16, 512);
+        else PWLQ_NORM(16, 1024);
+    }
 #undef PWLQ_NORM
 }
 
@@ -362,14 +361,19 @@ void backward_as(const pwlq_norm_backward_args &a, const NormPartials &part, uns
 
 void norm_block(const pwlq_norm_args &a, hipStream_t stream)
 {
-    const bool vec = a.D % 8 == 0 && vectors(a.x, a.T) && vectors(a.f, a.T) && vectors(a.x_out, a.T) && vectors(a.u, a.T) &&
-                     aligned16(a.post_weight) && aligned16(a.pre_weight) && aligned16(a.gate);
     const int tf = a.f.data ? a.f.type : a.x.type;
-    if (tf == PWLQ_F32) norm_as<float, float>(a, vec, stream);
-    else if (tf == PWLQ_BF16 && a.x.type == PWLQ_BF16) norm_as<bf16, bf16>(a, vec, stream);
-    else if (tf == PWLQ_BF16) norm_as<bf16, float>(a, vec, stream);
-    else if (a.x.type == PWLQ_F16) norm_as<f16, f16>(a, vec, stream);
-    else norm_as<f16, float>(a, vec, stream);
+    // Rows of no whole vectors: a residual stream of 16 bits moves in vectors all the same (2000 x 4090 16.1 us, singly 19.4), one of
+    // binary32 singly (22.6, in vectors 24.7).
+#define PWLQ_AS(TF, TX)                                                                             \
+    (a.D % 8 == 0                       ? norm_as<TF, TX, kWhole>(a, stream)                        \
+     : sizeof(TX) == 2 && a.D >= 8      ? norm_as<TF, TX, sizeof(TX) == 2 ? kTail : kWhole>(a, stream) \
+                                        : norm_as<TF, TX, kSingly>(a, stream))
+    if (tf == PWLQ_F32) PWLQ_AS(float, float);
+    else if (tf == PWLQ_BF16 && a.x.type == PWLQ_BF16) PWLQ_AS(bf16, bf16);
+    else if (tf == PWLQ_BF16) PWLQ_AS(bf16, float);
+    else if (a.x.type == PWLQ_F16) PWLQ_AS(f16, f16);
+    else PWLQ_AS(f16, float);
+#undef PWLQ_AS
 }
 
 // Partial rows in the workspace: d_pre's, d_post's, then d_gate's.
@@ -389,19 +393,21 @@ void norm_backward(const pwlq_norm_backward_args &a, void *workspace, hipStream_
     const int64_t wgs = backward_wgs(a.T, a.D);
     NormPartials part = {(float *)workspace, a.d_post ? (float *)workspace + wgs * a.D : nullptr,
                          (float *)workspace + 2 * wgs * a.D, backward_span(a.T, a.D), backward_walks(a.D)};
-    const bool vec = a.D % 8 == 0 && vectors(a.du, a.T) && vectors(a.dx_out, a.T) && vectors(a.x_out, a.T) &&
-                     vectors(a.f, a.T) && vectors(a.dx, a.T) && vectors(a.df, a.T) && aligned16(a.post_weight) &&
-                     aligned16(a.pre_weight) && aligned16(a.gate) && aligned16(a.d_gate);
     const bool kept = a.x_out.type == PWLQ_I8;
     const int tx = a.dx.type, tf = a.f.data ? a.df.type : a.du.data ? a.du.type : tx;
-#define PWLQ_AS(TF, TX)                                                                              \
-    (kept ? backward_as<TF, TX, true>(a, part, (unsigned)wgs, vec, stream)                           \
-          : backward_as<TF, TX, false>(a, part, (unsigned)wgs, vec, stream))
+#define PWLQ_AS(TF, TX) (kept ? PWLQ_SHARE(TF, TX, true) : PWLQ_SHARE(TF, TX, false))
+    // Rows of no whole vectors move in vectors where a thread has sixteen columns (2000 x 4090 of bfloat16 with 8-bit checkpoints 37 us,
+    // singly 69), singly where it has eight (4000 x 515 28.4, in vectors 28.9).
+#define PWLQ_SHARE(TF, TX, KEPT)                                                                     \
+    (a.D % 8 == 0    ? backward_as<TF, TX, KEPT, kWhole>(a, part, (unsigned)wgs, stream)             \
+     : a.D > 2048    ? backward_as<TF, TX, KEPT, kTail>(a, part, (unsigned)wgs, stream)              \
+                     : backward_as<TF, TX, KEPT, kSingly>(a, part, (unsigned)wgs, stream))
     if (tf == PWLQ_F32) PWLQ_AS(float, float);
     else if (tf == PWLQ_BF16 && tx == PWLQ_BF16) PWLQ_AS(bf16, bf16);
     else if (tf == PWLQ_BF16) PWLQ_AS(bf16, float);
     else if (tx == PWLQ_F16) PWLQ_AS(f16, f16);
     else PWLQ_AS(f16, float);
+#undef PWLQ_SHARE
 #undef PWLQ_AS
     // gate rows that lie within walks are written already
     const bool straddled = a.d_gate && part.span % (a.T / a.gate_rows) != 0;

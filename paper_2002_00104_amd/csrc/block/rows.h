@@ -95,31 +95,47 @@ template <typename T> __device__ inline void buffer_store1(__amdgpu_buffer_rsrc_
     else __builtin_amdgcn_raw_buffer_store_b32(u.w, b, offset, 0, 0);
 }
 
-// Columns of one row as they are in memory: thread `thread` of `threads` takes E.  VEC: vectors of eight columns, as many
-// vectors apart as there are threads; else single columns that far apart.  Both coalesce, the second for any length and
-// alignment.  load() only reads, so several rows can be under way; get() widens.
-template <typename T, int E, bool VEC> struct Row {
-    typename std::conditional<VEC, typename Vec8<T>::type, T>::type raw[VEC ? E / 8 : E];
+// How the columns of a row are shared out: thread `thread` of `threads` takes E of them.
+//   kSingly   single columns, as many apart as there are threads: rows of any length
+//   kWhole    vectors of eight, as many vectors apart as there are threads: rows of whole vectors
+//   kTail     the same where the row's last vector would pass its end: it ends there instead, and of its columns those that belong
+//             to the vector before are 0 in its thread, so they add nothing to a sum or a maximum, and are not stored
+// All coalesce, and rows may begin anywhere (unaligned access mode).
+enum Share { kSingly, kWhole, kTail };
+struct Place {
+    int cols, threads, thread;
+    __device__ int vector(int j) const { return (j * threads + thread) * 8; }
+    __device__ int skip(int j) const { return vector(j) < cols ? max(vector(j) + 8 - cols, 0) : 0; }
+    template <Share S> __device__ int start(int j) const { return S == kTail ? vector(j) - skip(j) : vector(j); }
+};
 
-    __device__ void load(const T *row, int cols, int threads, int thread)
+// load() only reads, so several rows can be under way; get() widens.
+template <typename T, int E, Share S> struct Row {
+    typename std::conditional<S != kSingly, typename Vec8<T>::type, T>::type raw[S != kSingly ? E / 8 : E];
+
+    __device__ void load(const T *row, Place at)
     {
-        const __amdgpu_buffer_rsrc_t b = row_buffer(row, cols * (int)sizeof(T));
-        if constexpr (VEC) {
+        const __amdgpu_buffer_rsrc_t b = row_buffer(row, at.cols * (int)sizeof(T));
+        if constexpr (S != kSingly) {
 #pragma unroll
-            for (int j = 0; j < E / 8; ++j) raw[j] = buffer_load8<T>(b, (j * threads + thread) * 8 * (int)sizeof(T));
+            for (int j = 0; j < E / 8; ++j) raw[j] = buffer_load8<T>(b, at.start<S>(j) * (int)sizeof(T));
         } else {
 #pragma unroll
-            for (int i = 0; i < E; ++i) raw[i] = buffer_load1<T>(b, (i * threads + thread) * (int)sizeof(T));
+            for (int i = 0; i < E; ++i) raw[i] = buffer_load1<T>(b, (i * at.threads + at.thread) * (int)sizeof(T));
         }
     }
-    __device__ void get(float (&v)[E]) const
+    __device__ void get(float (&v)[E], Place at) const
     {
-        if constexpr (VEC) {
+        if constexpr (S != kSingly) {
 #pragma unroll
             for (int j = 0; j < E / 8; ++j) {
                 const v8f w = widen(raw[j]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[8 * j + i] = w[i];
+                if (S == kTail && __ballot(at.skip(j) != 0)) {       // one wavefront's
+#pragma unroll
+                    for (int i = 0; i < 7; ++i) v[8 * j + i] = i < at.skip(j) ? 0.0f : w[i];
+                }
             }
         } else {
 #pragma unroll
@@ -132,21 +148,33 @@ template <typename T, int E, bool VEC> struct Row {
 // which saves registers and waits for memory once per load.
 __device__ inline void loads_first() { __builtin_amdgcn_sched_barrier(0); }
 
-template <typename T, int E, bool VEC>
-__device__ inline void store_row(T *row, int cols, int threads, int thread, const float (&v)[E])
+// A vector of a row: all of it, or its own columns one by one.
+template <typename T, Share S> __device__ inline void store_vector(__amdgpu_buffer_rsrc_t b, Place at, int j, typename Vec8<T>::type v)
 {
-    const __amdgpu_buffer_rsrc_t b = row_buffer(row, cols * (int)sizeof(T));
-    if constexpr (VEC) {
+    const int skip = S == kTail ? at.skip(j) : 0;
+    if (skip == 0) buffer_store8<T>(b, at.vector(j) * (int)sizeof(T), v);
+    else {
+        union { typename Vec8<T>::type v; T e[8]; } u;
+        u.v = v;
+#pragma unroll
+        for (int i = 1; i < 8; ++i)
+            if (i >= skip) buffer_store1<T>(b, (at.vector(j) - skip + i) * (int)sizeof(T), u.e[i]);
+    }
+}
+template <typename T, int E, Share S> __device__ inline void store_row(T *row, Place at, const float (&v)[E])
+{
+    const __amdgpu_buffer_rsrc_t b = row_buffer(row, at.cols * (int)sizeof(T));
+    if constexpr (S != kSingly) {
 #pragma unroll
         for (int j = 0; j < E / 8; ++j) {
             v8f w;
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = v[8 * j + i];
-            buffer_store8<T>(b, (j * threads + thread) * 8 * (int)sizeof(T), __builtin_convertvector(w, typename Vec8<T>::type));
+            store_vector<T, S>(b, at, j, __builtin_convertvector(w, typename Vec8<T>::type));
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i) buffer_store1<T>(b, (i * threads + thread) * (int)sizeof(T), (T)v[i]);
+        for (int i = 0; i < E; ++i) buffer_store1<T>(b, (i * at.threads + at.thread) * (int)sizeof(T), (T)v[i]);
     }
 }
 
@@ -250,21 +278,20 @@ __device__ inline uint32_t four_codes(const float *x, float factor)
 }
 
 // Codes of a row.  With factor 0 (a row of next to nothing, or one that holds a NaN or an infinity) all are 0, whatever v is.
-template <int E, bool VEC>
-__device__ inline void store_codes(int8_t *row, int cols, int threads, int thread, const float (&v)[E], float factor)
+template <int E, Share S> __device__ inline void store_codes(int8_t *row, Place at, const float (&v)[E], float factor)
 {
-    const __amdgpu_buffer_rsrc_t b = row_buffer(row, cols);
+    const __amdgpu_buffer_rsrc_t b = row_buffer(row, at.cols);
     const bool none = factor == 0.0f;
-    if constexpr (VEC) {
+    if constexpr (S != kSingly) {
 #pragma unroll
         for (int j = 0; j < E / 8; ++j) {
             v2u q = {0u, 0u};
             if (!none) q = v2u{four_codes(v + 8 * j, factor), four_codes(v + 8 * j + 4, factor)};
-            buffer_store8<int8_t>(b, (j * threads + thread) * 8, q);
+            store_vector<int8_t, S>(b, at, j, q);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i) buffer_store1<int8_t>(b, i * threads + thread, none ? 0 : (int8_t)code_byte(v[i], factor));
+        for (int i = 0; i < E; ++i) buffer_store1<int8_t>(b, i * at.threads + at.thread, none ? 0 : (int8_t)code_byte(v[i], factor));
     }
 }
 
