@@ -745,7 +745,7 @@ struct TokenArgs {
     float *h;
     int R, adapters, base_type, out_type;
 };
-constexpr int kTokenThreads = 1024, kTokenColumns = 512, kTokenWaves = kTokenThreads / 64, kTokenRanks = 64;
+constexpr int kTokenThreads = 1024, kTokenColumns = 512, kTokenWaves = kTokenThreads / 64, kTokenRanks = 48;
 
 template <typename TX, typename TW, bool VEC>
 __global__ __launch_bounds__(kTokenThreads) void k_adapter_token(TokenArgs a)
@@ -1098,7 +1098,6 @@ __global__ void k_zero(float *a, int64_t na, float *b, int64_t nb)
 // --------------------------------------------------------------------------
 // launches
 // --------------------------------------------------------------------------
-constexpr int64_t kTokenRows = 16;     // up to so many rows each is done by itself
 
 int rank_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }
 int rank_blocks(int R) { return (R + 16 * rank_tiles(R) - 1) / (16 * rank_tiles(R)); }
@@ -1210,11 +1209,18 @@ void first(const FirstArgs &a, int x_type, int w_type, bool vec, hipStream_t str
 }
 
 
-constexpr int64_t kSingleRows = 64;    // up to so many rows the second product does each by itself
+// Whether the second product does each row by itself, reading its adapter for it alone.  Both products of 4096 x 4096, 16 ranks, in us,
+// by tiles -> by rows, adapters alternating: 32 rows of 8 adapters 13.5 -> 9.3, 128 rows 14.6 -> 10.5, 256 rows 14.2 -> 12.7, 384 rows
+// 15.4 -> 15.7; of 32 adapters 256 rows 24.0 -> 17.1; of one adapter 128 rows 9.3 both ways, 384 rows 9.8 -> 13.7; of 8 adapters of 64
+// ranks 128 rows 18.1 -> 17.0, 256 rows 19.4 -> 21.2.
+bool by_rows(int64_t rows, int R, int adapters)
+{
+    return rows <= (adapters > 1 ? 256 : 64) && rows * ((R + 15) / 16 * 16) <= 8192;
+}
 
 template <typename TW, typename TB> void second_as(SecondArgs a, bool vec, hipStream_t stream)
 {
-    if (a.rows <= kSingleRows) {
+    if (by_rows(a.rows, a.R, a.adapters)) {
         const dim3 grid((unsigned)((a.C + 511) / 512), (unsigned)a.rows);
         const int base_type = std::is_same<TB, float>::value ? PWLQ_F32 : -1;
         if (vec) k_adapter_second_row<TW, true><<<grid, 256, 0, stream>>>(a, base_type);
@@ -1274,8 +1280,16 @@ void outer(const OuterArgs &up, const OuterArgs &down, int splits, int x_type, i
     else x_type == PWLQ_I8 ? outer_as<int8_t, f16>(up, down, splits, vec, stream) : outer_as<f16, f16>(up, down, splits, vec, stream);
 }
 
-// Whether few rows go through one launch.
-bool by_token(int64_t T, int R) { return T <= kTokenRows && R <= kTokenRanks; }
+// Whether rows go through one launch: few rounds of a wavefront's ranks and columns, and one workgroup to a CU, or few rows.  Against two
+// launches, bfloat16, in us, 8 adapters: 1 row of 4096 x 4096 with 16 ranks 5.7 and 7.3, 16 rows 6.0 and 9.4, 32 rows 6.3 and 9.4, 48 rows
+// 10.4 and 9.4; 8 rows with 32 ranks 9.1 and 10.3, with 48 11.8 and 11.9, with 64 14.9 and 12.8; 8 rows of 11008 x 4096 with 16 ranks
+// 11.0 and 13.1, with 32 19.3 and 14.2; 4096 x 11008 with 16 ranks 8 rows 6.2 and 8.8, 12 rows 7.1 and 9.2, 24 rows 11.4 and 9.5.
+constexpr int64_t kTokenRows = 12;
+bool few_ranks(int64_t K, int R) { return (R + 15) / 16 * ((K + 4095) / 4096) <= kTokenRanks / 16; }
+bool by_token(int64_t T, int64_t K, int64_t N, int R)
+{
+    return few_ranks(K, R) && (T <= kTokenRows || T * ((N + kTokenColumns - 1) / kTokenColumns) <= 256);
+}
 
 template <typename TX, typename TW> void token_as(const TokenArgs &a, int64_t rows, bool vec, hipStream_t stream)
 {
@@ -1316,14 +1330,14 @@ void token(const pwlq_adapter_args &a, hipStream_t stream)
 
 size_t adapter_workspace(int64_t T, int64_t K, int R)
 {
-    if (by_token(T, R)) return 0;
+    if (T <= kTokenRows && few_ranks(K, R)) return 0;
     const int splits = first_splits(T, K, R);
     return splits > 1 ? (size_t)splits * (size_t)T * (size_t)R * sizeof(float) : 0;
 }
 
 void adapter_forward(const pwlq_adapter_args &a, void *workspace, hipStream_t stream)
 {
-    if (by_token(a.T, a.R)) {
+    if (by_token(a.T, a.K, a.N, a.R)) {
         token(a, stream);
         return;
     }

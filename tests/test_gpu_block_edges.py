@@ -10,7 +10,9 @@ pytestmark = pytest.mark.gpu
 # rows, columns in, columns out, rank, adapters: on both sides of the rule by which rows are collected, T * n * sixteens of ranks >= 2048;
 # rows of one adapter that fill no tile, one more than a span, as many adapters as rows and more
 MANY = [(255, 136, 72, 16, 8), (256, 136, 72, 16, 8), (257, 200, 200, 3, 8), (513, 65, 129, 33, 3), (65, 264, 520, 100, 5),
-        (300, 72, 1160, 17, 300), (770, 520, 40, 8, 1000)]
+        (300, 72, 1160, 17, 300), (770, 520, 40, 8, 1000),
+        # few rows: in one launch or two, by the ranks, the columns and the rows
+        (5, 264, 520, 64, 3), (5, 264, 520, 48, 3), (12, 4100, 600, 40, 4), (20, 5000, 700, 16, 4), (200, 600, 1400, 16, 6), (200, 600, 400, 16, 6)]
 
 
 def ids_of(order, T, n, g):
