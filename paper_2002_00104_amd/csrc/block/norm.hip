@@ -6,7 +6,9 @@
 //   dx   = dx' + b (pre du - xh mean(pre du xh)),   d_pre  = sum over rows of du xh
 //   dv   = alpha gate dx,                           d_gate = sum over its rows of alpha v dx
 //   df   = a (post dv - fh mean(post dv fh)),       d_post = sum over rows of dv fh
-// All of it is bound by memory: a workgroup holds a row in registers and reads each of its values once.
+// The forward pass is bound by memory: a workgroup holds a row in registers and reads each of its values once, the next row's on their
+// way meanwhile.  4096 x 4096, f in bfloat16, the residual stream in binary32, codes out: 36 us, 185 MB, 5.1 TB/s; 8 rows of
+// bfloat16 4.2 us, a launch and a row's chain of three reductions.
 #include <algorithm>
 
 #include "launch.h"
@@ -17,8 +19,8 @@
 namespace pwlq_block {
 namespace {
 
-// Wavefronts that walk the rows at once, as many as are resident: sixteen to a CU, and for the backward pass, which keeps more
-// of a row and the columns' sums in registers, eight.
+// Wavefronts that walk the rows at once, as many as are resident: sixteen to a CU (4096 x 4096 36.8 us; 24 43.8), and for the backward
+// pass, which keeps more of a row and the columns' sums in registers, eight.
 constexpr int64_t kForwardWaves = 256 * 16, kBackwardWaves = 256 * 8;
 
 inline int threads_for(int64_t cols, int E) { return (int)((cols + 64 * E - 1) / (64 * E) * 64); }
@@ -104,7 +106,8 @@ __device__ inline float *gate_sums(const pwlq_norm_backward_args &a, const NormP
     return (g * per >= first && (g + 1) * per <= last ? a.d_gate + g * a.D : part.gate + (walk + g) * a.D);
 }
 
-// What vector instructions there are per element bounds this as much as memory, so a row's factors are joined before they meet
+// 4096 x 4096 of bfloat16 from 8-bit x and f: 42 us for 168 MB, 4.0 TB/s, and 6.7 for the sums of its walks; 515 x 1155 of binary32 9.6
+// and 4.3.  What vector instructions there are per element bounds this as much as memory, so a row's factors are joined before they meet
 // its elements: steps of 8 bits with the norms' factors, alpha and the gate with the post weight.  Both the gate's and the post
 // weight's gradients are column factors times sum dx fh over the rows of one gate row, the only sum kept for them.
 template <typename TF, typename TX, bool KEPT, int E, Share S, int THREADS>
