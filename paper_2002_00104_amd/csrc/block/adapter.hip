@@ -1126,22 +1126,26 @@ int64_t first_chunk(int64_t K, int splits) { return ((K + splits - 1) / splits +
 // Parts of the rows for the outer products: as many workgroups as are resident, four to a CU up to 16 ranks (25.0 us where two
 // take 28.6), two beyond; in blocks of 32 ranks (20.7 us for 64 ranks; of 64 at once 23.3).
 int outer_blocks(int R) { return R <= 16 ? 1 : (R + 31) / 32; }
-int64_t outer_span(int64_t T, int64_t K, int64_t N, int R)
+// A part leaves a sum for each adapter that has rows in it, to be written and read again, so a part has 64 rows for each adapter on
+// average.  The whole backward pass of 4096 x 4096 of bfloat16, 16 ranks, parts for the whole chip -> these, in us: 534 rows of 32 adapters
+// in runs 67 -> 41, alternating 130 -> 50; 4096 rows of 8 adapters 57 -> 56 and 91 -> 73, of 32 85 -> 88 and 254 -> 129, and where
+// all the rows have one of the 32 55 -> 71.
+int64_t outer_span(int64_t T, int64_t K, int64_t N, int R, int adapters)
 {
     const int64_t wgs = ((K + 127) / 128 + (N + 127) / 128) * outer_blocks(R);
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((R <= 16 ? 1024 : 512) / wgs, (T + 63) / 64));
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((R <= 16 ? 1024 : 512) / wgs, adapters > 1 ? T / (64 * adapters) : (T + 63) / 64));
     return ((T + splits - 1) / splits + 63) / 64 * 64;
 }
-int outer_splits(int64_t T, int64_t K, int64_t N, int R)
+int outer_splits(int64_t T, int64_t K, int64_t N, int R, int adapters)
 {
-    const int64_t span = outer_span(T, K, N, R);
+    const int64_t span = outer_span(T, K, N, R, adapters);
     return (int)((T + span - 1) / span);
 }
 
 // Where that leaves CUs idle the adapters are done beside each other.
 int outer_slots(int64_t T, int64_t K, int64_t N, int R, int adapters)
 {
-    const int64_t wgs = ((K + 127) / 128 + (N + 127) / 128) * outer_blocks(R) * outer_splits(T, K, N, R);
+    const int64_t wgs = ((K + 127) / 128 + (N + 127) / 128) * outer_blocks(R) * outer_splits(T, K, N, R, adapters);
     int slots = 1;
     while (2 * slots <= adapters && 2 * slots * wgs <= 1024) slots *= 2;
     return slots;
@@ -1167,7 +1171,7 @@ struct BackwardSpace {
     {
         Carver c = {(char *)workspace};
         const int first = first_splits(T, N, R);
-        splits = outer_splits(T, K, N, R);
+        splits = outer_splits(T, K, N, R, adapters);
         dh = c.take<float>(T * R);
         parts = first > 1 ? c.take<float>(first * T * R) : dh;
         const int64_t all = splits > 1 ? (int64_t)splits * adapters : 0;
@@ -1434,7 +1438,7 @@ void adapter_backward(const pwlq_adapter_backward_args &a, void *workspace, hipS
            a.K >= 8, stream);
     OuterArgs up = {}, down = {};
     up.rows = down.rows = a.T;
-    up.span = down.span = outer_span(a.T, a.K, a.N, a.R);
+    up.span = down.span = outer_span(a.T, a.K, a.N, a.R, a.adapters);
     up.ids = down.ids = a.ids;
     up.R = down.R = a.R;
     up.adapters = down.adapters = a.adapters;
