@@ -49,11 +49,6 @@ __device__ inline float widen(bf16 v) { return (float)v; }
 __device__ inline float widen(f16 v) { return (float)v; }
 __device__ inline float widen(int8_t v) { return (float)v; }
 
-template <typename T> __device__ inline void store8(T *p, v8f v)
-{
-    *(typename Vec8<T>::type *)p = __builtin_convertvector(v, typename Vec8<T>::type);
-}
-
 // A row, or neighbouring rows, as a buffer of their own length: reads beyond its end give 0 and writes there do nothing, by the
 // hardware's bounds check, so threads past the end need no branch and no select.  `row` is the same for the whole wavefront.
 __device__ inline __amdgpu_buffer_rsrc_t row_buffer(const void *row, uint32_t bytes)
