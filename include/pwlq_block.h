@@ -8,8 +8,8 @@
  *
  * Conventions: those of pwlq.h (device pointers owned by the caller, work
  * enqueued on `stream`, nothing allocated, pwlq_last_error), and
- *   - T is the number of rows (tokens).  T = 0 is an empty batch: nothing is
- *     read, and only the gradients of parameters are written (zeros).
+ *   - T is the number of rows (tokens), at most 2^26.  T = 0 is an empty batch:
+ *     nothing is read, and only the gradients of parameters are written (zeros).
  *   - Rows are given as a pwlq_rows: `stride` elements from one row to the next,
  *     the columns of a row next to each other, so a block of columns of a wider
  *     matrix can be passed as it stands.  Outputs must not overlap inputs or
@@ -126,8 +126,8 @@ int pwlq_norm_block_backward(const pwlq_norm_backward_args *args, void *workspac
  *   h      [T, R] binary32: kept for the backward pass
  * Rows without an adapter, and rows of another adapter, are not touched by an
  * adapter's infinities or NaN (its own rows get NaN where the product of such a
- * value may have been an infinity).  1 <= R <= 256, 1 <= adapters <= 65535, an
- * adapter below 2 GiB, strides up to 2^20.
+ * value may have been an infinity).  1 <= R <= 256, 1 <= adapters <= 65535, K, N
+ * and strides up to 2^20, an adapter (R K or R N values) below 2 GiB.
  * Workspace: device, 256-byte aligned, pwlq_adapter_workspace_bytes(T, K, R).
  */
 typedef struct {

@@ -5,7 +5,9 @@
 
 namespace {
 
-constexpr int64_t kMostRows = 1LL << 26;       // grids of all launches stay below 2^32 threads a dimension
+// Grids of all launches stay below 2^32 threads a dimension.  Most have the adapters' collected tiles: 24 workgroups of 256 threads for
+// each 256 rows, 1.6e9 threads, once the rows alone fill the chip; columns add none to that.
+constexpr int64_t kMostRows = 1LL << 26;
 
 constexpr int64_t kMostStride = 1LL << 20;     // 256 rows of binary32 stay below 2 GiB
 bool float_type(int type) { return type == PWLQ_F32 || type == PWLQ_BF16 || type == PWLQ_F16; }
@@ -54,7 +56,6 @@ int check_adapter(int64_t T, int64_t K, int64_t N, int R, int adapters, int type
     if (R < 1 || R > 256) return fail(PWLQ_EINVAL, "R=%d outside [1,256]", R);
     if (adapters < 1 || adapters > 65535) return fail(PWLQ_EINVAL, "adapters=%d outside [1,65535]", adapters);
     if (!float_type(type)) return fail(PWLQ_EINVAL, "weight_type=%d is none of the float types", type);
-    if ((T + 255) / 256 * 512 * ((N > K ? N : K) / 512 + 4) > 0xffffffffLL / 256) return fail(PWLQ_EINVAL, "grid too large");
     // rows and adapters are addressed within tiles by 32 bits
     const int64_t most = (1LL << 31) / pwlq_block::type_size(type);
     if (R * K >= most || R * N >= most) return fail(PWLQ_EINVAL, "an adapter of 2 GiB or more");
