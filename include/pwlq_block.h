@@ -88,11 +88,11 @@ int pwlq_norm_block(const pwlq_norm_args *args, void *stream);
  * Its backward pass: from du and dx_out, the gradients with respect to u and
  * x_out (either may be left out: zero), the gradients
  *     dx      of x (and of x_out in all), type of dx_out or, without it, of x
- *     df      of f, type of du (of f without it)
+ *     df      of f, type of du (without it of f, as the forward pass had it)
  *     d_pre   [D], d_post [D] (NULL where there is no post_weight), d_gate
  *             [gate_rows, D] (NULL where there is no gate): binary32
  * x_out and f are the forward pass's, either both as they were or both as 8-bit
- * rows (PWLQ_I8, with steps).  gate has du's type.  With f left out there is
+ * rows (PWLQ_I8, with steps).  gate has df's type.  With f left out there is
  * only the norm: dx and d_pre.
  * Workspace: device, 256-byte aligned,
  * pwlq_norm_block_backward_workspace_bytes(T, D, gate_rows) bytes.

@@ -54,12 +54,14 @@ def norm_block(x: Tensor, f: Optional[Tensor] = None, *, pre_weight: Tensor, pos
 def norm_block_backward(du: Optional[Tensor], dx_out: Optional[Tensor], x_out: Tensor, f: Optional[Tensor] = None, *,
                         pre_weight: Tensor, post_weight: Optional[Tensor] = None, gate: Optional[Tensor] = None,
                         alpha: float = 1.0, eps: float = 1e-6, x_step: Optional[Tensor] = None,
-                        f_step: Optional[Tensor] = None, workspace: Optional[Tensor] = None) -> Dict[str, Optional[Tensor]]:
+                        f_step: Optional[Tensor] = None, dtype: Optional[torch.dtype] = None,
+                        workspace: Optional[Tensor] = None) -> Dict[str, Optional[Tensor]]:
     """pwlq_norm_block_backward: gradients of norm_block's inputs from those of its outputs, du of u and dx_out of x_out
-    (one of them may be None).  x_out and f as the forward pass had them, or both int8 with their steps.
-    Returns dx, df, d_pre, d_post and d_gate (None where there is no such input)."""
+    (one of them may be None).  x_out and f as the forward pass had them, or both int8 with their steps.  dx has dx_out's type,
+    without it x_out's, or du's where x_out is int8; df has du's, without it f's, or where f is int8 the gate's, else `dtype` (dx's
+    type by default).  Returns dx, df, d_pre, d_post and d_gate (None where there is no such input)."""
     dx, df, d_pre, d_post, d_gate = _pwlq_block.norm_block_backward(
-        du, dx_out, x_out, f, pre_weight, post_weight, gate, alpha, eps, x_step, f_step, workspace, _stream())
+        du, dx_out, x_out, f, pre_weight, post_weight, gate, alpha, eps, x_step, f_step, dtype, workspace, _stream())
     return dict(dx=dx, df=df, d_pre=d_pre, d_post=d_post, d_gate=d_gate)
 
 

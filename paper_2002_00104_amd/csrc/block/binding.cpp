@@ -245,18 +245,20 @@ PyObject *norm_block(PyObject *, PyObject *const *a, Py_ssize_t n)
 }
 
 // du or None, dx_out or None, x_out, f or None, pre_weight, post_weight or None, gate or None, alpha, eps, x_step or None,
-// f_step or None, workspace or None, stream
+// f_step or None, dtype or None, workspace or None, stream
 PyObject *norm_block_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    count("norm_block_backward", n, 13);
+    count("norm_block_backward", n, 14);
     const Tensor *du = tensor("du", a[0]), *dx_out = tensor("dx_out", a[1]), &x_out = needed("x_out", a[2]), *f = tensor("f", a[3]);
     const Tensor &pre = needed("pre_weight", a[4]), *post = tensor("post_weight", a[5]), *gate = tensor("gate", a[6]);
     if (!du && !dx_out) refuse("du and dx_out are both None");
     const Call c("x_out", x_out);
     const bool kept = x_out.scalar_type() == at::kChar;
     const ScalarType stream_type = dx_out ? dx_out->scalar_type() : kept ? du->scalar_type() : x_out.scalar_type();
-    const ScalarType type = du ? du->scalar_type() : f && !kept ? f->scalar_type() : stream_type;
+    // 8-bit checkpoints do not say the type that f had: the gate has it too, or the caller says it
+    const ScalarType said = dtype_of(a[11], stream_type);
+    const ScalarType type = du ? du->scalar_type() : !f ? stream_type : !kept ? f->scalar_type() : gate ? gate->scalar_type() : said;
     if (!is_float(stream_type) || !is_float(type)) refuse("gradients of rows must be float32, bfloat16 or float16");
     pwlq_norm_backward_args args = {};
     args.T = c.T;
@@ -271,7 +273,7 @@ PyObject *norm_block_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     args.gate = gate_of(c, gate, args.D, type, args.gate_rows);
     args.alpha = real(a[7]);
     args.eps = real(a[8]);
-    void *stream = stream_of(a[12]);
+    void *stream = stream_of(a[13]);
     Tensor dx = c.make({c.T, args.D}, stream_type), df, d_pre = c.make({args.D}, at::kFloat), d_post, d_gate, keep;
     args.dx = c.rows("dx", &dx, args.D, stream_type, stream_type);
     args.d_pre = (float *)d_pre.data_ptr();
@@ -288,7 +290,7 @@ PyObject *norm_block_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         args.d_gate = (float *)d_gate.data_ptr();
     }
     size_t bytes = 0;
-    void *room = c.room(a[11], pwlq_norm_block_backward_workspace_bytes(c.T, args.D, args.gate_rows), keep, bytes);
+    void *room = c.room(a[12], pwlq_norm_block_backward_workspace_bytes(c.T, args.D, args.gate_rows), keep, bytes);
     call([&] { return pwlq_norm_block_backward(&args, room, bytes, stream); });
     return tuple(dx, df, d_pre, d_post, d_gate);
     END_HANDLE_TH_ERRORS
