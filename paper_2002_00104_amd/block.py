@@ -10,7 +10,10 @@ last block's output f:
     y, h = adapter(codes, down, up, ids, scale, base=y, x_step=step, base_step=step, dtype=torch.bfloat16)
 
 In training `codes` and `step` are the activation checkpoint that adapter_backward reads, and pack_rows makes those of
-norm_block_backward.  Argument marshalling only: the work is the library's, on the current stream.
+norm_block_backward.  Autograd sees none of it: norm_block and adapter refuse tensors that require gradients unless they are
+called under torch.no_grad(), as in the forward pass of a torch.autograd.Function whose backward calls theirs.
+
+Argument marshalling only: the work is the library's, on the current stream.
 """
 from __future__ import annotations
 

@@ -8,10 +8,14 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <initializer_list>
+#include <utility>
 
 #include "../../../include/pwlq.h"
 #include "../../../include/pwlq_block.h"
@@ -44,6 +48,16 @@ const Tensor &needed(const char *name, PyObject *o)
     const Tensor *t = tensor(name, o);
     if (!t) refuse("%s is None", name);
     return *t;
+}
+
+// What autograd would have to follow through a forward call is refused: the result would be a constant to it.
+void untracked(const char *backward, std::initializer_list<std::pair<const char *, const Tensor *>> tensors)
+{
+    if (!at::GradMode::is_enabled()) return;
+    for (const auto &[name, t] : tensors)
+        if (t && t->requires_grad())
+            refuse("%s requires gradients, and this call records nothing for autograd: %s is its backward pass; call it under torch.no_grad()", name,
+                   backward);
 }
 
 int type_of(ScalarType t)
@@ -220,6 +234,7 @@ PyObject *norm_block(PyObject *, PyObject *const *a, Py_ssize_t n)
     const Tensor &x = needed("x", a[0]), *f = tensor("f", a[1]), &pre = needed("pre_weight", a[2]);
     const Tensor *post = tensor("post_weight", a[3]), *gate = tensor("gate", a[4]);
     const Call c("x", x);
+    untracked("norm_block_backward", {{"x", &x}, {"f", f}, {"pre_weight", &pre}, {"post_weight", post}, {"gate", gate}});
     const ScalarType stream_type = x.scalar_type(), type = f ? f->scalar_type() : stream_type;
     if (!is_float(stream_type) || !is_float(type)) refuse("x and f must be float32, bfloat16 or float16");
     const int pack = PyObject_IsTrue(a[7]);
@@ -328,11 +343,15 @@ PyObject *adapter(PyObject *, PyObject *const *a, Py_ssize_t n)
     const Tensor &x = needed("x", a[0]);
     const Call c("x", x);
     const int64_t K = x.size(1);
-    pwlq_adapter_args args = {};
-    const ScalarType type = adapters(c, args, K, needed("down", a[1]), needed("up", a[2]), needed("ids", a[3]), needed("scale", a[4]));
-    args.x = c.rows("x", &x, K, type, at::kChar, tensor("x_step", a[6]));
-    args.base = c.rows("base", tensor("base", a[5]), args.N, type, at::kFloat, tensor("base_step", a[7]), true);
+    const Tensor &down = needed("down", a[1]), &up = needed("up", a[2]), &scale = needed("scale", a[4]);
+    const Tensor *base = tensor("base", a[5]), *x_step = tensor("x_step", a[6]), *base_step = tensor("base_step", a[7]);
     const Tensor *given = tensor("out", a[9]);
+    untracked("adapter_backward", {{"x", &x}, {"down", &down}, {"up", &up}, {"scale", &scale}, {"base", base}, {"x_step", x_step},
+                                   {"base_step", base_step}, {"out", given}});
+    pwlq_adapter_args args = {};
+    const ScalarType type = adapters(c, args, K, down, up, needed("ids", a[3]), scale);
+    args.x = c.rows("x", &x, K, type, at::kChar, x_step);
+    args.base = c.rows("base", base, args.N, type, at::kFloat, base_step, true);
     void *stream = stream_of(a[11]);
     Tensor out = given ? *given : c.make({c.T, args.N}, dtype_of(a[8], type)), h = c.make({c.T, args.R}, at::kFloat), keep;
     args.out = c.rows("out", &out, args.N, type, at::kFloat);
