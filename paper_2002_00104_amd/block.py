@@ -13,7 +13,7 @@ In training `codes` and `step` are the activation checkpoint that adapter_backwa
 norm_block_backward.  Autograd sees none of it: norm_block and adapter refuse tensors that require gradients unless they are
 called under torch.no_grad(), as in the forward pass of a torch.autograd.Function whose backward calls theirs.
 
-Argument marshalling only: the work is the library's, on the current stream.
+Argument marshalling only: the work is the library's, on the current stream of the current device, where all tensors are.
 """
 from __future__ import annotations
 

@@ -10,6 +10,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -75,7 +76,7 @@ ScalarType dtype_of(PyObject *o, ScalarType otherwise)
     return reinterpret_cast<THPDtype *>(o)->scalar_type;
 }
 
-// What every tensor of a call is checked against.
+// What every tensor of a call is checked against.  The device is the current one: the work is launched there, on its stream.
 struct Call {
     at::Device device;
     int64_t T;
@@ -83,6 +84,8 @@ struct Call {
     Call(const char *name, const Tensor &x) : device(x.device()), T(0)
     {
         if (!x.is_cuda() || x.dim() != 2) refuse("%s must be a matrix on the GPU", name);
+        const at::Device current = c10::impl::VirtualGuardImpl(at::kCUDA).getDevice();
+        if (device != current) refuse("%s is on GPU %d, and the current device is GPU %d", name, (int)device.index(), (int)current.index());
         T = x.size(0);
     }
     Tensor make(at::IntArrayRef sizes, ScalarType type) const { return at::empty(sizes, at::TensorOptions().dtype(type).device(device)); }
