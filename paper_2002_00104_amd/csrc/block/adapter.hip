@@ -1130,10 +1130,15 @@ int outer_blocks(int R) { return R <= 16 ? 1 : (R + 31) / 32; }
 // average.  The whole backward pass of 4096 x 4096 of bfloat16, 16 ranks, parts for the whole chip -> these, in us: 534 rows of 32 adapters
 // in runs 67 -> 41, alternating 130 -> 50; 4096 rows of 8 adapters 57 -> 56 and 91 -> 73, of 32 85 -> 88 and 254 -> 129, and where
 // all the rows have one of the 32 55 -> 71.
+// But a part has fewer than 8192 rows, as far as the sums of parts of 4096 fit 4 GiB: each of its workgroups walks all of it for the adapters of
+// its slot, and a large bank may have few in use.  One part -> these, of 512 adapters: 32768 rows of one 703 -> 383, in runs of all
+// 3119 -> 868, alternating among 8 407 -> 471 and among all 6166 -> 6744; 8192 rows of one 226 -> 208, alternating among 8 144 -> 190.
 int64_t outer_span(int64_t T, int64_t K, int64_t N, int R, int adapters)
 {
     const int64_t wgs = ((K + 127) / 128 + (N + 127) / 128) * outer_blocks(R);
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((R <= 16 ? 1024 : 512) / wgs, adapters > 1 ? T / (64 * adapters) : (T + 63) / 64));
+    const int64_t least = std::min<int64_t>(T / 4096, (4LL << 30) / ((int64_t)sizeof(float) * adapters * R * (K + N)));
+    const int64_t most = adapters > 1 ? std::max<int64_t>(T / (64 * adapters), least) : (T + 63) / 64;
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>((R <= 16 ? 1024 : 512) / wgs, most));
     return ((T + splits - 1) / splits + 63) / 64 * 64;
 }
 int outer_splits(int64_t T, int64_t K, int64_t N, int R, int adapters)
