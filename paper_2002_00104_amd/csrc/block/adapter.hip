@@ -110,6 +110,8 @@ template <int ROWS, int SPAN> struct Tiles {
 // first product
 // --------------------------------------------------------------------------
 // Matrix instructions of eight reduction elements a lane, operands of the weights' type.  Codes of 8 bits are exact in all of them.
+// Products of binary16 values below its normal range (2^-14) are summed with an error of up to 2^-37 by measurement, which is
+// 2^-13 of what one unit of such a value adds.
 template <typename TW> struct Operand { typedef typename Vec8<TW>::type type; };
 template <typename TW, typename TX> __device__ inline typename Operand<TW>::type operand(typename Vec8<TX>::type v)
 {
@@ -897,7 +899,8 @@ struct OuterArgs {
 // after the other.  Its rows are listed in LDS first, 512 at a time, so that no other row is read; the four wavefronts take
 // sixteen of them each in turn, the next ones' loads under way, and add up in LDS.  Bound by memory and, at 64 ranks, by the matrix
 // instructions' thirds: 4096 rows, 4096 codes and 11008 columns of bfloat16, 16 ranks 26 us for 107 MB (4.1 TB/s); 2048 rows, 4096 codes
-// and 4096 columns of bfloat16, 64 ranks 21.5 us, each of its two passes over 32 ranks reading the rows again.
+// and 4096 columns of bfloat16, 64 ranks 21.3 us, each of its two passes over 32 ranks reading the rows again.  With binary32 weights and
+// more than 16 ranks 12 to 36 registers spill.
 constexpr int kListed = 512;
 
 template <int RT> struct OuterLds {
@@ -1306,6 +1309,8 @@ void outer(const OuterArgs &up, const OuterArgs &down, int splits, int x_type, i
 // launches, bfloat16, in us, 8 adapters: 1 row of 4096 x 4096 with 16 ranks 5.7 and 7.3, 16 rows 6.0 and 9.4, 32 rows 6.3 and 9.4, 48 rows
 // 10.4 and 9.4; 8 rows with 32 ranks 9.1 and 10.3, with 48 11.8 and 11.9, with 64 14.9 and 12.8; 8 rows of 11008 x 4096 with 16 ranks
 // 11.0 and 13.1, with 32 19.3 and 14.2; 4096 x 11008 with 16 ranks 8 rows 6.2 and 8.8, 12 rows 7.1 and 9.2, 24 rows 11.4 and 9.5.
+// In binary32, whose rounds are of 2048 columns, the rule is the same: 1 row of 4096 x 4096 with 16 ranks 6.6 and 8.2, 32 rows 7.3 and
+// 10.0; 8 rows with 32 ranks 13.4 and 12.0, with 48 18.3 and 14.9; of 2048 x 4096 with 48 10.4 and 13.9; of 8192 x 4096 with 16 12.8 and 11.9.
 constexpr int64_t kTokenRows = 12;
 bool few_ranks(int64_t K, int R) { return (R + 15) / 16 * ((K + 4095) / 4096) <= kTokenRanks / 16; }
 bool by_token(int64_t T, int64_t K, int64_t N, int R)

@@ -7,8 +7,9 @@
 //   dv   = alpha gate dx,                           d_gate = sum over its rows of alpha v dx
 //   df   = a (post dv - fh mean(post dv fh)),       d_post = sum over rows of dv fh
 // The forward pass is bound by memory: a workgroup holds a row in registers and reads each of its values once, the next row's on their
-// way meanwhile.  4096 x 4096, f in bfloat16, the residual stream in binary32, codes out: 36 us, 185 MB, 5.1 TB/s; 8 rows of
-// bfloat16 4.2 us, a launch and a row's chain of three reductions.
+// way meanwhile.  4096 x 4096, f in bfloat16, the residual stream in binary32, codes out: 36 us, 185 MB, 5.1 TB/s; all in bfloat16 24 us,
+// the norm alone 13 (replayed, inputs partly in the last-level cache); 8 rows of bfloat16 4.0 us, a launch and a row's chain of three
+// reductions.
 #include <algorithm>
 
 #include "launch.h"
@@ -106,10 +107,12 @@ __device__ inline float *gate_sums(const pwlq_norm_backward_args &a, const NormP
     return (g * per >= first && (g + 1) * per <= last ? a.d_gate + g * a.D : part.gate + (walk + g) * a.D);
 }
 
-// 4096 x 4096 of bfloat16 from 8-bit x and f: 42 us for 168 MB, 4.0 TB/s, and 6.7 for the sums of its walks; 515 x 1155 of binary32 9.6
-// and 4.3.  What vector instructions there are per element bounds this as much as memory, so a row's factors are joined before they meet
-// its elements: steps of 8 bits with the norms' factors, alpha and the gate with the post weight.  Both the gate's and the post
-// weight's gradients are column factors times sum dx fh over the rows of one gate row, the only sum kept for them.
+// Bound by memory: 4096 x 4096 of bfloat16 from 8-bit x and f 42 us for 168 MB of rows and 25 MB of partial sums (512 walks, a row for each of
+// three gradients), 4.6 TB/s, and 6.7 to read those again; 515 x 1155 of binary32 10.6 and 4.1.  Some 25 vector instructions an element
+// would take 11 us by themselves and are in the way only where wavefronts wait for each other at the two barriers of a row, so a
+// row's factors are joined before they meet its elements: steps of 8 bits with the norms' factors, alpha and the gate with the post
+// weight.  Both the gate's and the post weight's gradients are column factors times sum dx fh over the rows of one gate row, the only sum
+// kept for them; where all rows have one gate row that sum could be stored once instead of twice.
 template <typename TF, typename TX, bool KEPT, int E, Share S, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_norm_backward(pwlq_norm_backward_args a, NormPartials part)
 {
@@ -319,11 +322,17 @@ __global__ void k_zero(float *a, int64_t na, float *b, int64_t nb, float *c, int
 // Elements of a thread, by the row's length, and the registers a kernel may have by its most threads.  The forward pass takes 8 up
 // to 4096 columns and 16 beyond; the backward pass 8 up to 2048, 16 beyond (at 4096 16 of 256 threads 45.6 us, 8 of 512
 // 55.5: fewer wavefronts meet at each of its two barriers a row).
+// Beyond 8192 columns a workgroup has more than 512 threads, which leaves a thread 128 registers.  The forward pass spills 10 to 85 of
+// them, none with whole vectors of 16 bits throughout (2048 x 16384 47.6 us, 5.6 TB/s; all in binary32 181, 3.0 TB/s); the backward
+// pass, which keeps five values a column, 160 to 342: 4096 x 12288 of bfloat16 599 us and 2048 x 16384 468, 0.9 to 1.0 TB/s, where
+// 4096 x 8192 takes 98, 4.1 TB/s (replayed, inputs partly in the last-level cache).
 int forward_elements(int64_t D) { return D <= 4096 ? 8 : 16; }
 int backward_elements(int64_t D) { return D <= 2048 ? 8 : 16; }
 
 int backward_walks(int64_t D) { return D <= kWalkColumns ? kWalks : 1; }
-// Rows of a walk: two at least, since what a walk leaves behind is read again.
+// Rows of a walk: two at least, since what a walk leaves behind is read again.  Both kernels with at least 1, 2 and 3 rows, in us: 515 x 1155
+// of binary32 16.4, 12.9 and 13.6, 300 x 4096 of bfloat16 19.6, 16.4 and 16.4, 1500 x 296 18.9, 14.0 and 12.9; with so few rows that they wait
+// for nothing else 130 x 600 of binary32 8.3, 9.2 and 10.5, 40 x 8192 12.9, 14.1 and 16.1.
 int64_t backward_span(int64_t T, int64_t D)
 {
     const int64_t walks = kBackwardWaves / (threads_for(D, backward_elements(D)) / 64);
@@ -379,7 +388,8 @@ void norm_block(const pwlq_norm_args &a, hipStream_t stream)
 #undef PWLQ_AS
 }
 
-// Partial rows in the workspace: d_pre's, d_post's, then d_gate's.
+// Partial rows in the workspace: d_pre's, d_post's, then d_gate's, which has one for each gate row also where those that lie within a walk
+// never use theirs: with a gate for each row as many bytes as d_gate.
 size_t norm_backward_workspace(int64_t T, int64_t D, int64_t gate_rows)
 {
     if (!T) return 0;

@@ -50,7 +50,9 @@ __global__ __launch_bounds__(1024) void k_unpack_rows(const int8_t *codes, const
 
 inline int threads_for(int cols, int E) { return (cols + 64 * E - 1) / (64 * E) * 64; }
 
-// Elements of a thread: 16 up to 16384 columns (a workgroup holds 1024 threads), else what the longest rows need.
+// Elements of a thread: 16 up to 16384 columns (a workgroup holds 1024 threads), else what the longest rows need: 2048 x 32768 of
+// bfloat16 31 us packed and 31 unpacked (6.5 TB/s), of binary32 64 and 82.  Where single columns are moved that spills 8 to 29 registers:
+// 4096 x 16388 of bfloat16 102 and 44, 4096 x 16384 31 and 30 (replayed, inputs partly in the last-level cache).
 template <typename T, Share S>
 void pack_as(const pwlq_rows &x, int64_t rows, int K, int8_t *codes, float *step, hipStream_t stream)
 {
