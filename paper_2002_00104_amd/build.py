@@ -15,12 +15,20 @@ CALL = os.path.join(HERE, "_pwlq_call" + (sysconfig.get_config_var("EXT_SUFFIX")
 BLOCK = os.path.join(CSRC, "block")
 BINDING_SOURCE = os.path.join(BLOCK, "binding.cpp")
 BINDING = os.path.join(HERE, "_pwlq_block" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = [os.path.join(BLOCK, f) for f in ("library.hip", "adapter.hip", "norm.hip", "pack.hip")]
+ATTENTION = os.path.join(CSRC, "attention")
+ATTENTION_BINDING_SOURCE = os.path.join(ATTENTION, "binding.cpp")
+ATTENTION_BINDING = os.path.join(HERE, "_pwlq_attention" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
+SOURCES = [os.path.join(BLOCK, f) for f in ("library.hip", "adapter.hip", "norm.hip", "pack.hip")] + [
+    os.path.join(ATTENTION, f) for f in ("append.hip", "attend.hip", "attend_bf16.hip", "attend_bf16_codes.hip", "attend_f16.hip",
+                                         "attend_f16_codes.hip")]
 BLOCK_HEADERS = [os.path.join(BLOCK, f) for f in ("launch.h", "rows.h")] + [
     os.path.join(os.path.dirname(HERE), "include", f) for f in ("pwlq.h", "pwlq_block.h")]
+ATTENTION_HEADERS = [os.path.join(ATTENTION, f) for f in ("launch.h", "cache.h", "attend.h", "attend_few.h", "attend_many.h", "attend_launch.h")] + [
+    os.path.join(BLOCK, "rows.h"), *BLOCK_HEADERS[2:], os.path.join(os.path.dirname(HERE), "include", "pwlq_attention.h")]
+BINDING_HEADERS = [os.path.join(BLOCK, "binding.h"), *ATTENTION_HEADERS[-3:]]
 # pwlq_api.hip is part of library.hip
 HEADERS = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".h", ".hip"))] + [
-           os.path.join(BLOCK, "calls.h"), *BLOCK_HEADERS,
+           os.path.join(BLOCK, "calls.h"), *BLOCK_HEADERS, os.path.join(ATTENTION, "calls.h"), *ATTENTION_HEADERS,
            os.path.join(os.path.dirname(HERE), "include", "pwlq_bench.h")]
 OBJECTS = os.path.join(HERE, "_build")
 
@@ -63,9 +71,9 @@ def compile_library(lib: str, flags, force: bool, kind: str = "") -> None:
     os.makedirs(OBJECTS, exist_ok=True)
     running, objects = [], []
     for src in SOURCES:
-        obj = os.path.join(OBJECTS, os.path.basename(src) + kind + ".o")
+        obj = os.path.join(OBJECTS, os.path.basename(src) + kind + ".o")             # no two sources have one name
         objects.append(obj)
-        headers = HEADERS if src == SOURCES[0] else BLOCK_HEADERS
+        headers = HEADERS if src == SOURCES[0] else ATTENTION_HEADERS if os.path.dirname(src) == ATTENTION else BLOCK_HEADERS
         if force or stale(obj, [src, *headers]):
             cmd = [hipcc(), *flags, "-c", src, "-o", obj]
             running.append((cmd, subprocess.Popen(cmd)))
@@ -75,15 +83,22 @@ def compile_library(lib: str, flags, force: bool, kind: str = "") -> None:
     subprocess.run([hipcc(), *flags, "-shared", *objects, "-o", lib], check=True)
 
 
-def build_binding() -> None:
-    """The module that calls pwlq_block.h with tensors: torch's headers and libraries, and libpwlq.so beside it."""
+def build_bindings(which) -> None:
+    """The modules that call pwlq_block.h and pwlq_attention.h with tensors: torch's headers and libraries, and libpwlq.so beside them.
+    `which`: (source, module) pairs, compiled beside each other."""
     import torch
     from torch.utils import cpp_extension
-    subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-fvisibility=hidden",
-                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-                    "-I" + sysconfig.get_paths()["include"], *("-isystem" + p for p in cpp_extension.include_paths()),
-                    BINDING_SOURCE, "-o", BINDING, "-L" + HERE, "-lpwlq", "-Wl,-rpath,$ORIGIN",
-                    *("-L" + p for p in cpp_extension.library_paths()), "-lc10", "-ltorch_cpu", "-ltorch_python"], check=True)
+    running = []
+    for source, module in which:
+        cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-fvisibility=hidden",
+               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+               "-I" + sysconfig.get_paths()["include"], *("-isystem" + p for p in cpp_extension.include_paths()),
+               source, "-o", module, "-L" + HERE, "-lpwlq", "-Wl,-rpath,$ORIGIN",
+               *("-L" + p for p in cpp_extension.library_paths()), "-lc10", "-ltorch_cpu", "-ltorch_python"]
+        running.append((cmd, subprocess.Popen(cmd)))
+    failed = [subprocess.CalledProcessError(p.returncode, cmd) for cmd, p in running if p.wait() != 0]
+    if failed:
+        raise failed[0]
 
 
 def build(force: bool = True, extra=()) -> str:
@@ -92,8 +107,9 @@ def build(force: bool = True, extra=()) -> str:
     if force or stale(CALL, [CALL_SOURCE]):
         subprocess.run(["gcc", "-O2", "-std=c11", "-Wall", "-Wextra", "-fPIC", "-shared",
                         "-I" + sysconfig.get_paths()["include"], CALL_SOURCE, "-o", CALL], check=True)
-    if force or stale(BINDING, [BINDING_SOURCE, *BLOCK_HEADERS]):
-        build_binding()
+    bindings = [pair for pair in ((BINDING_SOURCE, BINDING), (ATTENTION_BINDING_SOURCE, ATTENTION_BINDING))
+                if force or stale(pair[1], [pair[0], *BINDING_HEADERS])]
+    build_bindings(bindings)
     return LIB
 
 

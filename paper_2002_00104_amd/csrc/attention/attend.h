@@ -1,0 +1,382 @@
+// Attention over the paged cache: what its kernels share.
+//
+//   s = scale (q . k), capped by a tanh, less slope |own - slot|;  out = sum softmax(s) v
+//
+// A query row is one head of one row of the call.  The rows of a sequence whose heads read the same head of the cache are
+// taken together, `group` heads of each row of the call after the other, in tiles: a tile's keys and values are read once for
+// all of them.  One pass over the keys keeps for each row a reference m, the sum of exp2(s - m) and the sum of exp2(s - m) v;
+// s is in units of log 2.
+//
+// Keys of an item (a tile and a head of the cache) may be split among workgroups.  All items' units of keys lie one after the other
+// on a line, which is cut into equal parts, so lengths may differ as they like; lengths are known on the device only.  A part
+// that is no whole item leaves its sums in the workspace, and k_attend_join puts them together in the order of the keys.
+#pragma once
+
+#include "launch.h"
+#include "cache.h"
+
+namespace pwlq_attention {
+
+struct Attend {
+    Cache c;
+    Batch b;
+    const char *q;
+    char *out;
+    int64_t q_stride, q_head, out_stride, out_head;
+    int group;                           // heads of queries for one of the cache
+    float scale, cap;
+    const float *slopes;
+    int window;                          // 0: none
+    const int32_t *prefix;
+    const uint64_t *tree;
+    int tree_words;
+    int tiles;                           // numbers of tiles, of which some may stand for none
+    int each;                            // without starts: tiles of a sequence
+    int parts;                           // workgroups that the line is cut for; 0: a workgroup for each item
+    int least;                           // units of a part, at least
+    uint64_t *part;                      // workspace: units of a part,
+    uint32_t *begin;                     // where each tile begins on the line,
+    float2 *top_sum;                     // m and the sum of each row of two sums for each part,
+    float *sums;                         // and their values
+};
+
+constexpr int kMostTiles = 2047;         // of a call that is split
+constexpr float kLog2e = 1.4426950408889634f;
+// The reference is moved when a score passes it by more than this, so that most tiles move no sums.  exp2(8) keeps within binary16.
+constexpr float kSlack = 8.0f;
+
+// A tile: rows first to first + M - 1 of a sequence's `rows` query rows, and the slots that any of them may see.
+struct Tile {
+    int s, first, rows, prefix, lo, hi;
+    Sequence q;
+    __device__ bool none() const { return first < 0 || first >= rows; }
+};
+__device__ inline int tile_key(const Attend &a, int start, int s, int M) { return min(max(start, 0), a.b.T) * a.group / M + s; }
+
+__device__ inline Tile tile_of(const Attend &a, int s, int i, Sequence q, int M)
+{
+    Tile t;
+    t.s = s;
+    t.q = q;
+    t.first = i * M;
+    t.rows = q.rows * a.group;
+    t.prefix = a.prefix ? min(max(a.prefix[s], 0), q.length) : 0;
+    t.lo = t.hi = 0;
+    if (t.none()) return t;
+    const int j0 = t.first / a.group, j1 = (min(t.first + M, t.rows) - 1) / a.group, kept = q.kept();
+    if (a.tree) t.hi = q.length;
+    else {
+        t.hi = min(max(max(kept + j1 + 1, t.prefix), 0), q.length);
+        if (a.window && !t.prefix) t.lo = min(max(kept + j0 - a.window + 1, 0), t.hi);
+    }
+    return t;
+}
+// Tile number u; s found by one wavefront, or known.
+__device__ inline Tile tile(const Attend &a, int u, int M)
+{
+    int s, i;
+    if (a.b.starts) {
+        s = find_rising(a.b.S, u, [&](int k) { return tile_key(a, a.b.starts[k], k, M); });
+        i = u - tile_key(a, a.b.starts[s], s, M);
+    } else {
+        s = u / a.each;
+        i = u - s * a.each;
+    }
+    return tile_of(a, s, i, sequence(a.b, s), M);
+}
+// Units of keys of a tile: one at least, where its rows get zeros.
+__device__ inline int units_of(const Tile &t, int unit) { return t.none() ? 0 : max((t.hi + unit - 1) / unit - t.lo / unit, 1); }
+
+// Sum over the threads before this one, and over all, in a workgroup of 256.  `slots`: LDS of four words, not in use.
+__device__ inline uint32_t sum_before(uint32_t v, uint32_t *slots, uint32_t &all)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t s = v;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) {
+        const uint32_t o = (uint32_t)__shfl_up((int)s, k);
+        if (lane >= k) s += o;
+    }
+    if (lane == 63) slots[wave] = s;
+    __syncthreads();
+    uint32_t before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) before += slots[w];
+        all += slots[w];
+    }
+    return before + s - v;
+}
+
+// Where a workgroup's part of the line begins: units x to end - 1, the first of them unit `skip` of head `head` of tile u.
+struct Part { int64_t x, end, part; int u, head, skip; };
+
+// The line, in LDS (`room`: 4 (2 S + 8) bytes with starts and 4 (tiles + 8) at least; free again after the caller's next barrier).  The first workgroup leaves it
+// in the workspace too, for the join.
+template <int M, int UNIT> __device__ Part plan(const Attend &a, uint32_t *room)
+{
+    uint32_t *const slots = room, *const begin = room + 8;
+    int32_t *const starts = (int32_t *)(begin + kMostTiles + 1);
+    const int each = (a.tiles + 255) / 256, from = min((int)threadIdx.x * each, a.tiles), to = min(from + each, a.tiles);
+    if (a.b.starts) {
+        for (int i = threadIdx.x; i <= a.b.S; i += 256) starts[i] = a.b.starts[i];
+        __syncthreads();
+    }
+    uint32_t mine = 0;
+    for (int u = from; u < to; ++u) {
+        int s, i;
+        Sequence q;
+        if (a.b.starts) {
+            int lo = 0, hi = a.b.S;                         // the last s whose tiles begin at u or before
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (tile_key(a, starts[mid], mid, M) <= u) lo = mid;
+                else hi = mid;
+            }
+            s = lo;
+            i = u - tile_key(a, starts[s], s, M);
+            q = sequence(a.b, s, starts[s], starts[s + 1], a.b.lengths[s]);
+        } else {
+            s = u / a.each;
+            i = u - s * a.each;
+            q = sequence(a.b, s);
+        }
+        const int n = units_of(tile_of(a, s, i, q, M), UNIT);
+        begin[u] = (uint32_t)n;
+        mine += (uint32_t)n;
+    }
+    uint32_t all, at = sum_before(mine, slots, all);
+    for (int u = from; u < to; ++u) {
+        const uint32_t n = begin[u];
+        begin[u] = at;
+        at += n;
+    }
+    if (threadIdx.x == 0) begin[a.tiles] = all;
+    __syncthreads();
+    Part p;
+    const int64_t line = (int64_t)all * a.c.heads;
+    p.part = max((line + a.parts - 1) / a.parts, (int64_t)a.least);
+    p.x = (int64_t)blockIdx.x * p.part;
+    p.end = min(p.x + p.part, line);
+    if (blockIdx.x == 0) {
+        for (int u = threadIdx.x; u <= a.tiles; u += 256) a.begin[u] = begin[u];
+        if (threadIdx.x == 0) *a.part = (uint64_t)p.part;
+    }
+    p.u = p.head = p.skip = 0;
+    if (p.x < p.end) {
+        int lo = 0, hi = a.tiles;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if ((int64_t)begin[mid] * a.c.heads <= p.x) lo = mid;
+            else hi = mid;
+        }
+        const int n = (int)(begin[lo + 1] - begin[lo]), into = (int)(p.x - (int64_t)begin[lo] * a.c.heads);
+        p.u = lo;
+        p.head = into / n;
+        p.skip = into - p.head * n;
+    }
+    p.u = __builtin_amdgcn_readfirstlane(p.u);
+    p.head = __builtin_amdgcn_readfirstlane(p.head);
+    p.skip = __builtin_amdgcn_readfirstlane(p.skip);
+    return p;
+}
+
+// The segments of a workgroup, one after the other: units begin to stop - 1 of a tile for a head of the cache, counted from
+// slot 0, and which of the workspace's sums they leave (-1: a whole item, which needs none).
+template <int M, int UNIT> struct Segments {
+    Tile t;
+    int head, begin, stop, sums;
+    Part p;
+    int64_t item;
+    int units;                           // of t; -1: not looked up
+
+    __device__ Segments(const Attend &a, uint32_t *room) : item(blockIdx.x), units(-1)
+    {
+        if (a.parts == 0) return;
+        p = plan<M, UNIT>(a, room);
+        __syncthreads();
+    }
+    __device__ bool next(const Attend &a)
+    {
+        if (a.parts == 0) {
+            for (; item < (int64_t)a.tiles * a.c.heads; item += gridDim.x) {
+                // the last tiles, which see most, begin first; the workgroups of one head of the cache are on the same L2s
+                head = (int)(item % a.c.heads);
+                t = tile(a, a.tiles - 1 - (int)(item / a.c.heads), M);
+                if (t.none()) continue;
+                begin = t.lo / UNIT;
+                stop = begin + units_of(t, UNIT);
+                sums = -1;
+                item += gridDim.x;
+                return true;
+            }
+            return false;
+        }
+        if (p.x >= p.end) return false;
+        while (units <= 0) {
+            t = tile(a, p.u, M);
+            units = units_of(t, UNIT);
+            if (units == 0 && ++p.u >= a.tiles) return false;
+        }
+        const int n = (int)min((int64_t)(units - p.skip), p.end - p.x);
+        if (n <= 0) return false;                           // starts that do not rise: the line does not fit them
+        head = p.head;
+        begin = t.lo / UNIT + p.skip;
+        stop = begin + n;
+        // its sums are the first of the part if the item began before the part or with it
+        sums = n == units ? -1 : 2 * (int)blockIdx.x + (p.skip == 0 && p.x > (int64_t)blockIdx.x * p.part);
+        p.x += n;
+        p.skip = 0;
+        if (++p.head == a.c.heads) {
+            p.head = 0;
+            ++p.u;
+            units = -1;
+        }
+        return true;
+    }
+};
+
+// --------------------------------------------------------------------------
+// a row's scores
+// --------------------------------------------------------------------------
+// cap tanh(x / cap) log2(e) from y = x / cap.  Below a quarter by the series, whose error is then below 4e-7 of the value; above it by
+// 1 - 2 / (exp(2y) + 1), which would lose what it subtracts for small values.
+__device__ inline float capped(float y, float cap2)
+{
+    const float z = y * y;
+    const float small = y * (1.0f + z * (-0.333333333f + z * (0.133333333f + z * -0.0539682540f)));
+    const float large = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * kLog2e)) + 1.0f);
+    return (fabsf(y) < 0.25f ? small : large) * cap2;
+}
+
+// What a lane knows of its query row: it sees slots lo to hi - 1 and those below `prefix`, and where there is a tree those from kept to length - 1
+// whose bits are set.
+struct RowState {
+    int own, lo, hi, prefix;
+    float slope;                         // in units of log 2
+    uint64_t bits;                       // of the tree's first word
+    const uint64_t *words;
+};
+__device__ inline RowState row_state(const Attend &a, const Tile &t, int row, int head)
+{
+    RowState r = {-1, 0, 0, 0, 0.0f, 0, nullptr};
+    if (row >= t.rows) return r;
+    const int j = row / a.group, h = head * a.group + row - j * a.group, kept = t.q.kept();
+    if (a.slopes) r.slope = a.slopes[h] * kLog2e;
+    if (kept + j < 0) return r;
+    r.own = kept + j;
+    if (a.tree) {
+        r.hi = max(kept, 0);
+        r.words = a.tree + (int64_t)(t.q.start + j) * a.tree_words;
+        r.bits = r.words[0];
+    } else {
+        r.hi = r.own + 1;
+        if (a.window) r.lo = max(r.own - a.window + 1, 0);
+        r.prefix = t.prefix;
+    }
+    return r;
+}
+// Without branches but the call's own: all of a lane's keys take the same instructions.
+__device__ inline bool sees(const Attend &a, const Tile &t, const RowState &r, int slot)
+{
+    bool seen = ((uint32_t)(slot - r.lo) < (uint32_t)(r.hi - r.lo)) | (slot < r.prefix);
+    if (a.tree) {
+        const int j = slot - t.q.kept();
+        seen |= ((uint32_t)j < 64u) & ((uint32_t)(r.bits >> (j & 63)) & 1u);
+        if (a.tree_words > 1 && r.words && j >= 64 && (j >> 6) < a.tree_words) seen = r.words[j >> 6] >> (j & 63) & 1;
+    }
+    return seen & (slot < t.q.length);
+}
+// Whether rows first to last (of the tile's sequence) all see slots from to end - 1.
+__device__ inline bool all_see(const Attend &a, const Tile &t, int first, int last, int from, int end)
+{
+    if (end > t.q.length || t.q.kept() + first / a.group < 0) return false;
+    if (a.tree) return end <= t.q.kept();
+    if (end <= t.prefix) return true;
+    const int kept = t.q.kept();
+    return end <= kept + first / a.group + 1 && (!a.window || kept + last / a.group - from < a.window);
+}
+
+// --------------------------------------------------------------------------
+// matrix instructions, and vectors of 16-bit elements
+// --------------------------------------------------------------------------
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+__device__ inline v4f mfma16(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ inline v4f mfma16(v8h a, v8h b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ inline v16f mfma32(v8bf a, v8bf b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ inline v16f mfma32(v8h a, v8h b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+template <typename T> __device__ inline typename Vec8<T>::type as8(v4u w)
+{
+    union { v4u w; typename Vec8<T>::type v; } u;
+    u.w = w;
+    return u.v;
+}
+template <typename T> __device__ inline v4u words(typename Vec8<T>::type v)
+{
+    union { typename Vec8<T>::type v; v4u w; } u;
+    u.v = v;
+    return u.w;
+}
+// Eight codes as T, times a factor.
+template <typename T> __device__ inline typename Vec8<T>::type codes8(uint32_t a, uint32_t b)
+{
+    return __builtin_convertvector(pwlq_block::widen(v2u{a, b}), typename Vec8<T>::type);
+}
+template <typename T> __device__ inline typename Vec8<T>::type codes8(uint32_t a, uint32_t b, float factor)
+{
+    v8f w = pwlq_block::widen(v2u{a, b});
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] *= factor;
+    return __builtin_convertvector(w, typename Vec8<T>::type);
+}
+
+// Sixteen bytes of the cache; rows are whole numbers of them, at their alignment.
+__device__ inline v4u load16(const char *p) { return *(const v4u *)p; }
+
+// Four neighbouring rows' elements of one column, for each of sixteen columns: a group of sixteen lanes reads four rows of sixteen
+// elements from LDS, lane l the four of row l / 4 from column 4 (l % 4) on, and gets column l.
+__device__ inline v4s read_columns(const char *p)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)p);
+}
+template <typename T> __device__ inline typename Vec8<T>::type columns8(const char *p, const char *q)
+{
+    union { v4s h[2]; typename Vec8<T>::type v; } u;
+    u.h[0] = read_columns(p);
+    u.h[1] = read_columns(q);
+    return u.v;
+}
+
+// Infinities and NaN among 16-bit elements: bit 15 of each half where its exponent is all ones.
+template <typename T> __device__ inline uint32_t not_finite(uint32_t w)
+{
+    constexpr uint32_t exponent = sizeof(T) == 2 && __is_same(T, bf16) ? 0x7f807f80u : 0x7c007c00u;
+    constexpr uint32_t one = __is_same(T, bf16) ? 0x00800080u : 0x04000400u;
+    return ((w & exponent) + one) & 0x80008000u;
+}
+// ... taken out; whether there were any.
+template <typename T> __device__ inline bool make_finite(v4u &v)
+{
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t bad = not_finite<T>(v[i]);
+        any |= bad;
+        v[i] &= ~((bad >> 15) * 0xffffu);
+    }
+    return any != 0;
+}
+
+typedef float loose4f __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T> __device__ inline void store4(char *p, v4f v)
+{
+    typedef T v4 __attribute__((ext_vector_type(4)));
+    typedef T loose __attribute__((ext_vector_type(4), aligned(2)));
+    *(loose *)p = __builtin_convertvector(v, v4);
+}
+
+} // namespace pwlq_attention

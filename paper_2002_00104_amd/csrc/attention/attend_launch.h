@@ -1,0 +1,23 @@
+// The kernels of one pair of types: its own source, so that the pairs compile beside each other.
+#pragma once
+
+#include "attend_few.h"
+#include "attend_many.h"
+
+namespace pwlq_attention {
+
+template <typename T, typename C> void attend_launch(const Attend &a, int D, int rows, unsigned grid, hipStream_t stream)
+{
+#define PWLQ_ATTEND(DP)                                                                      \
+    do {                                                                                     \
+        if (rows == 16) k_attend_few<T, C, DP, 1><<<grid, 256, 0, stream>>>(a);              \
+        else if (rows == 32) k_attend_few<T, C, DP, 2><<<grid, 256, 0, stream>>>(a);         \
+        else k_attend_many<T, C, DP><<<grid, 256, 0, stream>>>(a);                           \
+    } while (0)
+    if (D == 64) PWLQ_ATTEND(64);
+    else if (D == 128) PWLQ_ATTEND(128);
+    else PWLQ_ATTEND(256);
+#undef PWLQ_ATTEND
+}
+
+} // namespace pwlq_attention

@@ -3,3 +3,5 @@
 #include "../pwlq_api.hip"
 
 #include "calls.h"
+
+#include "../attention/calls.h"
