@@ -12,11 +12,14 @@
 // that is no whole item leaves its sums in the workspace, and k_attend_join puts them together in the order of the keys.
 #pragma once
 
+#include <initializer_list>
+
 #include "launch.h"
 #include "cache.h"
 
 namespace pwlq_attention {
 
+struct Stretch;
 struct Attend {
     Cache c;
     Batch b;
@@ -35,7 +38,7 @@ struct Attend {
     int parts;                           // workgroups that the line is cut for; 0: a workgroup for each item
     int least;                           // units of a part, at least
     uint64_t *part;                      // workspace: units of a part,
-    uint32_t *begin;                     // where each tile begins on the line,
+    struct Stretch *stretches;           // of the tiles on the line,
     float2 *top_sum;                     // m and the sum of each row of two sums for each part,
     float *sums;                         // and their values
 };
@@ -71,6 +74,12 @@ __device__ inline Tile tile_of(const Attend &a, int s, int i, Sequence q, int M)
     }
     return t;
 }
+// The same for all lanes, and said to be: branches on it are the wavefront's.
+__device__ inline Tile uniform(Tile t)
+{
+    for (int *p : {&t.s, &t.first, &t.rows, &t.prefix, &t.lo, &t.hi, &t.q.start, &t.q.rows, &t.q.length}) *p = __builtin_amdgcn_readfirstlane(*p);
+    return t;
+}
 // Tile number u; s found by one wavefront, or known.
 __device__ inline Tile tile(const Attend &a, int u, int M)
 {
@@ -82,13 +91,20 @@ __device__ inline Tile tile(const Attend &a, int u, int M)
         s = u / a.each;
         i = u - s * a.each;
     }
-    return tile_of(a, s, i, sequence(a.b, s), M);
+    return uniform(tile_of(a, s, i, sequence(a.b, s), M));
 }
 // Units of keys of a tile: one at least, where its rows get zeros.
 __device__ inline int units_of(const Tile &t, int unit) { return t.none() ? 0 : max((t.hi + unit - 1) / unit - t.lo / unit, 1); }
 
-// Sum over the threads before this one, and over all, in a workgroup of 256.  `slots`: LDS of four words, not in use.
-__device__ inline uint32_t sum_before(uint32_t v, uint32_t *slots, uint32_t &all)
+// Where a tile lies on the line, and which rows it has; as it is read by the join.
+struct alignas(32) Stretch {
+    uint32_t begin, units;
+    int first, rows, start;
+    __device__ Stretch(uint32_t begin, int units, const Tile &t) : begin(begin), units((uint32_t)units), first(t.first), rows(t.rows), start(t.q.start) {}
+};
+
+// Sum over the threads before this one, and over all, in a workgroup of THREADS.  `slots`: LDS of a word for each wavefront, not in use.
+template <int THREADS> __device__ inline uint32_t sum_before(uint32_t v, uint32_t *slots, uint32_t &all)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t s = v;
@@ -102,7 +118,7 @@ __device__ inline uint32_t sum_before(uint32_t v, uint32_t *slots, uint32_t &all
     uint32_t before = 0;
     all = 0;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         if (w < wave) before += slots[w];
         all += slots[w];
     }
@@ -110,60 +126,116 @@ __device__ inline uint32_t sum_before(uint32_t v, uint32_t *slots, uint32_t &all
 }
 
 // Where a workgroup's part of the line begins: units x to end - 1, the first of them unit `skip` of head `head` of tile u.
-struct Part { int64_t x, end, part; int u, head, skip; };
+struct Part {
+    int64_t x, end, part;
+    int u, head, skip;
 
-// The line, in LDS (`room`: 4 (2 S + 8) bytes with starts and 4 (tiles + 8) at least; free again after the caller's next barrier).  The first workgroup leaves it
-// in the workspace too, for the join.
-template <int M, int UNIT> __device__ Part plan(const Attend &a, uint32_t *room)
+    __device__ void cut(const Attend &a, uint32_t all)
+    {
+        const int64_t line = (int64_t)all * a.c.heads;
+        part = max((line + a.parts - 1) / a.parts, (int64_t)a.least);
+        x = (int64_t)blockIdx.x * part;
+        end = min(x + part, line);
+        u = head = skip = 0;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.part = (uint64_t)part;
+    }
+    __device__ void start(const Attend &a, int tile, uint32_t begin, int units)
+    {
+        const int into = (int)(x - (int64_t)begin * a.c.heads);
+        u = __builtin_amdgcn_readfirstlane(tile);
+        head = __builtin_amdgcn_readfirstlane(into / units);
+        skip = __builtin_amdgcn_readfirstlane(into - into / units * units);
+    }
+};
+
+// The line of up to 64 tiles of up to 64 sequences, each wavefront for itself: a lane has a tile.  The tiles stay in LDS.  The first workgroup
+// leaves the line in the workspace too, for the join.
+constexpr int kFewTiles = 64;
+template <int M, int UNIT> __device__ Part plan_few(const Attend &a, Tile *tiles)
+{
+    const int lane = threadIdx.x & 63, u = min(lane, a.tiles - 1);
+    int s, i, start, end;
+    if (a.b.starts) {
+        const int mine = a.b.starts[min(lane, a.b.S - 1)], key = tile_key(a, mine, lane, M);
+        int lo = 0, hi = a.b.S;                             // the last s whose tiles begin at u or before
+#pragma unroll
+        for (int k = 0; k < 6; ++k) {
+            const int mid = (lo + hi) / 2;
+            const bool below = __shfl(key, mid) <= u;
+            if (hi - lo > 1) (below ? lo : hi) = mid;
+        }
+        s = lo;
+        start = a.b.starts[s];
+        end = a.b.starts[s + 1];
+        i = u - tile_key(a, start, s, M);
+    } else {
+        s = u / a.each;
+        i = u - s * a.each;
+        start = s;
+        end = s + 1;
+    }
+    const Tile t = tile_of(a, s, i, sequence(a.b, s, start, end, a.b.lengths[s]), M);
+    const int units = lane < a.tiles ? units_of(t, UNIT) : 0;
+    uint32_t stop = (uint32_t)units;                        // and so its end on the line
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) {
+        const uint32_t o = (uint32_t)__shfl_up((int)stop, k);
+        if (lane >= k) stop += o;
+    }
+    Part p;
+    p.cut(a, (uint32_t)__builtin_amdgcn_readlane((int)stop, 63));
+    if (blockIdx.x == 0 && threadIdx.x < a.tiles) a.stretches[lane] = Stretch(stop - units, units, t);
+    if (threadIdx.x < a.tiles) tiles[lane] = t;
+    if (p.x < p.end) {
+        const int at = __builtin_ctzll(__ballot((int64_t)stop * a.c.heads > p.x));
+        const int n = __builtin_amdgcn_readlane(units, at);
+        p.start(a, at, (uint32_t)(__builtin_amdgcn_readlane((int)stop, at) - n), n);
+    }
+    __syncthreads();
+    return p;
+}
+
+// The line of more, by the workgroup, in LDS (`room`: 4 (2 S + 8) bytes with starts and 4 (tiles + 8) at least; free again after the
+// caller's next barrier).
+template <int M, int UNIT, int THREADS> __device__ Part plan(const Attend &a, uint32_t *room)
 {
     uint32_t *const slots = room, *const begin = room + 8;
     int32_t *const starts = (int32_t *)(begin + kMostTiles + 1);
-    const int each = (a.tiles + 255) / 256, from = min((int)threadIdx.x * each, a.tiles), to = min(from + each, a.tiles);
+    const int each = (a.tiles + THREADS - 1) / THREADS, from = min((int)threadIdx.x * each, a.tiles), to = min(from + each, a.tiles);
     if (a.b.starts) {
-        for (int i = threadIdx.x; i <= a.b.S; i += 256) starts[i] = a.b.starts[i];
+        for (int i = threadIdx.x; i <= a.b.S; i += THREADS) starts[i] = a.b.starts[i];
         __syncthreads();
     }
+    auto tile_at = [&](int u) {
+        if (!a.b.starts) {
+            const int s = u / a.each;
+            return tile_of(a, s, u - s * a.each, sequence(a.b, s), M);
+        }
+        int lo = 0, hi = a.b.S;                             // the last s whose tiles begin at u or before
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (tile_key(a, starts[mid], mid, M) <= u) lo = mid;
+            else hi = mid;
+        }
+        return tile_of(a, lo, u - tile_key(a, starts[lo], lo, M), sequence(a.b, lo, starts[lo], starts[lo + 1], a.b.lengths[lo]), M);
+    };
     uint32_t mine = 0;
     for (int u = from; u < to; ++u) {
-        int s, i;
-        Sequence q;
-        if (a.b.starts) {
-            int lo = 0, hi = a.b.S;                         // the last s whose tiles begin at u or before
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if (tile_key(a, starts[mid], mid, M) <= u) lo = mid;
-                else hi = mid;
-            }
-            s = lo;
-            i = u - tile_key(a, starts[s], s, M);
-            q = sequence(a.b, s, starts[s], starts[s + 1], a.b.lengths[s]);
-        } else {
-            s = u / a.each;
-            i = u - s * a.each;
-            q = sequence(a.b, s);
-        }
-        const int n = units_of(tile_of(a, s, i, q, M), UNIT);
+        const int n = units_of(tile_at(u), UNIT);
         begin[u] = (uint32_t)n;
         mine += (uint32_t)n;
     }
-    uint32_t all, at = sum_before(mine, slots, all);
+    uint32_t all, at = sum_before<THREADS>(mine, slots, all);
     for (int u = from; u < to; ++u) {
         const uint32_t n = begin[u];
         begin[u] = at;
+        if (blockIdx.x == 0) a.stretches[u] = Stretch(at, (int)n, tile_at(u));
         at += n;
     }
     if (threadIdx.x == 0) begin[a.tiles] = all;
     __syncthreads();
     Part p;
-    const int64_t line = (int64_t)all * a.c.heads;
-    p.part = max((line + a.parts - 1) / a.parts, (int64_t)a.least);
-    p.x = (int64_t)blockIdx.x * p.part;
-    p.end = min(p.x + p.part, line);
-    if (blockIdx.x == 0) {
-        for (int u = threadIdx.x; u <= a.tiles; u += 256) a.begin[u] = begin[u];
-        if (threadIdx.x == 0) *a.part = (uint64_t)p.part;
-    }
-    p.u = p.head = p.skip = 0;
+    p.cut(a, all);
     if (p.x < p.end) {
         int lo = 0, hi = a.tiles;
         while (hi - lo > 1) {
@@ -171,31 +243,33 @@ template <int M, int UNIT> __device__ Part plan(const Attend &a, uint32_t *room)
             if ((int64_t)begin[mid] * a.c.heads <= p.x) lo = mid;
             else hi = mid;
         }
-        const int n = (int)(begin[lo + 1] - begin[lo]), into = (int)(p.x - (int64_t)begin[lo] * a.c.heads);
-        p.u = lo;
-        p.head = into / n;
-        p.skip = into - p.head * n;
+        p.start(a, lo, begin[lo], (int)(begin[lo + 1] - begin[lo]));
     }
-    p.u = __builtin_amdgcn_readfirstlane(p.u);
-    p.head = __builtin_amdgcn_readfirstlane(p.head);
-    p.skip = __builtin_amdgcn_readfirstlane(p.skip);
+    __syncthreads();
     return p;
 }
 
 // The segments of a workgroup, one after the other: units begin to stop - 1 of a tile for a head of the cache, counted from
 // slot 0, and which of the workspace's sums they leave (-1: a whole item, which needs none).
-template <int M, int UNIT> struct Segments {
+template <int M, int UNIT, int THREADS> struct Segments {
     Tile t;
     int head, begin, stop, sums;
     Part p;
     int64_t item;
     int units;                           // of t; -1: not looked up
 
-    __device__ Segments(const Attend &a, uint32_t *room) : item(blockIdx.x), units(-1)
+    const Tile *tiles;                   // in LDS, or NULL
+
+    // `few`: LDS for kFewTiles tiles
+    __device__ Segments(const Attend &a, uint32_t *room, Tile *few) : item(blockIdx.x), units(-1), tiles(nullptr)
     {
         if (a.parts == 0) return;
-        p = plan<M, UNIT>(a, room);
-        __syncthreads();
+        if (a.tiles <= kFewTiles && a.b.S <= kFewTiles) {
+            p = plan_few<M, UNIT>(a, few);
+            tiles = few;
+        } else {
+            p = plan<M, UNIT, THREADS>(a, room);
+        }
     }
     __device__ bool next(const Attend &a)
     {
@@ -215,7 +289,7 @@ template <int M, int UNIT> struct Segments {
         }
         if (p.x >= p.end) return false;
         while (units <= 0) {
-            t = tile(a, p.u, M);
+            t = tiles ? uniform(tiles[p.u]) : tile(a, p.u, M);
             units = units_of(t, UNIT);
             if (units == 0 && ++p.u >= a.tiles) return false;
         }
@@ -240,14 +314,33 @@ template <int M, int UNIT> struct Segments {
 // --------------------------------------------------------------------------
 // a row's scores
 // --------------------------------------------------------------------------
-// cap tanh(x / cap) log2(e) from y = x / cap.  Below a quarter by the series, whose error is then below 4e-7 of the value; above it by
-// 1 - 2 / (exp(2y) + 1), which would lose what it subtracts for small values.
-__device__ inline float capped(float y, float cap2)
+// cap tanh(x / cap) log2(e) for N products with to_cap = scale / cap, cap2 = cap log2(e).  With y = x / cap below 0.6 by a polynomial in y^2, which
+// interpolates tanh(y) / y at Chebyshev points and is off by at most 8e-8 of it; above by 1 - 2 / (exp(2y) + 1), which would lose what
+// it subtracts for small y.  Scores are mostly well below the cap: a wavefront of which all are takes 7 vector instructions for each.
+template <int N> __device__ inline void cap_scores(float (&s)[N], float to_cap, float cap2)
 {
-    const float z = y * y;
-    const float small = y * (1.0f + z * (-0.333333333f + z * (0.133333333f + z * -0.0539682540f)));
-    const float large = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * kLog2e)) + 1.0f);
-    return (fabsf(y) < 0.25f ? small : large) * cap2;
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        s[i] *= to_cap;
+        most = fmaxf(most, fabsf(s[i]));
+    }
+    auto small = [&](float y) {
+        const float z = y * y;
+        return y * __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, 0.0154687513f * cap2, -0.0520966534f * cap2), 0.133100644f * cap2),
+                                                    -0.33332302f * cap2), 0.999999926f * cap2);
+    };
+    // a NaN is no maximum: the polynomial keeps it
+    if (!__ballot(most >= 0.6f)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = small(s[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float large = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[i] * (2.0f * kLog2e)) + 1.0f);
+            s[i] = fabsf(s[i]) < 0.6f ? small(s[i]) : large * cap2;
+        }
+    }
 }
 
 // What a lane knows of its query row: it sees slots lo to hi - 1 and those below `prefix`, and where there is a tree those from kept to length - 1
@@ -271,31 +364,46 @@ __device__ inline RowState row_state(const Attend &a, const Tile &t, int row, in
         r.words = a.tree + (int64_t)(t.q.start + j) * a.tree_words;
         r.bits = r.words[0];
     } else {
-        r.hi = r.own + 1;
+        r.hi = min(r.own + 1, t.q.length);
         if (a.window) r.lo = max(r.own - a.window + 1, 0);
         r.prefix = t.prefix;
     }
     return r;
 }
-// Without branches but the call's own: all of a lane's keys take the same instructions.
-__device__ inline bool sees(const Attend &a, const Tile &t, const RowState &r, int slot)
+// Bits 0 to n - 1, n any number.
+__device__ inline uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+// Which of the 64 slots from `from` on the row sees, as bits.
+__device__ inline uint64_t seen_slots(const Attend &a, const Tile &t, const RowState &r, int from)
 {
-    bool seen = ((uint32_t)(slot - r.lo) < (uint32_t)(r.hi - r.lo)) | (slot < r.prefix);
+    uint64_t seen = (low_bits(r.hi - from) & ~low_bits(r.lo - from)) | low_bits(r.prefix - from);
     if (a.tree) {
-        const int j = slot - t.q.kept();
-        seen |= ((uint32_t)j < 64u) & ((uint32_t)(r.bits >> (j & 63)) & 1u);
-        if (a.tree_words > 1 && r.words && j >= 64 && (j >> 6) < a.tree_words) seen = r.words[j >> 6] >> (j & 63) & 1;
+        const int j = from - t.q.kept();                    // the first slot's row in the tree
+        if (a.tree_words == 1) {
+            if (r.own >= 0 && j > -64 && j < 64) seen |= j >= 0 ? r.bits >> j : r.bits << -j;
+        } else if (r.own >= 0 && j > -64) {
+            const int word = j >> 6, shift = j & 63;       // of the first slot, from -1 on
+            const uint64_t low = word >= 0 && word < a.tree_words ? r.words[word] : 0;
+            const uint64_t high = word + 1 < a.tree_words ? r.words[word + 1] : 0;
+            seen |= shift ? low >> shift | high << (64 - shift) : low;
+        }
+        seen &= low_bits(t.q.length - from);
     }
-    return seen & (slot < t.q.length);
+    return seen;
 }
-// Whether rows first to last (of the tile's sequence) all see slots from to end - 1.
-__device__ inline bool all_see(const Attend &a, const Tile &t, int first, int last, int from, int end)
+// The slots that rows first to last (of the tile's sequence) all see: begin to end - 1, and those below prefix.
+struct Common {
+    int prefix, begin, end;
+    __device__ bool has(int from, int stop) const { return stop <= prefix || (from >= begin && stop <= end); }
+};
+__device__ inline Common common(const Attend &a, const Tile &t, int first, int last)
 {
-    if (end > t.q.length || t.q.kept() + first / a.group < 0) return false;
-    if (a.tree) return end <= t.q.kept();
-    if (end <= t.prefix) return true;
-    const int kept = t.q.kept();
-    return end <= kept + first / a.group + 1 && (!a.window || kept + last / a.group - from < a.window);
+    const int kept = t.q.kept(), j0 = first / a.group, j1 = last / a.group;
+    Common c = {0, 0, 0};
+    if (kept + j0 < 0) return c;
+    c.prefix = t.prefix;
+    c.end = a.tree ? kept : min(kept + j0 + 1, t.q.length);
+    if (a.window) c.begin = kept + j1 - a.window + 1;
+    return c;
 }
 
 // --------------------------------------------------------------------------
@@ -369,6 +477,40 @@ template <typename T> __device__ inline bool make_finite(v4u &v)
         v[i] &= ~((bad >> 15) * 0xffffu);
     }
     return any != 0;
+}
+// Where some rows do not see all keys, a value that is not finite must reach the rows that see it and no others, and 0 times it would be NaN.  So
+// such values are taken out of the product.  An item's end, where its sums are all that is left in registers, adds what they are for the
+// rows that see them: two more products, with 1 for each key that a row sees, count them and add their signs; as many as the sum says are
+// infinities of one sign.  The values are read again, one by one, in the operand's layout: channel d of slots `from` to from + 3 and from + apart to
+// from + apart + 3.  `seen`: bits 0 to 3 and 4 to 7, of those slots.
+template <typename T, typename C> struct NotFinite {
+    typename Vec8<T>::type counts, signs, ones;
+
+    __device__ NotFinite(const Attend &a, const int32_t *table, int head, int from, int apart, int end, int d, uint32_t seen)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int slot = from + (i & 3) + (i / 4) * apart;
+            float n = 0.0f, s = 0.0f;
+            if (slot < end && d < a.c.D) {
+                const int page = table[slot >> a.c.shift];
+                if ((unsigned)page < (unsigned)a.c.pages) {
+                    const int64_t row = row_number(a.c, Place{page, slot & ((1 << a.c.shift) - 1)}, head);
+                    float v = pwlq_block::widen(((const C *)a.c.values)[row * a.c.D + d]);
+                    if constexpr (sizeof(C) == 1) v = (float)(T)(v * a.c.value_step[row]);
+                    if (!(fabsf(v) < INFINITY)) n = 1.0f;
+                    if (fabsf(v) == INFINITY) s = v > 0.0f ? 1.0f : -1.0f;
+                }
+            }
+            counts[i] = (T)n;
+            signs[i] = (T)s;
+            ones[i] = (T)(float)(seen >> i & 1);
+        }
+    }
+};
+__device__ inline float not_finite_sum(float count, float sign)
+{
+    return count == 0.0f ? 0.0f : count == fabsf(sign) ? copysignf(INFINITY, sign) : __builtin_nanf("");
 }
 
 typedef float loose4f __attribute__((ext_vector_type(4), aligned(4)));

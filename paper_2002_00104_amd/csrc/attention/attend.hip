@@ -12,39 +12,53 @@ extern template PWLQ_INTERNAL void attend_launch<f16, int8_t>(const Attend &, in
 
 namespace {
 
-// The parts of an item that workgroups left in the workspace, in the order of the keys: a workgroup for 16 rows of an item.
-template <typename T, int DP> __global__ __launch_bounds__(256) void k_attend_join(const Attend a, int rows)
+// The parts of an item that workgroups left in the workspace: DP / 4 lanes a group, a workgroup for ROWS rows, each of which has a group or several;
+// these take its parts in turn, each in the order of the keys, and the first adds up what they have, in their order.
+template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void k_attend_join(const Attend a, int rows)
 {
-    const int u = blockIdx.x, head = blockIdx.y;
-    const int64_t n = a.begin[u + 1] - a.begin[u];
-    if (n == 0) return;
-    const int64_t part = (int64_t)*a.part, x = (int64_t)a.begin[u] * a.c.heads + head * n, first = x / part, last = (x + n - 1) / part;
-    if (first == last) return;
-    const Tile t = tile(a, u, rows);
-    for (int i = threadIdx.x + blockIdx.z * (16 * DP / 4); i < (int)(blockIdx.z + 1) * (16 * DP / 4); i += 256) {
-        const int of = i / (DP / 4), d = i % (DP / 4) * 4, row = t.first + of;
-        if (row >= t.rows || d >= a.c.D) continue;
+    constexpr int kLanes = DP / 4, kGroups = 256 / kLanes, kEach = kGroups > ROWS ? kGroups / ROWS : 1;
+    __shared__ v4f sums[kGroups][kLanes];
+    __shared__ float2 tops[kGroups];
+    const Stretch t = a.stretches[blockIdx.x];
+    const int64_t part = (int64_t)*a.part, n = t.units, x = (int64_t)t.begin * a.c.heads + blockIdx.y * n;
+    if (n == 0 || x / part == (x + n - 1) / part || t.first + (int)blockIdx.z * ROWS >= t.rows) return;
+    const int64_t first = x / part, last = (x + n - 1) / part;
+    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, turn = group % kEach, d = 4 * lane;
+#pragma unroll
+    for (int r = 0; r < ROWS; r += kGroups / kEach) {
+        const int of = blockIdx.z * ROWS + r + group / kEach, row = t.first + of;
         v4f v = {};
         float top = -INFINITY, total = 0.0f;
-        for (int64_t w = first; w <= last; ++w) {
-            const int64_t at = (2 * w + (x > w * part)) * rows + of;
-            const float2 o = a.top_sum[at];
-            const v4f s = *(const v4f *)(a.sums + at * DP + d);
+        auto add = [&](float2 o, v4f s) {
             const float most = fmaxf(top, o.x);
             const float old = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - most);
             const float now = o.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(o.x - most);
             v = v * old + s * now;
             total = total * old + o.y * now;
             top = most;
+        };
+        if (row < t.rows) {
+#pragma unroll 4
+            for (int64_t w = first + turn; w <= last; w += kEach) {
+                const int64_t at = (2 * w + (x > w * part)) * rows + of;
+                add(a.top_sum[at], *(const v4f *)(a.sums + at * DP + d));
+            }
         }
-        const int j = row / a.group, h = head * a.group + row - j * a.group;
-        store4<T>(a.out + ((t.q.start + j) * a.out_stride + h * a.out_head + d) * 2, total == 0.0f ? v4f{} : v * (1.0f / total));
+        if constexpr (kEach > 1) {
+            sums[group][lane] = v;
+            if (lane == 0) tops[group] = make_float2(top, total);
+            __syncthreads();
+            if (turn == 0)
+                for (int g = 1; g < kEach; ++g) add(tops[group + g], sums[group + g][lane]);
+        }
+        if (turn != 0 || row >= t.rows || d >= a.c.D) continue;
+        const int j = row / a.group, h = blockIdx.y * a.group + row - j * a.group;
+        store4<T>(a.out + ((t.start + j) * a.out_stride + h * a.out_head + d) * 2, total == 0.0f ? v4f{} : v * (1.0f / total));
     }
 }
 
-constexpr int kParts = 512;              // two workgroups for each CU
 
-struct Shape { int rows, channels, unit, tiles, each, parts, least; size_t part, begin, top_sum, sums, bytes; };
+struct Shape { int rows, channels, unit, tiles, each, parts, least; size_t part, stretches, top_sum, sums, bytes; };
 
 Shape shape_of(const pwlq_attend_args &g)
 {
@@ -62,7 +76,8 @@ Shape shape_of(const pwlq_attend_args &g)
     if (tiles <= kMostTiles && g.batch.S <= kMostTiles && tiles * units < 1LL << 31 && !enough) {
         const int64_t all = items * (units > 1 ? units : 1);
         const int64_t parts = (all + s.least - 1) / s.least;
-        s.parts = (int)(parts < kParts ? parts : kParts);
+        const int most = s.channels == 256 ? 256 : 512;    // what the chip holds: 256 channels take a CU's registers
+        s.parts = (int)(parts < most ? parts : most);
     }
     auto place = [&](size_t bytes) {
         const size_t at = s.bytes;
@@ -71,7 +86,7 @@ Shape shape_of(const pwlq_attend_args &g)
     };
     if (s.parts) {
         s.part = place(8);
-        s.begin = place(4 * (size_t)(s.tiles + 1));
+        s.stretches = place(sizeof(Stretch) * (size_t)s.tiles);
         s.top_sum = place(8 * 2 * (size_t)s.parts * s.rows);
         s.sums = place(4 * 2 * (size_t)s.parts * s.rows * s.channels);
     }
@@ -106,7 +121,7 @@ void attend(const pwlq_attend_args &g, void *workspace, hipStream_t stream)
     a.least = s.least;
     char *const w = (char *)workspace;
     a.part = (uint64_t *)(w + s.part);
-    a.begin = (uint32_t *)(w + s.begin);
+    a.stretches = (Stretch *)(w + s.stretches);
     a.top_sum = (float2 *)(w + s.top_sum);
     a.sums = (float *)(w + s.sums);
     const int64_t items = (int64_t)s.tiles * a.c.heads;
@@ -120,16 +135,24 @@ void attend(const pwlq_attend_args &g, void *workspace, hipStream_t stream)
         else attend_launch<f16, f16>(a, s.channels, s.rows, grid, stream);
     }
     if (s.parts < 2) return;
-    const dim3 join((unsigned)s.tiles, (unsigned)a.c.heads, (unsigned)(s.rows / 16));
+#define PWLQ_JOIN_ROWS(T, DP, ROWS)                                                                                  \
+    k_attend_join<T, DP, ROWS><<<dim3((unsigned)s.tiles, (unsigned)a.c.heads, (unsigned)(s.rows / ROWS)), 256, 0, stream>>>(a, s.rows)
 #define PWLQ_JOIN(T)                                                                         \
     do {                                                                                     \
-        if (s.channels == 64) k_attend_join<T, 64><<<join, 256, 0, stream>>>(a, s.rows);     \
-        else if (s.channels == 128) k_attend_join<T, 128><<<join, 256, 0, stream>>>(a, s.rows); \
-        else k_attend_join<T, 256><<<join, 256, 0, stream>>>(a, s.rows);                     \
+        if (s.rows < 128) {                                                                  \
+            if (s.channels == 64) PWLQ_JOIN_ROWS(T, 64, 2);                                  \
+            else if (s.channels == 128) PWLQ_JOIN_ROWS(T, 128, 2);                           \
+            else PWLQ_JOIN_ROWS(T, 256, 2);                                                  \
+        } else {                                                                             \
+            if (s.channels == 64) PWLQ_JOIN_ROWS(T, 64, 16);                                 \
+            else if (s.channels == 128) PWLQ_JOIN_ROWS(T, 128, 16);                          \
+            else PWLQ_JOIN_ROWS(T, 256, 16);                                                 \
+        }                                                                                    \
     } while (0)
     if (g.q.type == PWLQ_BF16) PWLQ_JOIN(bf16);
     else PWLQ_JOIN(f16);
 #undef PWLQ_JOIN
+#undef PWLQ_JOIN_ROWS
 }
 
 } // namespace pwlq_attention

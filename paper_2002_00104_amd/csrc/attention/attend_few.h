@@ -14,7 +14,7 @@
 namespace pwlq_attention {
 
 template <typename T, typename C, int DP, int RB> struct Few {
-    static constexpr bool kCodes = sizeof(C) == 1;
+    static constexpr bool kCodes = sizeof(C) == 1, kMayBeBad = !kCodes || __is_same(T, f16);     // values that are not finite
     static constexpr int kUnit = 128, kRows = 16 * RB;
     static constexpr int kSteps = DP / 32, kColumns = DP / 16;
     static constexpr int kLoads = kCodes ? DP / 64 : DP / 32;                      // of 16 bytes, for 16 keys
@@ -56,8 +56,8 @@ template <typename T, typename C, int DP, int RB> struct Few {
         }
     }
 
-    // Values to LDS.  `checked`: some row does not see all keys; then what is neither finite nor past the end is taken out, and reported,
-    // and what is past the end is 0.
+    // Values to LDS.  `checked`: some row does not see all keys; then what is past the end is 0, and infinities and NaN before it are taken
+    // out and reported.
     __device__ bool put_values(const Attend &a, char *room, int lane, bool checked, int from, int end, const int *p) const
     {
         bool bad = false;
@@ -110,20 +110,21 @@ template <typename T, typename C, int DP, int RB> struct Few {
     static __device__ int channel(int step, int quarter) { return kCodes ? 64 * (step / 2) + 16 * quarter + 8 * (step & 1) : 32 * step + 8 * quarter; }
 };
 
-template <typename T, typename C, int DP, int RB>
+template <typename T, typename C, int DP, int RB, bool PLAIN>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Attend a)
 {
     typedef Few<T, C, DP, RB> F;
     typedef typename F::v8 v8;
     __shared__ __attribute__((aligned(16))) char room[F::kRoom];
     __shared__ float2 top_sum[4][F::kRows];
+    __shared__ Tile tiles[kFewTiles];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
     char *const values = room + wave * 32 * F::kStride;
     const char *const columns = values + (4 * quarter + (lane & 15) / 4) * F::kStride + (lane & 3) * 8;
     const bool factors = F::kCodes;
     const float to_cap = a.cap > 0.0f ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
 
-    Segments<F::kRows, F::kUnit> segments(a, (uint32_t *)room);
+    Segments<F::kRows, F::kUnit, 256> segments(a, (uint32_t *)room, tiles);
     while (segments.next(a)) {
         const Tile t = segments.t;
         const int head = segments.head, begin = segments.begin, stop = segments.stop, sums = segments.sums;
@@ -151,7 +152,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
         // this wavefront's units: 32 keys from 128 u + 32 wave on
         const int first = max(begin, (t.lo - 32 * wave + 96) >> 7), end = min(stop, (t.hi - 32 * wave + 127) >> 7);
         const int32_t *const table = a.b.table + t.s * a.b.table_stride;
-        const int last_row = min(t.first + F::kRows, t.rows) - 1;
+        const Common whole = common(a, t, t.first, min(t.first + F::kRows, t.rows) - 1);
+        bool bad = false;                                  // a value taken out
         F f;
         int pages = -1, p[2];                              // lane 2i + b: the page of block b of unit base + i
         int base = 0;
@@ -174,8 +176,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
         }
         for (int u = first; u < end; ++u) {
             const int from = 128 * u + 32 * wave, now[2] = {p[0], p[1]};
-            const bool full = now[0] >= 0 && now[1] >= 0 && all_see(a, t, t.first, last_row, from, from + 32);
-            const bool bad = f.put_values(a, values, lane, !full, from, t.hi, now);
+            const bool full = now[0] >= 0 && now[1] >= 0 && whole.has(from, from + 32);
+            bad |= f.put_values(a, values, lane, !full, from, t.hi, now);
             v4f s[RB][2];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
@@ -199,30 +201,28 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
                 find_pages(u + 1);
                 f.load(a, head, from + 128, p, lane);
             }
-            uint32_t seen[RB], above[RB];                  // by key, where `bad`
+            const uint32_t there = (now[0] < 0 ? 0u : 0xffffu) | (now[1] < 0 ? 0u : 0xffff0000u);
             v8 weight[RB];
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 float x[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = s[r][i / 4][i & 3] * to_cap;
-                if (a.cap > 0.0f) {
+                for (int i = 0; i < 8; ++i) x[i] = s[r][i / 4][i & 3];
+                if (!PLAIN && a.cap > 0.0f) {
+                    cap_scores(x, to_cap, cap2);
+                } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = capped(x[i], cap2);
+                    for (int i = 0; i < 8; ++i) x[i] *= to_cap;
                 }
-                if (a.slopes) {
+                if (!PLAIN && a.slopes) {
+                    const float away = (float)(state[r].own - from - 4 * quarter);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] -= state[r].slope * (float)abs(state[r].own - (from + 16 * (i / 4) + 4 * quarter + (i & 3)));
+                    for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(-state[r].slope, fabsf(away - (float)(16 * (i / 4) + (i & 3))), x[i]);
                 }
-                uint32_t see = 0xff;
                 if (!full) {
-                    see = 0;
+                    const uint32_t mine = ((uint32_t)seen_slots(a, t, state[r], from) & there) >> (4 * quarter);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const bool seen_it = (now[i / 4] >= 0) & sees(a, t, state[r], from + 16 * (i / 4) + 4 * quarter + (i & 3));
-                        see |= (uint32_t)seen_it << i;
-                        x[i] = seen_it ? x[i] : -INFINITY;
-                    }
+                    for (int i = 0; i < 8; ++i) x[i] = mine >> (16 * (i / 4) + (i & 3)) & 1 ? x[i] : -INFINITY;
                 }
                 float most = x[0];
 #pragma unroll
@@ -245,23 +245,17 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     w[i] = __builtin_amdgcn_exp2f(x[i] - reference[r]);
-                    if (!full && !(see >> i & 1)) w[i] = 0.0f;
                     sum[r] += w[i];
                 }
-                if (bad) {
-                    seen[r] = above[r] = 0;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int key = 16 * (i / 4) + 4 * quarter + (i & 3);
-                        seen[r] |= (see >> i & 1) << key;
-                        above[r] |= (w[i] > 0.0f ? 1u : 0u) << key;
-                    }
-                }
                 if constexpr (F::kCodes && !__is_same(T, f16)) {
-                    // a row's step joins its weight: one rounding to bfloat16, of their product
+                    // a row's step joins its weight: one rounding to bfloat16, of their product; a step may be NaN
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        w[i] = !full && !(see >> i & 1) ? 0.0f : w[i] * value_step[i / 4][i & 3];
+                    for (int i = 0; i < 8; ++i) w[i] *= value_step[i / 4][i & 3];
+                    if (!full) {
+                        const uint32_t mine = ((uint32_t)seen_slots(a, t, state[r], from) & there) >> (4 * quarter);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = mine >> (16 * (i / 4) + (i & 3)) & 1 ? w[i] : 0.0f;
+                    }
                 }
                 v8f all;
 #pragma unroll
@@ -276,36 +270,26 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
 #pragma unroll
                 for (int r = 0; r < RB; ++r) acc[r][c] = mfma16(v, weight[r], acc[r][c]);
             }
-            if (bad) {
-                // infinities and NaN among the values, of which some rows see less than all: row by row and key by key
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    seen[r] |= __shfl_xor(seen[r], 16);
-                    seen[r] |= __shfl_xor(seen[r], 32);
-                    above[r] |= __shfl_xor(above[r], 16);
-                    above[r] |= __shfl_xor(above[r], 32);
-                }
-                for (int key = 0; key < 32 && from + key < t.hi; ++key) {
-                    if (now[key / 16] < 0) continue;
-                    const int64_t n = row_number(a.c, Place{now[key / 16], (from + key) & ((1 << a.c.shift) - 1)}, head);
-#pragma unroll
-                    for (int c = 0; c < F::kColumns; ++c) {
-                        const int d = 16 * c + 4 * quarter;
-                        if (d >= a.c.D) continue;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float v = pwlq_block::widen(((const C *)a.c.values)[n * a.c.D + d + i]);
-                            if constexpr (F::kCodes) v = (float)(T)(v * a.c.value_step[n]);
-                            if (fabsf(v) < INFINITY) continue;
-#pragma unroll
-                            for (int r = 0; r < RB; ++r)
-                                if (seen[r] >> key & 1) acc[r][c][i] += (above[r] >> key & 1 ? 1.0f : 0.0f) * v;
-                        }
-                    }
-                }
-            }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
+        }
+
+        if (F::kMayBeBad && bad) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int c = 0; c < F::kColumns; ++c) {
+                    v4f count = {}, sign = {};
+                    for (int u = first; u < end; ++u) {
+                        const int from = 128 * u + 32 * wave;
+                        const uint32_t mine = (uint32_t)(seen_slots(a, t, state[r], from) >> (4 * quarter));
+                        const NotFinite<T, C> v(a, table, head, from + 4 * quarter, 16, t.hi, 16 * c + (lane & 15), (mine & 15) | (mine >> 12 & 0xf0));
+                        count = mfma16(v.counts, v.ones, count);
+                        sign = mfma16(v.signs, v.ones, sign);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[r][c][i] += not_finite_sum(count[i], sign[i]);
+                }
         }
 
         // the four wavefronts' sums

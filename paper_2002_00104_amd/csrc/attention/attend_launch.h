@@ -8,16 +8,24 @@ namespace pwlq_attention {
 
 template <typename T, typename C> void attend_launch(const Attend &a, int D, int rows, unsigned grid, hipStream_t stream)
 {
-#define PWLQ_ATTEND(DP)                                                                      \
+    // scores as the product has them, or capped or with a bias
+    const bool plain = !(a.cap > 0.0f) && !a.slopes;
+#define PWLQ_ATTEND_AS(DP, PLAIN)                                                            \
     do {                                                                                     \
-        if (rows == 16) k_attend_few<T, C, DP, 1><<<grid, 256, 0, stream>>>(a);              \
-        else if (rows == 32) k_attend_few<T, C, DP, 2><<<grid, 256, 0, stream>>>(a);         \
-        else k_attend_many<T, C, DP><<<grid, 256, 0, stream>>>(a);                           \
+        if (rows == 16) k_attend_few<T, C, DP, 1, PLAIN><<<grid, 256, 0, stream>>>(a);       \
+        else if (rows == 32) k_attend_few<T, C, DP, 2, PLAIN><<<grid, 256, 0, stream>>>(a);  \
+        else k_attend_many<T, C, DP, PLAIN><<<grid, 256, 0, stream>>>(a);                    \
+    } while (0)
+#define PWLQ_ATTEND(DP)                            \
+    do {                                           \
+        if (plain) PWLQ_ATTEND_AS(DP, true);       \
+        else PWLQ_ATTEND_AS(DP, false);            \
     } while (0)
     if (D == 64) PWLQ_ATTEND(64);
     else if (D == 128) PWLQ_ATTEND(128);
     else PWLQ_ATTEND(256);
 #undef PWLQ_ATTEND
+#undef PWLQ_ATTEND_AS
 }
 
 } // namespace pwlq_attention

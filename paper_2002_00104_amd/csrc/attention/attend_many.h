@@ -1,10 +1,11 @@
 // k_attend_many: tiles of 128 query rows, for prompts and larger trees.
 //
 // Bound by the matrix cores and by the exponentials beside them: a tile of 64 keys takes a wavefront's 32 rows 1024 cycles of matrix
-// instructions (128 channels) and as many of vector instructions for its 2048 weights.  Two workgroups share a CU, so one's
+// instructions (128 channels) and nearly as many of vector instructions for its 2048 weights.  Two workgroups share a CU, so that one's
 // products run beside the other's exponentials.
 //
-// Keys and values of a tile are staged in LDS, twice: one is filled while the other is worked on, a barrier a tile.  As for few
+// Keys and values of a tile are staged in LDS, twice: one is filled while the other is worked on, a barrier a tile; 16-bit elements
+// go there from memory directly, codes are widened on the way.  As for few
 // rows, S^T = K Q^T leaves a lane its query row's weights in the layout of the operand of O^T = V^T P^T.
 #pragma once
 
@@ -14,91 +15,156 @@ namespace pwlq_attention {
 
 template <typename T, typename C, int DP> struct Many {
     static constexpr bool kCodes = sizeof(C) == 1, kScaled = kCodes && __is_same(T, f16);    // values scaled as they are read
-    static constexpr int kRows = 128, kKeys = DP == 256 ? 32 : 64;
+    static constexpr bool kMayBeBad = !kCodes || kScaled;                          // values that are not finite
+    static constexpr int kRows = 128, kKeys = DP == 256 ? 32 : 64;                 // of a unit; a wavefront has 32 rows
     static constexpr int kSteps = DP / 16, kColumns = DP / 32, kBlocks = kKeys / 32;
-    static constexpr int kChunks = kCodes ? DP / 16 : DP / 8;                      // of 16 bytes, of a row
+    static constexpr int kChunks = kCodes ? DP / 16 : DP / 8;                      // of 16 bytes, of a row in memory
     static constexpr int kPass = 256 / kChunks, kLoads = kKeys / kPass, kWavePass = 64 / kChunks;
-    static constexpr int kKeyStride = 2 * DP + 16, kValueStride = 2 * DP + 64;     // bytes of a row in LDS
-    static constexpr int kStage = kKeys * (kKeyStride + kValueStride);
-    static_assert(2 * kStage >= 4 * (2 * kMostTiles + 16), "LDS");
+    static constexpr int kTurns = kPass % 16 ? 16 / kPass : 1;                     // loads after which rows lie in a block as at first
+    static constexpr int kAhead = kCodes ? 4 : 8;                                  // operands of keys under way; codes hold registers of their own
+    static constexpr int kRowBytes = 2 * DP, kPart = kKeys * kRowBytes;            // in LDS: keys, then values
+    static_assert(4 * kPart >= 4 * (2 * kMostTiles + 16), "LDS");
     typedef typename Vec8<T>::type v8;
 
-    v4u k[kLoads], v[kLoads];
-    float key_step[kLoads], value_step[kLoads];
+    // A row's chunks of 16 bytes in LDS are in an order of its own, so that the rows that are read together lie in different banks: for keys
+    // sixteen rows' chunks of one number, for values four rows' chunks of four numbers.
+    static __device__ int key_swizzle(int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; }
+    static __device__ int value_swizzle(int row) { return DP == 64 ? 4 * ((row >> 1) & 1) : 4 * (row & 3); }
 
-    // `pages`: lane i has the page of block base + i of sixteen keys
-    __device__ void load(const Attend &a, int head, int from, int pages, int base, int wave, int lane)
+    // of codes only
+    v4u k[kCodes ? kLoads : 1], v[kCodes ? kLoads : 1];
+    float key_step[kCodes ? kLoads : 1], value_step[kCodes ? kLoads : 1];
+
+    // What a lane fetches of a pass's rows, in bytes from their block's first row: of keys and of values.  16-bit elements go to LDS by
+    // themselves, where a wavefront fills whole rows one after the other: the lane that fills a chunk fetches what belongs there.  Negative: nothing,
+    // past D.
+    int key_from[kTurns], value_from[kTurns];
+    __device__ void prepare(const Attend &a, int wave, int lane)
     {
-        const int D = a.c.D, row = lane / kChunks, d = lane % kChunks * (16 / (int)sizeof(C));
+        const int D = a.c.D, chunk = lane % kChunks;
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int r = j * kPass + wave * kWavePass, slot = from + r;
-            const int page = __builtin_amdgcn_readlane(pages, (slot >> 4) - base);
-            const int64_t n = row_number(a.c, Place{max(page, 0), slot & ((1 << a.c.shift) - 1)}, head);
-            const uint32_t offset = (uint32_t)((row * D + (d < D ? d : 0)) * (int)sizeof(C));
-            k[j] = load16(a.c.keys + n * D * (int)sizeof(C) + offset);
-            v[j] = load16(a.c.values + n * D * (int)sizeof(C) + offset);
+        for (int j = 0; j < kTurns; ++j) {
+            const int row = (j * kPass + wave * kWavePass) % 16 + lane / kChunks;
             if constexpr (kCodes) {
-                key_step[j] = a.c.key_step[n + row];
-                value_step[j] = a.c.value_step[n + row];
+                key_from[j] = value_from[j] = row * D + (chunk * 16 < D ? chunk * 16 : 0);
+            } else {
+                const int of_key = 8 * (chunk ^ key_swizzle(row)), of_value = 8 * (chunk ^ value_swizzle(row));
+                key_from[j] = of_key < D ? 2 * (row * D + of_key) : -1;
+                value_from[j] = of_value < D ? 2 * (row * D + of_value) : -1;
             }
         }
     }
-    // To LDS.  `checked`: some row does not see all keys, see Few::put_values.
-    __device__ bool put(const Attend &a, char *room, float *steps, int lane, int wave, bool checked, int from, int end, int pages, int base) const
+    // Keys and values of a unit: 16-bit elements to LDS, codes to registers.  Its blocks are those of lane `block` on, `rows` the number of the first row of
+    // each.
+    __device__ void load(const Attend &a, char *room, int64_t rows, int block, int wave, int lane)
     {
-        char *const keys = room, *const values = room + kKeys * kKeyStride;
+        const int row_bytes = a.c.D * (int)sizeof(C);
+        int64_t at[kLoads];
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int r = j * kPass + wave * kWavePass;
+            const int64_t bytes = rows * row_bytes;        // of every lane's block, of which one is taken
+            at[j] = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)bytes, block + r / 16) |
+                              (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bytes >> 32), block + r / 16) << 32);
+            if constexpr (kCodes) {
+                const int64_t n = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)rows, block + r / 16) |
+                                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(rows >> 32), block + r / 16) << 32);
+                k[j] = load16(a.c.keys + at[j] + (uint32_t)key_from[0]);
+                v[j] = load16(a.c.values + at[j] + (uint32_t)value_from[0]);
+                key_step[j] = a.c.key_step[n + (uint32_t)(r % 16 + lane / kChunks)];
+                value_step[j] = a.c.value_step[n + (uint32_t)(r % 16 + lane / kChunks)];
+            }
+        }
+        if constexpr (!kCodes) {
+            const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)room + wave * kWavePass * kRowBytes;
+#pragma unroll
+            for (int turn = 0; turn < kTurns; ++turn) {
+                if (key_from[turn] >= 0) {
+#pragma unroll
+                    for (int j = turn; j < kLoads; j += kTurns) to_lds(a.c.keys + at[j], (uint32_t)key_from[turn], to + j * kPass * kRowBytes);
+                }
+                if (value_from[turn] >= 0) {
+#pragma unroll
+                    for (int j = turn; j < kLoads; j += kTurns) to_lds(a.c.values + at[j], (uint32_t)value_from[turn], to + j * kPass * kRowBytes + kPart);
+                }
+            }
+        }
+    }
+    // Sixteen bytes for each lane, to LDS from `to` on in the order of the lanes.  Written out, since the compiler takes what comes to LDS this way to
+    // come to all of it and would wait before every read of the other buffer; the wait is in arrive().  No register is written but m0, which the
+    // compiler allots to nothing and sets itself before each use of its own (here it has none).
+    static __device__ void to_lds(const char *from, uint32_t offset, uint32_t to)
+    {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory");
+    }
+    // Codes to LDS.  `checked`: some row does not see all keys, see Few::put_values.
+    __device__ bool put(const Attend &a, char *room, float *steps, int lane, int wave, bool checked, int from, int end, uint32_t none) const
+    {
         const int chunk = lane % kChunks;
         bool bad = false;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const int r = j * kPass + wave * kWavePass + lane / kChunks;
-            bool none = false;
-            if (checked) none = from + r >= end || __builtin_amdgcn_readlane(pages, ((from + j * kPass + wave * kWavePass) >> 4) - base) < 0;
-            if constexpr (kCodes) {
+            const bool gone = checked && (from + r >= end || (none >> (r / 16) & 1));
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    *(v4u *)(keys + r * kKeyStride + 32 * chunk + 16 * h) = words<T>(codes8<T>(k[j][2 * h], k[j][2 * h + 1]));
-                    v4u w;
-                    if constexpr (kScaled) {
-                        w = words<T>(codes8<T>(v[j][2 * h], v[j][2 * h + 1], none ? 0.0f : value_step[j]));
-                        if (checked) bad |= make_finite<T>(w) && chunk * 16 < a.c.D;
-                    } else {
-                        w = words<T>(codes8<T>(v[j][2 * h], v[j][2 * h + 1]));
-                    }
-                    *(v4u *)(values + r * kValueStride + 32 * chunk + 16 * h) = w;
+            for (int h = 0; h < 2; ++h) {
+                *(v4u *)(room + r * kRowBytes + 16 * ((2 * chunk + h) ^ key_swizzle(r))) = words<T>(codes8<T>(k[j][2 * h], k[j][2 * h + 1]));
+                v4u w;
+                if constexpr (kScaled) {
+                    w = words<T>(codes8<T>(v[j][2 * h], v[j][2 * h + 1], gone ? 0.0f : value_step[j]));
+                    if (checked) bad |= make_finite<T>(w) && chunk * 16 < a.c.D;
+                } else {
+                    w = words<T>(codes8<T>(v[j][2 * h], v[j][2 * h + 1]));
                 }
-                if (chunk == 0) {
-                    steps[r] = key_step[j];
-                    steps[kKeys + r] = value_step[j];
-                }
-            } else {
-                v4u w = k[j], x = v[j];
-                if (a.c.D != DP && chunk * 8 >= a.c.D) w = v4u{0u, 0u, 0u, 0u};
-                if (checked) {
-                    if (none) x = v4u{0u, 0u, 0u, 0u};
-                    bad |= make_finite<T>(x) && chunk * 8 < a.c.D;
-                }
-                *(v4u *)(keys + r * kKeyStride + 16 * chunk) = w;
-                *(v4u *)(values + r * kValueStride + 16 * chunk) = x;
+                *(v4u *)(room + kPart + r * kRowBytes + 16 * ((2 * chunk + h) ^ value_swizzle(r))) = w;
             }
+            if (chunk == 0) {
+                steps[r] = key_step[j];
+                steps[kKeys + r] = value_step[j];
+            }
+        }
+        return __ballot(bad) != 0;
+    }
+    // 16-bit values that are in LDS, of a tile of which some row does not see all keys.  `none`: blocks without a page.
+    __device__ static bool check(const Attend &a, char *room, int from, int end, uint32_t none)
+    {
+        bool bad = false;
+#pragma unroll 1
+        for (int i = threadIdx.x; i < kPart / 16; i += 256) {
+            const int r = i / (DP / 8), chunk = (i % (DP / 8)) ^ value_swizzle(r);
+            v4u *const at = (v4u *)(room + kPart) + i;
+            v4u w = *at;
+            if (from + r >= end || (none >> (r / 16) & 1)) w = v4u{0u, 0u, 0u, 0u};
+            bad |= make_finite<T>(w) && 8 * chunk < a.c.D;
+            *at = w;
         }
         return __ballot(bad) != 0;
     }
 };
 
-template <typename T, typename C, int DP>
+template <typename T, typename C, int DP, bool PLAIN>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const Attend a)
 {
     typedef Many<T, C, DP> F;
     typedef typename F::v8 v8;
-    __shared__ __attribute__((aligned(16))) char room[2 * F::kStage];
+    __shared__ __attribute__((aligned(16))) char room[2][2 * F::kPart];
     __shared__ float steps[2][F::kCodes ? 2 * F::kKeys : 4];
-    __shared__ int bad_tile[2][4];                         // by wavefront
+    __shared__ int bad;                                    // a value taken out
+    __shared__ Tile tiles[kFewTiles];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const float to_cap = a.cap > 0.0f ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+    // Plain scores stay as the product has them until the exponential, whose addition takes the factor too.  Where the scale is negative the
+    // queries change their sign; 0 times what is masked would be NaN, so the factor is next to 0 where the scale is 0.
+    const float factor = PLAIN ? fmaxf(fabsf(to_cap), 1.2e-38f) : 1.0f;
 
-    Segments<F::kRows, F::kKeys> segments(a, (uint32_t *)room);
+    Segments<F::kRows, F::kKeys, 256> segments(a, (uint32_t *)room[0], tiles);
+    if (!F::kCodes && a.c.D != DP) {
+        // channels past D, which nothing is fetched to
+        for (int i = threadIdx.x; i < 4 * F::kPart / 16; i += 256) ((v4u *)room[0])[i] = v4u{0u, 0u, 0u, 0u};
+        __syncthreads();
+    }
+    F f;
+    f.prepare(a, wave, lane);
     while (segments.next(a)) {
         const Tile t = segments.t;
         const int head = segments.head, sums = segments.sums;
@@ -112,6 +178,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
             const int d = 16 * s + 8 * half;
             q[s] = v8{};
             if (row < t.rows && d < a.c.D) q[s] = pwlq_block::load8<T>(in + d);
+            if (PLAIN && a.scale < 0.0f) q[s] = -q[s];
         }
         v16f acc[F::kColumns];
 #pragma unroll
@@ -121,207 +188,230 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
         const int last = min(t.first + F::kRows, t.rows) - 1;
         // this wavefront's rows, and the slots that any of them may see
         const int my_first = min(t.first + 32 * wave, last), my_last = min(my_first + 31, last);
-        const bool mine = t.first + 32 * wave <= last;
         int my_end = t.hi, my_begin = t.lo;
         if (!a.tree) {
             my_end = min(max(t.q.kept() + my_last / a.group + 1, t.prefix), t.hi);
             if (a.window && !t.prefix) my_begin = max(t.q.kept() + my_first / a.group - a.window + 1, t.lo);
         }
+        if (t.first + 32 * wave > last) my_end = 0;
+        const Common whole = common(a, t, t.first, last), my_whole = common(a, t, my_first, my_last);
         const int32_t *const table = a.b.table + t.s * a.b.table_stride;
         const int begin = segments.begin, end = min(segments.stop, (t.hi + F::kKeys - 1) / F::kKeys);
-        F f;
-        int pages = -1, base = 0;
-        auto find_pages = [&](int from, bool first) {      // of the blocks of the tile at `from`
-            if (first || (from >> 4) - base == 64) {
-                base = from >> 4;
+        int64_t rows = 0;                                  // lane i: the first row of block base + i of sixteen keys,
+        uint64_t missing = 0;                              // bit i: which has no page
+        int base = 0;
+        auto load = [&](int u, int to) {
+            const int block = u * (F::kKeys / 16);
+            if (u == begin || block - base == 64) {
+                base = block;
                 const int slot = 16 * (base + lane);
-                pages = -1;
+                int page = -1;
                 if (slot < t.hi) {
-                    pages = table[slot >> a.c.shift];
-                    if ((unsigned)pages >= (unsigned)a.c.pages) pages = -1;
+                    page = table[slot >> a.c.shift];
+                    if ((unsigned)page >= (unsigned)a.c.pages) page = -1;
                 }
+                missing = __ballot(page < 0);
+                rows = row_number(a.c, Place{max(page, 0), slot & ((1 << a.c.shift) - 1)}, head);
             }
+            f.load(a, room[to], rows, block - base, wave, lane);
         };
-        // whether all rows of the tile see all keys from `from` on
-        auto whole = [&](int from) {
-            bool there = true;
-#pragma unroll
-            for (int b = 0; b < F::kKeys / 16; ++b) there = there && __builtin_amdgcn_readlane(pages, (from >> 4) - base + b) >= 0;
-            return there && all_see(a, t, t.first, last, from, from + F::kKeys);
+        auto lacks_of = [&](int u) { return (uint32_t)(missing >> (u * (F::kKeys / 16) - base)) & ((1u << F::kKeys / 16) - 1); };
+        // What was loaded last is in LDS for all wavefronts, and nobody reads the other buffer any more.
+        auto arrive_whole = [&](int to) {
+            if constexpr (F::kCodes) f.put(a, room[to], steps[to], lane, wave, false, 0, 0, 0u);
+            else __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0)
+            __syncthreads();
         };
-        bool full = false;
-        uint32_t lacks = 0;                                // blocks without a page of the tile that is worked on
-        auto put = [&](int from, int to) {
-            full = whole(from);
-            lacks = 0;
-#pragma unroll
-            for (int b = 0; b < F::kKeys / 16; ++b) lacks |= (uint32_t)(__builtin_amdgcn_readlane(pages, (from >> 4) - base + b) < 0) << b;
-            const bool bad = f.put(a, room + to * F::kStage, steps[to], lane, wave, !full, from, t.hi, pages, base);
-            if (lane == 0) bad_tile[to][wave] = bad;
-        };
-        if (begin < end) {
-            find_pages(begin * F::kKeys, true);
-            f.load(a, head, begin * F::kKeys, pages, base, wave, lane);
-            put(begin * F::kKeys, 0);
-        }
-        __syncthreads();
-        for (int u = begin; u < end; ++u) {
-            const int at = (u - begin) & 1, from = u * F::kKeys;
-            const bool all_full = full;
-            const uint32_t none = lacks;
-            if (u + 1 < end) {
-                find_pages(from + F::kKeys, false);
-                f.load(a, head, from + F::kKeys, pages, base, wave, lane);
+        auto arrive = [&](int u, int to) {
+            const int from = u * F::kKeys;
+            const uint32_t none = lacks_of(u);
+            if (none == 0 && whole.has(from, from + F::kKeys)) {
+                arrive_whole(to);
+                return;
             }
-            if (mine && from < my_end && from + F::kKeys > my_begin) {
-                const char *const keys = room + at * F::kStage + (lane & 31) * F::kKeyStride + 16 * half;
-                const char *const values = room + at * F::kStage + F::kKeys * F::kKeyStride +
-                                           (4 * half + (lane & 15) / 4) * F::kValueStride + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-                const bool my_full = all_full || (!none && all_see(a, t, my_first, my_last, from, from + F::kKeys));
-                v16f s[F::kBlocks];
+            if constexpr (F::kCodes) {
+                if (f.put(a, room[to], steps[to], lane, wave, true, from, t.hi, none)) bad = 1;
+            } else {
+                __builtin_amdgcn_s_waitcnt(0x0f70);
+                __syncthreads();
+                if (F::check(a, room[to], from, t.hi, none)) bad = 1;
+            }
+            __syncthreads();
+        };
+        const int key_at = (lane & 31) * F::kRowBytes + 16 * (F::key_swizzle(lane & 31) ^ half);
+        const int value_row = 4 * half + (lane & 15) / 4;
+        const int value_at = F::kPart + value_row * F::kRowBytes + 16 * (F::value_swizzle(value_row) ^ (2 * ((lane >> 4) & 1) + (lane >> 1 & 1))) + 8 * (lane & 1);
+        // A unit's work; `masked`: some row of the wavefront's may not see all keys.
+        auto work = [&](int u, int at, auto masked, uint32_t none) {
+            const int from = u * F::kKeys;
+            const float *const step = steps[at];
+            // operands are read from LDS some products before they are needed
+            auto key = [&](int b, int i) { return as8<T>(*(const v4u *)(room[at] + (key_at ^ 32 * i) + b * 32 * F::kRowBytes)); };
+            auto value = [&](int step, int c) {
+                const char *const p = room[at] + (value_at ^ 64 * c) + 16 * step * F::kRowBytes;
+                return columns8<T>(p, p + 8 * F::kRowBytes);
+            };
+            v16f s[F::kBlocks];
+            v8 k[F::kAhead], v[F::kColumns];
 #pragma unroll
-                for (int b = 0; b < F::kBlocks; ++b) {
-                    s[b] = v16f{};
+            for (int i = 0; i < F::kAhead; ++i) k[i] = key(i / F::kSteps, i % F::kSteps);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int step = 0; step < F::kSteps; ++step)
-                        s[b] = mfma32(as8<T>(*(const v4u *)(keys + b * 32 * F::kKeyStride + 32 * step)), q[step], s[b]);
-                }
-                // element i of block b is key 32 b + 8 (i / 4) + 4 half + i % 4
+            for (int n = 0; n < F::kBlocks * F::kSteps; ++n) {
+                const int b = n / F::kSteps, next = n + F::kAhead;
+                if (n % F::kSteps == 0) s[b] = v16f{};
+                s[b] = mfma32(k[n % F::kAhead], q[n % F::kSteps], s[b]);
+                if (next < F::kBlocks * F::kSteps) k[n % F::kAhead] = key(next / F::kSteps, next % F::kSteps);
+            }
 #pragma unroll
-                for (int b = 0; b < F::kBlocks; ++b) {
-                    if constexpr (F::kCodes) {
+            for (int c = 0; c < F::kColumns; ++c) v[c] = value(0, c);
+            __builtin_amdgcn_sched_barrier(0);
+            // element i of block b is key 32 b + 8 (i / 4) + 4 half + i % 4
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            const v4f step = *(const v4f *)(steps[at] + 32 * b + 2 * i + 4 * half);
+            for (int b = 0; b < F::kBlocks; ++b) {
+                if constexpr (F::kCodes) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) s[b][i + e] *= step[e];
-                        }
+                    for (int i = 0; i < 16; i += 4) {
+                        const v4f w = *(const v4f *)(step + 32 * b + 2 * i + 4 * half);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[b][i + e] *= w[e];
                     }
+                }
+                if constexpr (!PLAIN) {
+                    float x[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[b][i] *= to_cap;
+                    for (int i = 0; i < 16; ++i) x[i] = s[b][i];
                     if (a.cap > 0.0f) {
+                        cap_scores(x, to_cap, cap2);
+                    } else {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[b][i] = capped(s[b][i], cap2);
+                        for (int i = 0; i < 16; ++i) x[i] *= to_cap;
                     }
                     if (a.slopes) {
+                        const float away = (float)(state.own - from - 32 * b - 4 * half);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            s[b][i] -= state.slope * (float)abs(state.own - (from + 32 * b + 8 * (i / 4) + 4 * half + (i & 3)));
-                    }
-                }
-                uint32_t see[F::kBlocks];
-#pragma unroll
-                for (int b = 0; b < F::kBlocks; ++b) see[b] = 0xffff;
-                if (!my_full) {
-#pragma unroll
-                    for (int b = 0; b < F::kBlocks; ++b) {
-                        see[b] = 0;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int key = 32 * b + 8 * (i / 4) + 4 * half + (i & 3);
-                            const bool seen_it = !(none >> (2 * b + i / 8) & 1) & sees(a, t, state, from + key);
-                            see[b] |= (uint32_t)seen_it << i;
-                            s[b][i] = seen_it ? s[b][i] : -INFINITY;
-                        }
-                    }
-                }
-                float most = -INFINITY;
-#pragma unroll
-                for (int b = 0; b < F::kBlocks; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) most = fmaxf(most, s[b][i]);
-                if (__ballot(most > top + kSlack)) {
-                    most = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)));
-                    const float next = most == -INFINITY ? 0.0f : most;
-                    // a sum that is NaN already stays NaN
-                    const float old = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(reference - next);
-                    sum *= old;
-#pragma unroll
-                    for (int c = 0; c < F::kColumns; ++c)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[c][i] *= old;
-                    top = most;
-                    reference = next;
-                }
-                uint32_t above[F::kBlocks];
-                v8 weight[F::kBlocks][2];
-#pragma unroll
-                for (int b = 0; b < F::kBlocks; ++b) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        s[b][i] = __builtin_amdgcn_exp2f(s[b][i] - reference);
-                        if (!my_full && !(see[b] >> i & 1)) s[b][i] = 0.0f;
-                        sum += s[b][i];
-                    }
-                    above[b] = 0;
-                    if (!all_full) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) above[b] |= (s[b][i] > 0.0f ? 1u : 0u) << i;
-                    }
-                    if constexpr (F::kCodes && !F::kScaled) {
-                        // a row's step joins its weight: one rounding to bfloat16, of their product
-#pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
-                            const v4f step = *(const v4f *)(steps[at] + F::kKeys + 32 * b + 2 * i + 4 * half);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                s[b][i + e] = !my_full && !(see[b] >> (i + e) & 1) ? 0.0f : s[b][i + e] * step[e];
-                        }
+                        for (int i = 0; i < 16; ++i) x[i] = __builtin_fmaf(-state.slope, fabsf(away - (float)(8 * (i / 4) + (i & 3))), x[i]);
                     }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        v8f w;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) w[i] = s[b][8 * e + i];
-                        weight[b][e] = __builtin_convertvector(w, v8);
-                    }
-                }
-#pragma unroll
-                for (int b = 0; b < F::kBlocks; ++b)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-#pragma unroll
-                        for (int c = 0; c < F::kColumns; ++c) {
-                            const char *const p = values + (32 * b + 16 * e) * F::kValueStride + 64 * c;
-                            acc[c] = mfma32(columns8<T>(p, p + 8 * F::kValueStride), weight[b][e], acc[c]);
-                        }
-                if (!all_full && (bad_tile[at][0] | bad_tile[at][1] | bad_tile[at][2] | bad_tile[at][3])) {
-                    // infinities and NaN among the values, of which some rows see less than all: row by row and key by key
-                    uint32_t other_see[F::kBlocks], other_above[F::kBlocks];
-#pragma unroll
-                    for (int b = 0; b < F::kBlocks; ++b) {
-                        other_see[b] = __shfl_xor(see[b], 32);
-                        other_above[b] = __shfl_xor(above[b], 32);
-                    }
-                    for (int key = 0; key < F::kKeys && from + key < t.hi; ++key) {
-                        if (none >> (key / 16) & 1) continue;
-                        const int64_t n = row_number(a.c, Place{table[(from + key) >> a.c.shift], (from + key) & ((1 << a.c.shift) - 1)}, head);
-                        const int bit = (key & 3) + 4 * ((key >> 3) & 3);
-                        const bool own = ((key >> 2) & 1) == half;
-                        uint32_t sees_it = 0, weighs = 0;
-#pragma unroll
-                        for (int b = 0; b < F::kBlocks; ++b)
-                            if (b == key / 32) {
-                                sees_it = (own ? see[b] : other_see[b]) >> bit & 1;
-                                weighs = (own ? above[b] : other_above[b]) >> bit & 1;
-                            }
-#pragma unroll
-                        for (int c = 0; c < F::kColumns; ++c)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const int d = 32 * c + 8 * (i / 4) + 4 * half + (i & 3);
-                                if (d >= a.c.D) continue;
-                                float v = pwlq_block::widen(((const C *)a.c.values)[n * a.c.D + d]);
-                                if constexpr (F::kCodes) v = (float)(T)(v * a.c.value_step[n]);
-                                if (!(fabsf(v) < INFINITY) && sees_it) acc[c][i] += (weighs ? 1.0f : 0.0f) * v;
-                            }
-                    }
+                    for (int i = 0; i < 16; ++i) s[b][i] = x[i];
                 }
             }
-            if (u + 1 < end) put(from + F::kKeys, at ^ 1);
-            __syncthreads();
+            uint64_t seen = ~0ull;
+            if constexpr (masked.value) {
+                seen = seen_slots(a, t, state, from);
+#pragma unroll
+                for (int b = 0; b < F::kKeys / 16; ++b)
+                    if (none >> b & 1) seen &= ~(0xffffull << (16 * b));
+#pragma unroll
+                for (int b = 0; b < F::kBlocks; ++b) {
+                    const uint32_t of = (uint32_t)(seen >> (32 * b)) >> (4 * half);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = of >> (8 * (i / 4) + (i & 3)) & 1 ? s[b][i] : -INFINITY;
+                }
+            }
+            float most = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < F::kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, s[b][i]);
+            most *= factor;
+            if (__ballot(most > top + kSlack)) {
+                most = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)));
+                const float next = most == -INFINITY ? 0.0f : most;
+                // a sum that is NaN already stays NaN
+                const float old = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(reference - next);
+                sum *= old;
+#pragma unroll
+                for (int c = 0; c < F::kColumns; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[c][i] *= old;
+                top = most;
+                reference = next;
+            }
+            v8 weight[F::kBlocks][2];
+#pragma unroll
+            for (int b = 0; b < F::kBlocks; ++b) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], factor, -reference));
+                    sum += s[b][i];
+                }
+                if constexpr (F::kCodes && !F::kScaled) {
+                    // a row's step joins its weight: one rounding to bfloat16, of their product; a step may be NaN
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const v4f w = *(const v4f *)(step + F::kKeys + 32 * b + 2 * i + 4 * half);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[b][i + e] *= w[e];
+                    }
+                    if constexpr (masked.value) {
+                        const uint32_t of = (uint32_t)(seen >> (32 * b)) >> (4 * half);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) s[b][i] = of >> (8 * (i / 4) + (i & 3)) & 1 ? s[b][i] : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    v8f w;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = s[b][8 * e + i];
+                    weight[b][e] = __builtin_convertvector(w, v8);
+                }
+            }
+#pragma unroll
+            for (int step = 0; step < 2 * F::kBlocks; ++step)
+#pragma unroll
+                for (int c = 0; c < F::kColumns; ++c) {
+                    acc[c] = mfma32(v[c], weight[step / 2][step & 1], acc[c]);
+                    if (step + 1 < 2 * F::kBlocks) v[c] = value(step + 1, c);
+                }
+        };
+        if (threadIdx.x == 0) bad = 0;
+        __syncthreads();
+        if (begin < end) {
+            load(begin, 0);
+            arrive(begin, 0);
+        }
+        // Units that all rows see whole, as they mostly are, have a loop of their own, with nothing about masks in it.
+        int u = begin, at = 0;
+        auto whole_to = [&](int u) {                       // the end of such units from u on, none of which lacks a page
+            const int from = u * F::kKeys;
+            int stop = u;
+            if (whole.has(from, from + F::kKeys)) stop = max(from >= whole.begin ? whole.end : 0, whole.prefix) / F::kKeys;
+            stop = min(stop, end);
+            const uint64_t holes = missing >> (u * (F::kKeys / 16) - base);
+            // as far as the pages are known that are there
+            return min(stop, u + min((int)__builtin_ctzll(holes | 1ull << 63), 64 - (u * (F::kKeys / 16) - base)) / (F::kKeys / 16));
+        };
+        while (u < end) {
+            for (const int stop = whole_to(u) - 1; u < stop; ++u, at ^= 1) {
+                load(u + 1, at ^ 1);
+                work(u, at, std::false_type(), 0u);
+                arrive_whole(at ^ 1);
+            }
+            const uint32_t none = lacks_of(u);
+            const int from = u * F::kKeys;
+            if (u + 1 < end) load(u + 1, at ^ 1);
+            if (from < my_end && from + F::kKeys > my_begin) work(u, at, std::true_type(), none);
+            if (u + 1 < end) arrive(u + 1, at ^ 1);
+            ++u;
+            at ^= 1;
         }
 
+        if (F::kMayBeBad && __builtin_amdgcn_readfirstlane(bad)) {
+#pragma unroll
+            for (int c = 0; c < F::kColumns; ++c) {
+                v16f count = {}, sign = {};
+                for (int from = begin * F::kKeys; from < end * F::kKeys; from += 16) {
+                    const uint32_t mine = (uint32_t)(seen_slots(a, t, state, from) >> (4 * half));
+                    const NotFinite<T, C> v(a, table, head, from + 4 * half, 8, t.hi, 32 * c + (lane & 31), (mine & 15) | (mine >> 4 & 0xf0));
+                    count = mfma32(v.counts, v.ones, count);
+                    sign = mfma32(v.signs, v.ones, sign);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[c][i] += not_finite_sum(count[i], sign[i]);
+            }
+        }
         sum += __shfl_xor(sum, 32);
         if (row < t.rows) {
             const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
