@@ -27,6 +27,7 @@ struct Attend {
     char *out;
     int64_t q_stride, q_head, out_stride, out_head;
     int group;                           // heads of queries for one of the cache
+    uint64_t per_group;                  // ceil(2^40 / group)
     float scale, cap;
     const float *slopes;
     int window;                          // 0: none
@@ -36,7 +37,8 @@ struct Attend {
     int tiles;                           // numbers of tiles, of which some may stand for none
     int each;                            // without starts: tiles of a sequence
     int parts;                           // workgroups that the line is cut for; 0: a workgroup for each item
-    int least;                           // units of a part, at least
+    int least;                           // units of a part, at least,
+    int alone;                           // and where that leaves no more parts than CUs: a second workgroup there pays for longer ones
     uint64_t *part;                      // workspace: units of a part,
     struct Stretch *stretches;           // of the tiles on the line,
     float2 *top_sum;                     // m and the sum of each row of two sums for each part,
@@ -47,6 +49,10 @@ constexpr int kMostTiles = 2047;         // of a call that is split
 constexpr float kLog2e = 1.4426950408889634f;
 // The reference is moved when a score passes it by more than this, so that most tiles move no sums.  exp2(8) keeps within binary16.
 constexpr float kSlack = 8.0f;
+
+// n / group for 0 <= n < 2^30: what per_group is too large by adds less than n / 2^40 <= 1 / group.  A division takes 25 instructions, and those that
+// run once before the first key are fetched once each, which is what they cost.
+__device__ inline int by_group(const Attend &a, int n) { return (int)((uint64_t)(uint32_t)n * a.per_group >> 40); }
 
 // A tile: rows first to first + M - 1 of a sequence's `rows` query rows, and the slots that any of them may see.
 struct Tile {
@@ -66,7 +72,7 @@ __device__ inline Tile tile_of(const Attend &a, int s, int i, Sequence q, int M)
     t.prefix = a.prefix ? min(max(a.prefix[s], 0), q.length) : 0;
     t.lo = t.hi = 0;
     if (t.none()) return t;
-    const int j0 = t.first / a.group, j1 = (min(t.first + M, t.rows) - 1) / a.group, kept = q.kept();
+    const int j0 = by_group(a, t.first), j1 = by_group(a, min(t.first + M, t.rows) - 1), kept = q.kept();
     if (a.tree) t.hi = q.length;
     else {
         t.hi = min(max(max(kept + j1 + 1, t.prefix), 0), q.length);
@@ -96,7 +102,12 @@ __device__ inline Tile tile(const Attend &a, int u, int M)
 // Units of keys of a tile: one at least, where its rows get zeros.
 __device__ inline int units_of(const Tile &t, int unit) { return t.none() ? 0 : max((t.hi + unit - 1) / unit - t.lo / unit, 1); }
 
-// Where a tile lies on the line, and which rows it has; as it is read by the join.
+// An item has so many units more on the line, before its first one, for what a workgroup does beside its keys: queries, masks, the first keys' way
+// and the sums' take 4 to 8 us, a unit 1.2 to 2.4.  Without it a part of many short items takes twice as long as one of a long one.
+constexpr int kSetup = 3;
+__device__ inline int length_of(int units) { return units ? units + kSetup : 0; }
+
+// Where a tile lies on the line (of one head), its units, and which rows it has; as it is read by the join.
 struct alignas(32) Stretch {
     uint32_t begin, units;
     int first, rows, start;
@@ -125,7 +136,7 @@ template <int THREADS> __device__ inline uint32_t sum_before(uint32_t v, uint32_
     return before + s - v;
 }
 
-// Where a workgroup's part of the line begins: units x to end - 1, the first of them unit `skip` of head `head` of tile u.
+// Where a workgroup's part of the line begins: places x to end - 1, the first of them place `skip` of head `head` of tile u.
 struct Part {
     int64_t x, end, part;
     int u, head, skip;
@@ -133,18 +144,19 @@ struct Part {
     __device__ void cut(const Attend &a, uint32_t all)
     {
         const int64_t line = (int64_t)all * a.c.heads;
-        part = max((line + a.parts - 1) / a.parts, (int64_t)a.least);
+        part = line < 1LL << 31 ? (int64_t)(((uint32_t)line + (uint32_t)a.parts - 1) / (uint32_t)a.parts) : (line + a.parts - 1) / a.parts;
+        part = max(max(part, min((line + 255) / 256, (int64_t)a.alone)), (int64_t)a.least);
         x = (int64_t)blockIdx.x * part;
         end = min(x + part, line);
         u = head = skip = 0;
         if (blockIdx.x == 0 && threadIdx.x == 0) *a.part = (uint64_t)part;
     }
-    __device__ void start(const Attend &a, int tile, uint32_t begin, int units)
+    __device__ void start(const Attend &a, int tile, uint32_t begin, int length)
     {
-        const int into = (int)(x - (int64_t)begin * a.c.heads);
+        const uint32_t into = (uint32_t)(x - (int64_t)begin * a.c.heads);
         u = __builtin_amdgcn_readfirstlane(tile);
-        head = __builtin_amdgcn_readfirstlane(into / units);
-        skip = __builtin_amdgcn_readfirstlane(into - into / units * units);
+        head = __builtin_amdgcn_readfirstlane((int)(into / (uint32_t)length));
+        skip = __builtin_amdgcn_readfirstlane((int)into) - head * length;
     }
 };
 
@@ -176,7 +188,8 @@ template <int M, int UNIT> __device__ Part plan_few(const Attend &a, Tile *tiles
     }
     const Tile t = tile_of(a, s, i, sequence(a.b, s, start, end, a.b.lengths[s]), M);
     const int units = lane < a.tiles ? units_of(t, UNIT) : 0;
-    uint32_t stop = (uint32_t)units;                        // and so its end on the line
+    const int length = length_of(units);
+    uint32_t stop = (uint32_t)length;                       // and so its end on the line
 #pragma unroll
     for (int k = 1; k < 64; k *= 2) {
         const uint32_t o = (uint32_t)__shfl_up((int)stop, k);
@@ -184,11 +197,11 @@ template <int M, int UNIT> __device__ Part plan_few(const Attend &a, Tile *tiles
     }
     Part p;
     p.cut(a, (uint32_t)__builtin_amdgcn_readlane((int)stop, 63));
-    if (blockIdx.x == 0 && threadIdx.x < a.tiles) a.stretches[lane] = Stretch(stop - units, units, t);
+    if (blockIdx.x == 0 && threadIdx.x < a.tiles) a.stretches[lane] = Stretch(stop - length, units, t);
     if (threadIdx.x < a.tiles) tiles[lane] = t;
     if (p.x < p.end) {
         const int at = __builtin_ctzll(__ballot((int64_t)stop * a.c.heads > p.x));
-        const int n = __builtin_amdgcn_readlane(units, at);
+        const int n = __builtin_amdgcn_readlane(length, at);
         p.start(a, at, (uint32_t)(__builtin_amdgcn_readlane((int)stop, at) - n), n);
     }
     __syncthreads();
@@ -221,7 +234,7 @@ template <int M, int UNIT, int THREADS> __device__ Part plan(const Attend &a, ui
     };
     uint32_t mine = 0;
     for (int u = from; u < to; ++u) {
-        const int n = units_of(tile_at(u), UNIT);
+        const int n = length_of(units_of(tile_at(u), UNIT));
         begin[u] = (uint32_t)n;
         mine += (uint32_t)n;
     }
@@ -229,7 +242,7 @@ template <int M, int UNIT, int THREADS> __device__ Part plan(const Attend &a, ui
     for (int u = from; u < to; ++u) {
         const uint32_t n = begin[u];
         begin[u] = at;
-        if (blockIdx.x == 0) a.stretches[u] = Stretch(at, (int)n, tile_at(u));
+        if (blockIdx.x == 0) a.stretches[u] = Stretch(at, n ? (int)n - kSetup : 0, tile_at(u));
         at += n;
     }
     if (threadIdx.x == 0) begin[a.tiles] = all;
@@ -287,27 +300,32 @@ template <int M, int UNIT, int THREADS> struct Segments {
             }
             return false;
         }
-        if (p.x >= p.end) return false;
-        while (units <= 0) {
-            t = tiles ? uniform(tiles[p.u]) : tile(a, p.u, M);
-            units = units_of(t, UNIT);
-            if (units == 0 && ++p.u >= a.tiles) return false;
+        while (p.x < p.end) {
+            while (units <= 0) {
+                if (p.u >= a.tiles) return false;
+                t = tiles ? uniform(tiles[p.u]) : tile(a, p.u, M);
+                units = units_of(t, UNIT);
+                if (units == 0) ++p.u;
+            }
+            const int n = (int)min((int64_t)(units + kSetup - p.skip), p.end - p.x);
+            if (n <= 0) return false;                       // starts that do not rise: the line does not fit them
+            const int from = max(p.skip - kSetup, 0), to = max(p.skip + n - kSetup, 0);
+            head = p.head;
+            begin = t.lo / UNIT + from;
+            stop = t.lo / UNIT + to;
+            // its sums are the first of the part if the item began before the part or with it
+            sums = from == 0 && to == units ? -1 : 2 * (int)blockIdx.x + (p.x - p.skip > (int64_t)blockIdx.x * p.part);
+            p.x += n;
+            p.skip = 0;
+            const bool any = to > from;
+            if (++p.head == a.c.heads) {
+                p.head = 0;
+                ++p.u;
+                units = -1;
+            }
+            if (any) return true;
         }
-        const int n = (int)min((int64_t)(units - p.skip), p.end - p.x);
-        if (n <= 0) return false;                           // starts that do not rise: the line does not fit them
-        head = p.head;
-        begin = t.lo / UNIT + p.skip;
-        stop = begin + n;
-        // its sums are the first of the part if the item began before the part or with it
-        sums = n == units ? -1 : 2 * (int)blockIdx.x + (p.skip == 0 && p.x > (int64_t)blockIdx.x * p.part);
-        p.x += n;
-        p.skip = 0;
-        if (++p.head == a.c.heads) {
-            p.head = 0;
-            ++p.u;
-            units = -1;
-        }
-        return true;
+        return false;
     }
 };
 
@@ -355,7 +373,7 @@ __device__ inline RowState row_state(const Attend &a, const Tile &t, int row, in
 {
     RowState r = {-1, 0, 0, 0, 0.0f, 0, nullptr};
     if (row >= t.rows) return r;
-    const int j = row / a.group, h = head * a.group + row - j * a.group, kept = t.q.kept();
+    const int j = by_group(a, row), h = head * a.group + row - j * a.group, kept = t.q.kept();
     if (a.slopes) r.slope = a.slopes[h] * kLog2e;
     if (kept + j < 0) return r;
     r.own = kept + j;
@@ -397,7 +415,7 @@ struct Common {
 };
 __device__ inline Common common(const Attend &a, const Tile &t, int first, int last)
 {
-    const int kept = t.q.kept(), j0 = first / a.group, j1 = last / a.group;
+    const int kept = t.q.kept(), j0 = by_group(a, first), j1 = by_group(a, last);
     Common c = {0, 0, 0};
     if (kept + j0 < 0) return c;
     c.prefix = t.prefix;
@@ -488,23 +506,25 @@ template <typename T, typename C> struct NotFinite {
 
     __device__ NotFinite(const Attend &a, const int32_t *table, int head, int from, int apart, int end, int d, uint32_t seen)
     {
-#pragma unroll
+        uint32_t bad = 0, plus = 0, minus = 0;
+#pragma unroll 1
         for (int i = 0; i < 8; ++i) {
             const int slot = from + (i & 3) + (i / 4) * apart;
-            float n = 0.0f, s = 0.0f;
-            if (slot < end && d < a.c.D) {
-                const int page = table[slot >> a.c.shift];
-                if ((unsigned)page < (unsigned)a.c.pages) {
-                    const int64_t row = row_number(a.c, Place{page, slot & ((1 << a.c.shift) - 1)}, head);
-                    float v = pwlq_block::widen(((const C *)a.c.values)[row * a.c.D + d]);
-                    if constexpr (sizeof(C) == 1) v = (float)(T)(v * a.c.value_step[row]);
-                    if (!(fabsf(v) < INFINITY)) n = 1.0f;
-                    if (fabsf(v) == INFINITY) s = v > 0.0f ? 1.0f : -1.0f;
-                }
-            }
-            counts[i] = (T)n;
-            signs[i] = (T)s;
-            ones[i] = (T)(float)(seen >> i & 1);
+            if (slot >= end || d >= a.c.D) continue;
+            const int page = table[slot >> a.c.shift];
+            if ((unsigned)page >= (unsigned)a.c.pages) continue;
+            const int64_t row = row_number(a.c, Place{page, slot & ((1 << a.c.shift) - 1)}, head);
+            float v = pwlq_block::widen(((const C *)a.c.values)[row * a.c.D + d]);
+            if constexpr (sizeof(C) == 1) v = (float)(T)(v * a.c.value_step[row]);
+            bad |= (uint32_t)!(fabsf(v) < INFINITY) << i;
+            plus |= (uint32_t)(v == INFINITY) << i;
+            minus |= (uint32_t)(v == -INFINITY) << i;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            counts[i] = bad >> i & 1 ? (T)1.0f : (T)0.0f;
+            signs[i] = plus >> i & 1 ? (T)1.0f : minus >> i & 1 ? (T)-1.0f : (T)0.0f;
+            ones[i] = seen >> i & 1 ? (T)1.0f : (T)0.0f;
         }
     }
 };

@@ -20,9 +20,11 @@ template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void k
     __shared__ v4f sums[kGroups][kLanes];
     __shared__ float2 tops[kGroups];
     const Stretch t = a.stretches[blockIdx.x];
-    const int64_t part = (int64_t)*a.part, n = t.units, x = (int64_t)t.begin * a.c.heads + blockIdx.y * n;
-    if (n == 0 || x / part == (x + n - 1) / part || t.first + (int)blockIdx.z * ROWS >= t.rows) return;
-    const int64_t first = x / part, last = (x + n - 1) / part;
+    // the parts with its first unit and its last
+    const int64_t part = (int64_t)*a.part, n = t.units + kSetup, x = (int64_t)t.begin * a.c.heads + blockIdx.y * n;
+    if (t.units == 0 || t.first + (int)blockIdx.z * ROWS >= t.rows) return;
+    const int64_t first = (x + kSetup) / part, last = (x + n - 1) / part;
+    if (first == last) return;
     const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, turn = group % kEach, d = 4 * lane;
 #pragma unroll
     for (int r = 0; r < ROWS; r += kGroups / kEach) {
@@ -52,7 +54,7 @@ template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void k
                 for (int g = 1; g < kEach; ++g) add(tops[group + g], sums[group + g][lane]);
         }
         if (turn != 0 || row >= t.rows || d >= a.c.D) continue;
-        const int j = row / a.group, h = blockIdx.y * a.group + row - j * a.group;
+        const int j = by_group(a, row), h = blockIdx.y * a.group + row - j * a.group;
         store4<T>(a.out + ((t.start + j) * a.out_stride + h * a.out_head + d) * 2, total == 0.0f ? v4f{} : v * (1.0f / total));
     }
 }
@@ -65,7 +67,8 @@ Shape shape_of(const pwlq_attend_args &g)
     Shape s = {};
     const int64_t group = g.q_heads / g.cache.heads, longest = !g.batch.starts ? 1 : g.longest ? g.longest : g.batch.T;
     s.channels = g.cache.D <= 64 ? 64 : g.cache.D <= 128 ? 128 : 256;
-    s.rows = longest * group <= 16 ? 16 : longest * group <= 32 ? 32 : 128;
+    const int64_t rows = longest * group, most_few = s.channels == 256 ? 16 : 64;
+    s.rows = rows > most_few ? 128 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     s.unit = s.rows < 128 ? 128 : s.channels == 256 ? 32 : 64;
     s.each = (int)((group + s.rows - 1) / s.rows);
     const int64_t tiles = g.batch.starts ? g.batch.T * group / s.rows + g.batch.S : g.batch.S * s.each;
@@ -73,10 +76,10 @@ Shape shape_of(const pwlq_attend_args &g)
     s.least = s.rows < 128 ? 1 : 4;
     const int64_t units = (g.batch.table_pages * g.cache.page + s.unit - 1) / s.unit, items = tiles * g.cache.heads;
     const bool enough = s.rows == 128 && items >= 1024;
-    if (tiles <= kMostTiles && g.batch.S <= kMostTiles && tiles * units < 1LL << 31 && !enough) {
-        const int64_t all = items * (units > 1 ? units : 1);
+    if (tiles <= kMostTiles && g.batch.S <= kMostTiles && tiles * (units + kSetup + 1) < 1LL << 31 && !enough) {
+        const int64_t all = items * ((units > 1 ? units : 1) + kSetup);
         const int64_t parts = (all + s.least - 1) / s.least;
-        const int most = s.channels == 256 ? 256 : 512;    // what the chip holds: 256 channels take a CU's registers
+        const int most = s.rows < 128 ? (s.rows * s.channels > 2048 ? 256 : 512) : s.channels == 256 ? 256 : 512;    // what the chip holds at once
         s.parts = (int)(parts < most ? parts : most);
     }
     auto place = [&](size_t bytes) {
@@ -108,6 +111,7 @@ void attend(const pwlq_attend_args &g, void *workspace, hipStream_t stream)
     a.q_stride = g.q.stride, a.q_head = g.q.head_stride;
     a.out_stride = g.out.stride, a.out_head = g.out.head_stride;
     a.group = g.q_heads / g.cache.heads;
+    a.per_group = ((1ULL << 40) + a.group - 1) / a.group;
     a.scale = g.scale;
     a.cap = g.cap;
     a.slopes = g.slopes;
@@ -119,6 +123,7 @@ void attend(const pwlq_attend_args &g, void *workspace, hipStream_t stream)
     a.each = s.each;
     a.parts = s.parts;
     a.least = s.least;
+    a.alone = s.rows < 128 ? 1 : 8;
     char *const w = (char *)workspace;
     a.part = (uint64_t *)(w + s.part);
     a.stretches = (Stretch *)(w + s.stretches);
@@ -136,17 +141,21 @@ void attend(const pwlq_attend_args &g, void *workspace, hipStream_t stream)
     }
     if (s.parts < 2) return;
 #define PWLQ_JOIN_ROWS(T, DP, ROWS)                                                                                  \
-    k_attend_join<T, DP, ROWS><<<dim3((unsigned)s.tiles, (unsigned)a.c.heads, (unsigned)(s.rows / ROWS)), 256, 0, stream>>>(a, s.rows)
+    k_attend_join<T, DP, ROWS><<<dim3((unsigned)s.tiles, (unsigned)a.c.heads, (unsigned)(s.rows / (ROWS))), 256, 0, stream>>>(a, s.rows)
 #define PWLQ_JOIN(T)                                                                         \
     do {                                                                                     \
-        if (s.rows < 128) {                                                                  \
+        if (s.rows < 128 && s.parts >= 16 * s.tiles * a.c.heads) {                           \
+            if (s.channels == 64) PWLQ_JOIN_ROWS(T, 64, 1);                                  \
+            else if (s.channels == 128) PWLQ_JOIN_ROWS(T, 128, 1);                           \
+            else PWLQ_JOIN_ROWS(T, 256, 1);                                                  \
+        } else if (s.rows < 128) {                                                           \
             if (s.channels == 64) PWLQ_JOIN_ROWS(T, 64, 2);                                  \
             else if (s.channels == 128) PWLQ_JOIN_ROWS(T, 128, 2);                           \
             else PWLQ_JOIN_ROWS(T, 256, 2);                                                  \
         } else {                                                                             \
-            if (s.channels == 64) PWLQ_JOIN_ROWS(T, 64, 16);                                 \
-            else if (s.channels == 128) PWLQ_JOIN_ROWS(T, 128, 16);                          \
-            else PWLQ_JOIN_ROWS(T, 256, 16);                                                 \
+            if (s.channels == 64) PWLQ_JOIN_ROWS(T, 64, 8);                                 \
+            else if (s.channels == 128) PWLQ_JOIN_ROWS(T, 128, 8);                          \
+            else PWLQ_JOIN_ROWS(T, 256, 4);                                                 \
         }                                                                                    \
     } while (0)
     if (g.q.type == PWLQ_BF16) PWLQ_JOIN(bf16);

@@ -1,4 +1,4 @@
-// k_attend_few: tiles of 16 or 32 query rows, for single tokens and small trees.
+// k_attend_few: tiles of 16 to 64 query rows, for single tokens and trees.
 //
 // Bound by memory: keys and values are read once, with matrix instructions as good as idle (16 rows against 32 keys of 128
 // channels take 256 of their cycles for 16 KiB).  Each of the four wavefronts takes 32 keys of a unit of 128 by itself, with
@@ -111,7 +111,7 @@ template <typename T, typename C, int DP, int RB> struct Few {
 };
 
 template <typename T, typename C, int DP, int RB, bool PLAIN>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Attend a)
+__global__ __launch_bounds__(256, DP * RB > 128 ? 1 : 2) void k_attend_few(const Attend a)
 {
     typedef Few<T, C, DP, RB> F;
     typedef typename F::v8 v8;
@@ -128,31 +128,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
     while (segments.next(a)) {
         const Tile t = segments.t;
         const int head = segments.head, begin = segments.begin, stop = segments.stop, sums = segments.sums;
-        v8 q[RB][F::kSteps];
-        RowState state[RB];
-        v4f acc[RB][F::kColumns];
-        float top[RB], reference[RB], sum[RB];
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const int row = t.first + 16 * r + (lane & 15);
-            state[r] = row_state(a, t, row, head);
-            const int j = min(row, t.rows - 1) / a.group, h = head * a.group + min(row, t.rows - 1) - j * a.group;
-            const T *const in = (const T *)a.q + (int64_t)(t.q.start + j) * a.q_stride + h * a.q_head;
-#pragma unroll
-            for (int s = 0; s < F::kSteps; ++s) {
-                const int d = F::channel(s, quarter);
-                q[r][s] = v8{};
-                if (row < t.rows && d < a.c.D) q[r][s] = pwlq_block::load8<T>(in + d);
-            }
-#pragma unroll
-            for (int c = 0; c < F::kColumns; ++c) acc[r][c] = v4f{};
-            top[r] = -INFINITY;
-            reference[r] = sum[r] = 0.0f;
-        }
         // this wavefront's units: 32 keys from 128 u + 32 wave on
         const int first = max(begin, (t.lo - 32 * wave + 96) >> 7), end = min(stop, (t.hi - 32 * wave + 127) >> 7);
         const int32_t *const table = a.b.table + t.s * a.b.table_stride;
-        const Common whole = common(a, t, t.first, min(t.first + F::kRows, t.rows) - 1);
         bool bad = false;                                  // a value taken out
         F f;
         int pages = -1, p[2];                              // lane 2i + b: the page of block b of unit base + i
@@ -174,6 +152,29 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
             find_pages(first);
             f.load(a, head, 128 * first + 32 * wave, p, lane);
         }
+        // the queries while the first keys are on their way
+        v8 q[RB][F::kSteps];
+        RowState state[RB];
+        v4f acc[RB][F::kColumns];
+        float top[RB], reference[RB], sum[RB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int row = t.first + 16 * r + (lane & 15);
+            state[r] = row_state(a, t, row, head);
+            const int j = by_group(a, min(row, t.rows - 1)), h = head * a.group + min(row, t.rows - 1) - j * a.group;
+            const T *const in = (const T *)a.q + (int64_t)(t.q.start + j) * a.q_stride + h * a.q_head;
+#pragma unroll
+            for (int s = 0; s < F::kSteps; ++s) {
+                const int d = F::channel(s, quarter);
+                q[r][s] = v8{};
+                if (row < t.rows && d < a.c.D) q[r][s] = pwlq_block::load8<T>(in + d);
+            }
+#pragma unroll
+            for (int c = 0; c < F::kColumns; ++c) acc[r][c] = v4f{};
+            top[r] = -INFINITY;
+            reference[r] = sum[r] = 0.0f;
+        }
+        const Common whole = common(a, t, t.first, min(t.first + F::kRows, t.rows) - 1);
         for (int u = first; u < end; ++u) {
             const int from = 128 * u + 32 * wave, now[2] = {p[0], p[1]};
             const bool full = now[0] >= 0 && now[1] >= 0 && whole.has(from, from + 32);
@@ -274,24 +275,6 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
             __builtin_amdgcn_wave_barrier();
         }
 
-        if (F::kMayBeBad && bad) {
-#pragma unroll
-            for (int r = 0; r < RB; ++r)
-#pragma unroll
-                for (int c = 0; c < F::kColumns; ++c) {
-                    v4f count = {}, sign = {};
-                    for (int u = first; u < end; ++u) {
-                        const int from = 128 * u + 32 * wave;
-                        const uint32_t mine = (uint32_t)(seen_slots(a, t, state[r], from) >> (4 * quarter));
-                        const NotFinite<T, C> v(a, table, head, from + 4 * quarter, 16, t.hi, 16 * c + (lane & 15), (mine & 15) | (mine >> 12 & 0xf0));
-                        count = mfma16(v.counts, v.ones, count);
-                        sign = mfma16(v.signs, v.ones, sign);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[r][c][i] += not_finite_sum(count[i], sign[i]);
-                }
-        }
-
         // the four wavefronts' sums
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
@@ -310,6 +293,24 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
 #pragma unroll
             for (int c = 0; c < F::kColumns; ++c)
                 *(v4f *)(all + (wave * 16 + (lane & 15)) * F::kSumStride + 16 * c + 4 * quarter) = acc[r][c] * factor;
+            if (F::kMayBeBad && bad) {
+#pragma unroll 1
+                for (int c = 0; c < F::kColumns; ++c) {
+                    v4f count = {}, sign = {};
+                    for (int u = first; u < end; ++u) {
+                        const int from = 128 * u + 32 * wave;
+                        const uint32_t mine = (uint32_t)(seen_slots(a, t, state[r], from) >> (4 * quarter));
+                        const NotFinite<T, C> v(a, table, head, from + 4 * quarter, 16, t.hi, 16 * c + (lane & 15), (mine & 15) | (mine >> 12 & 0xf0));
+                        count = mfma16(v.counts, v.ones, count);
+                        sign = mfma16(v.signs, v.ones, sign);
+                    }
+                    v4f *const at = (v4f *)(all + (wave * 16 + (lane & 15)) * F::kSumStride + 16 * c + 4 * quarter);
+                    v4f v = *at;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] += not_finite_sum(count[i], sign[i]);
+                    *at = v;
+                }
+            }
             __syncthreads();
             for (int i = threadIdx.x; i < 16 * DP / 4; i += 256) {
                 const int of = i / (DP / 4), d = i % (DP / 4) * 4, row = t.first + 16 * r + of;
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_few(const Att
                     *(v4f *)(a.sums + at * DP + d) = v;
                     if (d == 0) a.top_sum[at] = make_float2(m, total);
                 } else {
-                    const int j = row / a.group, h = head * a.group + row - j * a.group;
+                    const int j = by_group(a, row), h = head * a.group + row - j * a.group;
                     store4<T>(a.out + ((t.q.start + j) * a.out_stride + h * a.out_head + d) * 2, total == 0.0f ? v4f{} : v * (1.0f / total));
                 }
             }

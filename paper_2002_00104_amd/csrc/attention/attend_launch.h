@@ -10,11 +10,14 @@ template <typename T, typename C> void attend_launch(const Attend &a, int D, int
 {
     // scores as the product has them, or capped or with a bias
     const bool plain = !(a.cap > 0.0f) && !a.slopes;
-#define PWLQ_ATTEND_AS(DP, PLAIN)                                                            \
-    do {                                                                                     \
-        if (rows == 16) k_attend_few<T, C, DP, 1, PLAIN><<<grid, 256, 0, stream>>>(a);       \
-        else if (rows == 32) k_attend_few<T, C, DP, 2, PLAIN><<<grid, 256, 0, stream>>>(a);  \
-        else k_attend_many<T, C, DP, PLAIN><<<grid, 256, 0, stream>>>(a);                    \
+#define PWLQ_ATTEND_AS(DP, PLAIN)                                                                            \
+    do {                                                                                                     \
+        if (rows == 16) k_attend_few<T, C, DP, 1, PLAIN><<<grid, 256, 0, stream>>>(a);                       \
+        else if (rows == 128) k_attend_many<T, C, DP, PLAIN><<<grid, 256, 0, stream>>>(a);                   \
+        else if constexpr (DP != 256) {                                                                      \
+            if (rows == 32) k_attend_few<T, C, DP, 2, PLAIN><<<grid, 256, 0, stream>>>(a);                   \
+            else k_attend_few<T, C, DP, 4, PLAIN><<<grid, 256, 0, stream>>>(a);                              \
+        }                                                                                                    \
     } while (0)
 #define PWLQ_ATTEND(DP)                            \
     do {                                           \

@@ -168,33 +168,6 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
     while (segments.next(a)) {
         const Tile t = segments.t;
         const int head = segments.head, sums = segments.sums;
-        const int row = t.first + 32 * wave + (lane & 31), clamped = min(row, t.rows - 1);
-        const RowState state = row_state(a, t, row, head);
-        const int j = clamped / a.group, h = head * a.group + clamped - j * a.group;
-        const T *const in = (const T *)a.q + (int64_t)(t.q.start + j) * a.q_stride + h * a.q_head;
-        v8 q[F::kSteps];
-#pragma unroll
-        for (int s = 0; s < F::kSteps; ++s) {
-            const int d = 16 * s + 8 * half;
-            q[s] = v8{};
-            if (row < t.rows && d < a.c.D) q[s] = pwlq_block::load8<T>(in + d);
-            if (PLAIN && a.scale < 0.0f) q[s] = -q[s];
-        }
-        v16f acc[F::kColumns];
-#pragma unroll
-        for (int c = 0; c < F::kColumns; ++c) acc[c] = v16f{};
-        float top = -INFINITY, reference = 0.0f, sum = 0.0f;
-
-        const int last = min(t.first + F::kRows, t.rows) - 1;
-        // this wavefront's rows, and the slots that any of them may see
-        const int my_first = min(t.first + 32 * wave, last), my_last = min(my_first + 31, last);
-        int my_end = t.hi, my_begin = t.lo;
-        if (!a.tree) {
-            my_end = min(max(t.q.kept() + my_last / a.group + 1, t.prefix), t.hi);
-            if (a.window && !t.prefix) my_begin = max(t.q.kept() + my_first / a.group - a.window + 1, t.lo);
-        }
-        if (t.first + 32 * wave > last) my_end = 0;
-        const Common whole = common(a, t, t.first, last), my_whole = common(a, t, my_first, my_last);
         const int32_t *const table = a.b.table + t.s * a.b.table_stride;
         const int begin = segments.begin, end = min(segments.stop, (t.hi + F::kKeys - 1) / F::kKeys);
         int64_t rows = 0;                                  // lane i: the first row of block base + i of sixteen keys,
@@ -215,6 +188,36 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
             }
             f.load(a, room[to], rows, block - base, wave, lane);
         };
+        if (threadIdx.x == 0) bad = 0;
+        if (begin < end) load(begin, 0);
+        // the queries and masks while the first keys are on their way
+        const int row = t.first + 32 * wave + (lane & 31), clamped = min(row, t.rows - 1);
+        const RowState state = row_state(a, t, row, head);
+        const int j = by_group(a, clamped), h = head * a.group + clamped - j * a.group;
+        const T *const in = (const T *)a.q + (int64_t)(t.q.start + j) * a.q_stride + h * a.q_head;
+        v8 q[F::kSteps];
+#pragma unroll
+        for (int s = 0; s < F::kSteps; ++s) {
+            const int d = 16 * s + 8 * half;
+            q[s] = v8{};
+            if (row < t.rows && d < a.c.D) q[s] = pwlq_block::load8<T>(in + d);
+            if (PLAIN && a.scale < 0.0f) q[s] = -q[s];
+        }
+        v16f acc[F::kColumns];
+#pragma unroll
+        for (int c = 0; c < F::kColumns; ++c) acc[c] = v16f{};
+        float top = -INFINITY, reference = 0.0f, sum = 0.0f;
+
+        const int last = min(t.first + F::kRows, t.rows) - 1;
+        // this wavefront's rows, and the slots that any of them may see
+        const int my_first = min(t.first + 32 * wave, last), my_last = min(my_first + 31, last);
+        int my_end = t.hi, my_begin = t.lo;
+        if (!a.tree) {
+            my_end = min(max(t.q.kept() + by_group(a, my_last) + 1, t.prefix), t.hi);
+            if (a.window && !t.prefix) my_begin = max(t.q.kept() + by_group(a, my_first) - a.window + 1, t.lo);
+        }
+        if (t.first + 32 * wave > last) my_end = 0;
+        const Common whole = common(a, t, t.first, last), my_whole = common(a, t, my_first, my_last);
         auto lacks_of = [&](int u) { return (uint32_t)(missing >> (u * (F::kKeys / 16) - base)) & ((1u << F::kKeys / 16) - 1); };
         // What was loaded last is in LDS for all wavefronts, and nobody reads the other buffer any more.
         auto arrive_whole = [&](int to) {
@@ -366,12 +369,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
                     if (step + 1 < 2 * F::kBlocks) v[c] = value(step + 1, c);
                 }
         };
-        if (threadIdx.x == 0) bad = 0;
         __syncthreads();
-        if (begin < end) {
-            load(begin, 0);
-            arrive(begin, 0);
-        }
+        if (begin < end) arrive(begin, 0);
         // Units that all rows see whole, as they mostly are, have a loop of their own, with nothing about masks in it.
         int u = begin, at = 0;
         auto whole_to = [&](int u) {                       // the end of such units from u on, none of which lacks a page
