@@ -214,10 +214,13 @@ void append(const pwlq_append_args &g, hipStream_t stream)
     a.interleaved = g.interleaved;
     a.positions = g.positions;
     a.frequencies = g.frequencies;
-    // Few rows: one to a workgroup, its heads shared out among workgroups so that each lane group has one head or two.
+    // Few rows: one to a workgroup, its heads shared out among workgroups so that each group of lanes has one (one row of 32 + 16 heads 3.3 us, two
+    // to a group 3.7, three 4.4).  Many: two to a workgroup and all heads, so that angles are few and workgroups enough (3795 rows 21.3 us; one row
+    // 22.6, four 24.6).
     const int all = a.q_heads + 2 * a.c.heads;
-    a.rows = a.b.T >= 1024 ? kRows : 1;
-    a.heads_each = a.rows > 1 ? all : 32;
+    a.rows = a.b.T >= 1024 ? 2 : 1;
+    const int groups = a.c.D <= 16 ? 128 : a.c.D <= 32 ? 64 : a.c.D <= 64 ? 32 : a.c.D <= 128 ? 16 : 8;
+    a.heads_each = a.rows > 1 ? all : groups;
     const dim3 grid((unsigned)((a.b.T + a.rows - 1) / a.rows), (unsigned)((all + a.heads_each - 1) / a.heads_each));
     PWLQ_TYPES(k_append, g.k.type, g.cache.type, a.c.D, <<<grid, 256, 0, stream>>>(a));
 }

@@ -332,32 +332,44 @@ template <int M, int UNIT, int THREADS> struct Segments {
 // --------------------------------------------------------------------------
 // a row's scores
 // --------------------------------------------------------------------------
-// cap tanh(x / cap) log2(e) for N products with to_cap = scale / cap, cap2 = cap log2(e).  With y = x / cap below 0.6 by a polynomial in y^2, which
-// interpolates tanh(y) / y at Chebyshev points and is off by at most 8e-8 of it; above by 1 - 2 / (exp(2y) + 1), which would lose what
-// it subtracts for small y.  Scores are mostly well below the cap: a wavefront of which all are takes 7 vector instructions for each.
-template <int N> __device__ inline void cap_scores(float (&s)[N], float to_cap, float cap2)
+// Plain ones as the product has them; sloped: less a bias that grows with the distance; capped, and sloped if there are slopes.
+enum Scores { kPlain, kSloped, kCapped };
+
+// cap tanh(y) log2(e) for N values of y = x / cap; cap2 = cap log2(e).  Below a half by a polynomial in y^2, which interpolates tanh(y) / y at
+// Chebyshev points and is off by at most 6e-7 of it; above by 1 - 2 / (exp(2y) + 1), which would lose what it subtracts for small y.  Scores are mostly
+// well below the cap: a wavefront of which all are takes 5 vector instructions for each.
+__device__ inline float cap_near(float y, float cap2)
+{
+    const float z = y * y;
+    return y * __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, -0.0443927384f * cap2, 0.131899394f * cap2), -0.333262842f * cap2), 0.999999451f * cap2);
+}
+typedef float v16f __attribute__((ext_vector_type(16)));
+// ... the rest is a function of its own, so that it takes no registers from what is not rare.
+__device__ __attribute__((noinline)) v16f cap_far(v16f y, float cap2)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float far = cap2 - 2.0f * cap2 * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y[i] * (2.0f * kLog2e)) + 1.0f);
+        y[i] = fabsf(y[i]) >= 0.5f ? far : cap_near(y[i], cap2);
+    }
+    return y;
+}
+template <int N> __device__ inline void cap_scores(float (&y)[N], float cap2)
 {
     float most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        s[i] *= to_cap;
-        most = fmaxf(most, fabsf(s[i]));
-    }
-    auto small = [&](float y) {
-        const float z = y * y;
-        return y * __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, __builtin_fmaf(z, 0.0154687513f * cap2, -0.0520966534f * cap2), 0.133100644f * cap2),
-                                                    -0.33332302f * cap2), 0.999999926f * cap2);
-    };
+    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(y[i]));
     // a NaN is no maximum: the polynomial keeps it
-    if (!__ballot(most >= 0.6f)) {
+    if (!__ballot(most >= 0.5f)) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = small(s[i]);
+        for (int i = 0; i < N; ++i) y[i] = cap_near(y[i], cap2);
     } else {
+        v16f x = {};
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float large = 1.0f - 2.0f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s[i] * (2.0f * kLog2e)) + 1.0f);
-            s[i] = fabsf(s[i]) < 0.6f ? small(s[i]) : large * cap2;
-        }
+        for (int i = 0; i < N; ++i) x[i] = y[i];
+        x = cap_far(x, cap2);
+#pragma unroll
+        for (int i = 0; i < N; ++i) y[i] = x[i];
     }
 }
 
@@ -427,7 +439,6 @@ __device__ inline Common common(const Attend &a, const Tile &t, int first, int l
 // --------------------------------------------------------------------------
 // matrix instructions, and vectors of 16-bit elements
 // --------------------------------------------------------------------------
-typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
 __device__ inline v4f mfma16(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }

@@ -110,7 +110,7 @@ template <typename T, typename C, int DP, int RB> struct Few {
     static __device__ int channel(int step, int quarter) { return kCodes ? 64 * (step / 2) + 16 * quarter + 8 * (step & 1) : 32 * step + 8 * quarter; }
 };
 
-template <typename T, typename C, int DP, int RB, bool PLAIN>
+template <typename T, typename C, int DP, int RB, Scores SCORES>
 __global__ __launch_bounds__(256, DP * RB > 128 ? 1 : 2) void k_attend_few(const Attend a)
 {
     typedef Few<T, C, DP, RB> F;
@@ -121,8 +121,7 @@ __global__ __launch_bounds__(256, DP * RB > 128 ? 1 : 2) void k_attend_few(const
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
     char *const values = room + wave * 32 * F::kStride;
     const char *const columns = values + (4 * quarter + (lane & 15) / 4) * F::kStride + (lane & 3) * 8;
-    const bool factors = F::kCodes;
-    const float to_cap = a.cap > 0.0f ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+    const float to_cap = SCORES == kCapped ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
 
     Segments<F::kRows, F::kUnit, 256> segments(a, (uint32_t *)room, tiles);
     while (segments.next(a)) {
@@ -190,11 +189,12 @@ __global__ __launch_bounds__(256, DP * RB > 128 ? 1 : 2) void k_attend_few(const
 #pragma unroll
                     for (int r = 0; r < RB; ++r) s[r][b] = mfma16(k, q[r][step], s[r][b]);
                 }
-                if (factors) {
+                if constexpr (F::kCodes) {
+                    const v4f step = f.key_step[b] * to_cap;
 #pragma unroll
                     for (int r = 0; r < RB; ++r)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) s[r][b][i] *= f.key_step[b][i];
+                        for (int i = 0; i < 4; ++i) s[r][b][i] *= step[i];
                 }
             }
             const v4f value_step[2] = {f.value_step[0], f.value_step[1]};
@@ -208,14 +208,9 @@ __global__ __launch_bounds__(256, DP * RB > 128 ? 1 : 2) void k_attend_few(const
             for (int r = 0; r < RB; ++r) {
                 float x[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = s[r][i / 4][i & 3];
-                if (!PLAIN && a.cap > 0.0f) {
-                    cap_scores(x, to_cap, cap2);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] *= to_cap;
-                }
-                if (!PLAIN && a.slopes) {
+                for (int i = 0; i < 8; ++i) x[i] = F::kCodes ? s[r][i / 4][i & 3] : s[r][i / 4][i & 3] * to_cap;
+                if constexpr (SCORES == kCapped) cap_scores(x, cap2);
+                if (SCORES != kPlain && a.slopes) {
                     const float away = (float)(state[r].own - from - 4 * quarter);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(-state[r].slope, fabsf(away - (float)(16 * (i / 4) + (i & 3))), x[i]);

@@ -8,21 +8,20 @@ namespace pwlq_attention {
 
 template <typename T, typename C> void attend_launch(const Attend &a, int D, int rows, unsigned grid, hipStream_t stream)
 {
-    // scores as the product has them, or capped or with a bias
-    const bool plain = !(a.cap > 0.0f) && !a.slopes;
-#define PWLQ_ATTEND_AS(DP, PLAIN)                                                                            \
+#define PWLQ_ATTEND_AS(DP, SCORES)                                                                           \
     do {                                                                                                     \
-        if (rows == 16) k_attend_few<T, C, DP, 1, PLAIN><<<grid, 256, 0, stream>>>(a);                       \
-        else if (rows == 128) k_attend_many<T, C, DP, PLAIN><<<grid, 256, 0, stream>>>(a);                   \
+        if (rows == 16) k_attend_few<T, C, DP, 1, SCORES><<<grid, 256, 0, stream>>>(a);                      \
+        else if (rows == 128) k_attend_many<T, C, DP, SCORES><<<grid, 256, 0, stream>>>(a);                  \
         else if constexpr (DP != 256) {                                                                      \
-            if (rows == 32) k_attend_few<T, C, DP, 2, PLAIN><<<grid, 256, 0, stream>>>(a);                   \
-            else k_attend_few<T, C, DP, 4, PLAIN><<<grid, 256, 0, stream>>>(a);                              \
+            if (rows == 32) k_attend_few<T, C, DP, 2, SCORES><<<grid, 256, 0, stream>>>(a);                  \
+            else k_attend_few<T, C, DP, 4, SCORES><<<grid, 256, 0, stream>>>(a);                             \
         }                                                                                                    \
     } while (0)
-#define PWLQ_ATTEND(DP)                            \
-    do {                                           \
-        if (plain) PWLQ_ATTEND_AS(DP, true);       \
-        else PWLQ_ATTEND_AS(DP, false);            \
+#define PWLQ_ATTEND(DP)                                       \
+    do {                                                      \
+        if (a.cap > 0.0f) PWLQ_ATTEND_AS(DP, kCapped);        \
+        else if (a.slopes) PWLQ_ATTEND_AS(DP, kSloped);       \
+        else PWLQ_ATTEND_AS(DP, kPlain);                      \
     } while (0)
     if (D == 64) PWLQ_ATTEND(64);
     else if (D == 128) PWLQ_ATTEND(128);

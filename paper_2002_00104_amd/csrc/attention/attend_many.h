@@ -5,7 +5,7 @@
 // products run beside the other's exponentials.
 //
 // Keys and values of a tile are staged in LDS, twice: one is filled while the other is worked on, a barrier a tile; 16-bit elements
-// go there from memory directly, codes are widened on the way.  As for few
+// go there from memory directly, codes too, and are widened there between two barriers.  As for few
 // rows, S^T = K Q^T leaves a lane its query row's weights in the layout of the operand of O^T = V^T P^T.
 #pragma once
 
@@ -21,9 +21,11 @@ template <typename T, typename C, int DP> struct Many {
     static constexpr int kChunks = kCodes ? DP / 16 : DP / 8;                      // of 16 bytes, of a row in memory
     static constexpr int kPass = 256 / kChunks, kLoads = kKeys / kPass, kWavePass = 64 / kChunks;
     static constexpr int kTurns = kPass % 16 ? 16 / kPass : 1;                     // loads after which rows lie in a block as at first
-    static constexpr int kAhead = kCodes ? 4 : 8;                                  // operands of keys under way; codes hold registers of their own
-    static constexpr int kRowBytes = 2 * DP, kPart = kKeys * kRowBytes;            // in LDS: keys, then values
-    static_assert(4 * kPart >= 4 * (2 * kMostTiles + 16), "LDS");
+    static constexpr int kAhead = 8;                                               // operands of keys under way
+    // In LDS, a stage: keys, then values.  16-bit elements have two; codes one, and then codes of keys and of values as they come.
+    static constexpr int kRowBytes = 2 * DP, kPart = kKeys * kRowBytes, kStage = 2 * kPart, kCodePart = kKeys * DP;
+    static constexpr int kRoom = kCodes ? kStage + 2 * kCodePart : 2 * kStage;
+    static_assert(kRoom >= 4 * (2 * kMostTiles + 16), "LDS");
     typedef typename Vec8<T>::type v8;
 
     // A row's chunks of 16 bytes in LDS are in an order of its own, so that the rows that are read together lie in different banks: for keys
@@ -31,13 +33,10 @@ template <typename T, typename C, int DP> struct Many {
     static __device__ int key_swizzle(int row) { return DP == 64 ? (row >> 1) & 7 : row & 15; }
     static __device__ int value_swizzle(int row) { return DP == 64 ? 4 * ((row >> 1) & 1) : 4 * (row & 3); }
 
-    // of codes only
-    v4u k[kCodes ? kLoads : 1], v[kCodes ? kLoads : 1];
-    float key_step[kCodes ? kLoads : 1], value_step[kCodes ? kLoads : 1];
+    float step;                                                                    // of codes: a key's or a value's, by the wavefront
 
-    // What a lane fetches of a pass's rows, in bytes from their block's first row: of keys and of values.  16-bit elements go to LDS by
-    // themselves, where a wavefront fills whole rows one after the other: the lane that fills a chunk fetches what belongs there.  Negative: nothing,
-    // past D.
+    // What a lane fetches of a pass's rows, in bytes from their block's first row: of keys and of values.  It goes to LDS by itself, where a
+    // wavefront fills whole rows one after the other: the lane that fills a chunk fetches what belongs there.  Negative: nothing, past D.
     int key_from[kTurns], value_from[kTurns];
     __device__ void prepare(const Attend &a, int wave, int lane)
     {
@@ -46,7 +45,7 @@ template <typename T, typename C, int DP> struct Many {
         for (int j = 0; j < kTurns; ++j) {
             const int row = (j * kPass + wave * kWavePass) % 16 + lane / kChunks;
             if constexpr (kCodes) {
-                key_from[j] = value_from[j] = row * D + (chunk * 16 < D ? chunk * 16 : 0);
+                key_from[j] = value_from[j] = chunk * 16 < D ? row * D + chunk * 16 : -1;
             } else {
                 const int of_key = 8 * (chunk ^ key_swizzle(row)), of_value = 8 * (chunk ^ value_swizzle(row));
                 key_from[j] = of_key < D ? 2 * (row * D + of_key) : -1;
@@ -54,39 +53,35 @@ template <typename T, typename C, int DP> struct Many {
             }
         }
     }
-    // Keys and values of a unit: 16-bit elements to LDS, codes to registers.  Its blocks are those of lane `block` on, `rows` the number of the first row of
-    // each.
+    // A unit's keys and values to LDS, codes as they are.  Its blocks are those of lane `block` on, `rows` the number of the first row of each.
     __device__ void load(const Attend &a, char *room, int64_t rows, int block, int wave, int lane)
     {
-        const int row_bytes = a.c.D * (int)sizeof(C);
+        const int64_t bytes = rows * (a.c.D * (int)sizeof(C));                     // of every lane's block, of which one is taken
+        constexpr int kLine = kCodes ? DP : kRowBytes, kValues = kCodes ? kCodePart : kPart;
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)room + (kCodes ? kStage : 0) + wave * kWavePass * kLine;
         int64_t at[kLoads];
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int r = j * kPass + wave * kWavePass;
-            const int64_t bytes = rows * row_bytes;        // of every lane's block, of which one is taken
-            at[j] = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)bytes, block + r / 16) |
-                              (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bytes >> 32), block + r / 16) << 32);
-            if constexpr (kCodes) {
-                const int64_t n = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)rows, block + r / 16) |
-                                            (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(rows >> 32), block + r / 16) << 32);
-                k[j] = load16(a.c.keys + at[j] + (uint32_t)key_from[0]);
-                v[j] = load16(a.c.values + at[j] + (uint32_t)value_from[0]);
-                key_step[j] = a.c.key_step[n + (uint32_t)(r % 16 + lane / kChunks)];
-                value_step[j] = a.c.value_step[n + (uint32_t)(r % 16 + lane / kChunks)];
+            const int from = block + (j * kPass + wave * kWavePass) / 16;
+            at[j] = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)bytes, from) |
+                              (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bytes >> 32), from) << 32);
+        }
+#pragma unroll
+        for (int turn = 0; turn < kTurns; ++turn) {
+            if (key_from[turn] >= 0) {
+#pragma unroll
+                for (int j = turn; j < kLoads; j += kTurns) to_lds(a.c.keys + at[j], (uint32_t)key_from[turn], to + j * kPass * kLine);
+            }
+            if (value_from[turn] >= 0) {
+#pragma unroll
+                for (int j = turn; j < kLoads; j += kTurns) to_lds(a.c.values + at[j], (uint32_t)value_from[turn], to + j * kPass * kLine + kValues);
             }
         }
-        if constexpr (!kCodes) {
-            const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)room + wave * kWavePass * kRowBytes;
-#pragma unroll
-            for (int turn = 0; turn < kTurns; ++turn) {
-                if (key_from[turn] >= 0) {
-#pragma unroll
-                    for (int j = turn; j < kLoads; j += kTurns) to_lds(a.c.keys + at[j], (uint32_t)key_from[turn], to + j * kPass * kRowBytes);
-                }
-                if (value_from[turn] >= 0) {
-#pragma unroll
-                    for (int j = turn; j < kLoads; j += kTurns) to_lds(a.c.values + at[j], (uint32_t)value_from[turn], to + j * kPass * kRowBytes + kPart);
-                }
+        if constexpr (kCodes) {
+            if (wave < 2 && lane < kKeys) {
+                const int of = block + lane / 16;
+                const int64_t n = (int64_t)((uint64_t)(uint32_t)__shfl((int)rows, of) | (uint64_t)(uint32_t)__shfl((int)(rows >> 32), of) << 32);
+                step = (wave ? a.c.value_step : a.c.key_step)[n + (lane & 15)];
             }
         }
     }
@@ -97,30 +92,32 @@ template <typename T, typename C, int DP> struct Many {
     {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory");
     }
-    // Codes to LDS.  `checked`: some row does not see all keys, see Few::put_values.
-    __device__ bool put(const Attend &a, char *room, float *steps, int lane, int wave, bool checked, int from, int end, uint32_t none) const
+    // The steps that load() fetched: keys' times what makes scores of products.
+    __device__ void put_steps(float *steps, float to_score, int wave, int lane) const
     {
-        const int chunk = lane % kChunks;
+        if (wave < 2 && lane < kKeys) steps[wave * kKeys + lane] = wave ? step : step * to_score;
+    }
+    // Codes that are in LDS as T in the stage.  `checked`: some row does not see all keys, see Few::put_values.
+    static __device__ bool widen_codes(const Attend &a, char *room, const float *steps, bool checked, int from, int end, uint32_t none)
+    {
         bool bad = false;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int r = j * kPass + wave * kWavePass + lane / kChunks;
-            const bool gone = checked && (from + r >= end || (none >> (r / 16) & 1));
+            const int i = j * 256 + threadIdx.x, r = i / kChunks, chunk = i % kChunks;
+            const v4u k = ((const v4u *)(room + kStage))[i], v = ((const v4u *)(room + kStage + kCodePart))[i];
+            float step = 0.0f;
+            if (kScaled && !(checked && (from + r >= end || (none >> (r / 16) & 1)))) step = steps[kKeys + r];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                *(v4u *)(room + r * kRowBytes + 16 * ((2 * chunk + h) ^ key_swizzle(r))) = words<T>(codes8<T>(k[j][2 * h], k[j][2 * h + 1]));
+                *(v4u *)(room + r * kRowBytes + 16 * ((2 * chunk + h) ^ key_swizzle(r))) = words<T>(codes8<T>(k[2 * h], k[2 * h + 1]));
                 v4u w;
                 if constexpr (kScaled) {
-                    w = words<T>(codes8<T>(v[j][2 * h], v[j][2 * h + 1], gone ? 0.0f : value_step[j]));
+                    w = words<T>(codes8<T>(v[2 * h], v[2 * h + 1], step));
                     if (checked) bad |= make_finite<T>(w) && chunk * 16 < a.c.D;
                 } else {
-                    w = words<T>(codes8<T>(v[j][2 * h], v[j][2 * h + 1]));
+                    w = words<T>(codes8<T>(v[2 * h], v[2 * h + 1]));
                 }
                 *(v4u *)(room + kPart + r * kRowBytes + 16 * ((2 * chunk + h) ^ value_swizzle(r))) = w;
-            }
-            if (chunk == 0) {
-                steps[r] = key_step[j];
-                steps[kKeys + r] = value_step[j];
             }
         }
         return __ballot(bad) != 0;
@@ -142,25 +139,25 @@ template <typename T, typename C, int DP> struct Many {
     }
 };
 
-template <typename T, typename C, int DP, bool PLAIN>
+template <typename T, typename C, int DP, Scores SCORES>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const Attend a)
 {
     typedef Many<T, C, DP> F;
     typedef typename F::v8 v8;
-    __shared__ __attribute__((aligned(16))) char room[2][2 * F::kPart];
-    __shared__ float steps[2][F::kCodes ? 2 * F::kKeys : 4];
+    __shared__ __attribute__((aligned(16))) char room[F::kRoom];
+    __shared__ float steps[2][F::kCodes ? 2 * F::kKeys : 4];   // of the unit that is worked on, and of the next
     __shared__ int bad;                                    // a value taken out
     __shared__ Tile tiles[kFewTiles];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const float to_cap = a.cap > 0.0f ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+    const float to_cap = SCORES == kCapped ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
     // Plain scores stay as the product has them until the exponential, whose addition takes the factor too.  Where the scale is negative the
     // queries change their sign; 0 times what is masked would be NaN, so the factor is next to 0 where the scale is 0.
-    const float factor = PLAIN ? fmaxf(fabsf(to_cap), 1.2e-38f) : 1.0f;
+    const float factor = SCORES == kPlain ? fmaxf(fabsf(to_cap), 1.2e-38f) : 1.0f;
 
-    Segments<F::kRows, F::kKeys, 256> segments(a, (uint32_t *)room[0], tiles);
-    if (!F::kCodes && a.c.D != DP) {
+    Segments<F::kRows, F::kKeys, 256> segments(a, (uint32_t *)room, tiles);
+    if (a.c.D != DP) {
         // channels past D, which nothing is fetched to
-        for (int i = threadIdx.x; i < 4 * F::kPart / 16; i += 256) ((v4u *)room[0])[i] = v4u{0u, 0u, 0u, 0u};
+        for (int i = threadIdx.x; i < F::kRoom / 16; i += 256) ((v4u *)room)[i] = v4u{0u, 0u, 0u, 0u};
         __syncthreads();
     }
     F f;
@@ -186,7 +183,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
                 missing = __ballot(page < 0);
                 rows = row_number(a.c, Place{max(page, 0), slot & ((1 << a.c.shift) - 1)}, head);
             }
-            f.load(a, room[to], rows, block - base, wave, lane);
+            f.load(a, room + to * F::kStage, rows, block - base, wave, lane);
         };
         if (threadIdx.x == 0) bad = 0;
         if (begin < end) load(begin, 0);
@@ -201,7 +198,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
             const int d = 16 * s + 8 * half;
             q[s] = v8{};
             if (row < t.rows && d < a.c.D) q[s] = pwlq_block::load8<T>(in + d);
-            if (PLAIN && a.scale < 0.0f) q[s] = -q[s];
+            if (SCORES == kPlain && a.scale < 0.0f) q[s] = -q[s];
         }
         v16f acc[F::kColumns];
 #pragma unroll
@@ -220,25 +217,26 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
         const Common whole = common(a, t, t.first, last), my_whole = common(a, t, my_first, my_last);
         auto lacks_of = [&](int u) { return (uint32_t)(missing >> (u * (F::kKeys / 16) - base)) & ((1u << F::kKeys / 16) - 1); };
         // What was loaded last is in LDS for all wavefronts, and nobody reads the other buffer any more.
-        auto arrive_whole = [&](int to) {
-            if constexpr (F::kCodes) f.put(a, room[to], steps[to], lane, wave, false, 0, 0, 0u);
-            else __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0)
+        auto arrive_whole = [&](int u) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);            // what was on its way to LDS: vmcnt(0)
+            if constexpr (F::kCodes) {
+                f.put_steps(steps[u & 1], SCORES == kPlain ? 1.0f : to_cap, wave, lane);
+                __syncthreads();
+                F::widen_codes(a, room, steps[u & 1], false, 0, 0, 0u);
+            }
             __syncthreads();
         };
         auto arrive = [&](int u, int to) {
             const int from = u * F::kKeys;
             const uint32_t none = lacks_of(u);
             if (none == 0 && whole.has(from, from + F::kKeys)) {
-                arrive_whole(to);
+                arrive_whole(u);
                 return;
             }
-            if constexpr (F::kCodes) {
-                if (f.put(a, room[to], steps[to], lane, wave, true, from, t.hi, none)) bad = 1;
-            } else {
-                __builtin_amdgcn_s_waitcnt(0x0f70);
-                __syncthreads();
-                if (F::check(a, room[to], from, t.hi, none)) bad = 1;
-            }
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+            if constexpr (F::kCodes) f.put_steps(steps[u & 1], SCORES == kPlain ? 1.0f : to_cap, wave, lane);
+            __syncthreads();
+            if (F::kCodes ? F::widen_codes(a, room, steps[u & 1], true, from, t.hi, none) : F::check(a, room + to * F::kStage, from, t.hi, none)) bad = 1;
             __syncthreads();
         };
         const int key_at = (lane & 31) * F::kRowBytes + 16 * (F::key_swizzle(lane & 31) ^ half);
@@ -247,11 +245,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
         // A unit's work; `masked`: some row of the wavefront's may not see all keys.
         auto work = [&](int u, int at, auto masked, uint32_t none) {
             const int from = u * F::kKeys;
-            const float *const step = steps[at];
             // operands are read from LDS some products before they are needed
-            auto key = [&](int b, int i) { return as8<T>(*(const v4u *)(room[at] + (key_at ^ 32 * i) + b * 32 * F::kRowBytes)); };
+            auto key = [&](int b, int i) { return as8<T>(*(const v4u *)(room + at * F::kStage + (key_at ^ 32 * i) + b * 32 * F::kRowBytes)); };
             auto value = [&](int step, int c) {
-                const char *const p = room[at] + (value_at ^ 64 * c) + 16 * step * F::kRowBytes;
+                const char *const p = room + at * F::kStage + (value_at ^ 64 * c) + 16 * step * F::kRowBytes;
                 return columns8<T>(p, p + 8 * F::kRowBytes);
             };
             v16f s[F::kBlocks];
@@ -275,21 +272,20 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
                 if constexpr (F::kCodes) {
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
-                        const v4f w = *(const v4f *)(step + 32 * b + 2 * i + 4 * half);
+                        const v4f w = *(const v4f *)(steps[u & 1] + 32 * b + 2 * i + 4 * half);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[b][i + e] *= w[e];
                     }
                 }
-                if constexpr (!PLAIN) {
+                if constexpr (SCORES != kPlain) {
                     float x[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = s[b][i];
-                    if (a.cap > 0.0f) {
-                        cap_scores(x, to_cap, cap2);
-                    } else {
+                    if constexpr (!F::kCodes) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) x[i] *= to_cap;
                     }
+                    if constexpr (SCORES == kCapped) cap_scores(x, cap2);
                     if (a.slopes) {
                         const float away = (float)(state.own - from - 32 * b - 4 * half);
 #pragma unroll
@@ -343,7 +339,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
                     // a row's step joins its weight: one rounding to bfloat16, of their product; a step may be NaN
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
-                        const v4f w = *(const v4f *)(step + F::kKeys + 32 * b + 2 * i + 4 * half);
+                        const v4f w = *(const v4f *)(steps[u & 1] + F::kKeys + 32 * b + 2 * i + 4 * half);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[b][i + e] *= w[e];
                     }
@@ -372,6 +368,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
         __syncthreads();
         if (begin < end) arrive(begin, 0);
         // Units that all rows see whole, as they mostly are, have a loop of their own, with nothing about masks in it.
+        constexpr int kOther = F::kCodes ? 0 : 1;          // of two stages the one that is filled
         int u = begin, at = 0;
         auto whole_to = [&](int u) {                       // the end of such units from u on, none of which lacks a page
             const int from = u * F::kKeys;
@@ -383,18 +380,18 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
             return min(stop, u + min((int)__builtin_ctzll(holes | 1ull << 63), 64 - (u * (F::kKeys / 16) - base)) / (F::kKeys / 16));
         };
         while (u < end) {
-            for (const int stop = whole_to(u) - 1; u < stop; ++u, at ^= 1) {
-                load(u + 1, at ^ 1);
+            for (const int stop = whole_to(u) - 1; u < stop; ++u, at ^= kOther) {
+                load(u + 1, at ^ kOther);
                 work(u, at, std::false_type(), 0u);
-                arrive_whole(at ^ 1);
+                arrive_whole(u + 1);
             }
             const uint32_t none = lacks_of(u);
             const int from = u * F::kKeys;
-            if (u + 1 < end) load(u + 1, at ^ 1);
+            if (u + 1 < end) load(u + 1, at ^ kOther);
             if (from < my_end && from + F::kKeys > my_begin) work(u, at, std::true_type(), none);
-            if (u + 1 < end) arrive(u + 1, at ^ 1);
+            if (u + 1 < end) arrive(u + 1, at ^ kOther);
             ++u;
-            at ^= 1;
+            at ^= kOther;
         }
 
         if (F::kMayBeBad && __builtin_amdgcn_readfirstlane(bad)) {
