@@ -39,7 +39,7 @@ struct Attend {
     int parts;                           // workgroups that the line is cut for; 0: a workgroup for each item
     int least;                           // units of a part, at least,
     int alone;                           // and where that leaves no more parts than CUs: a second workgroup there pays for longer ones
-    uint64_t *part;                      // workspace: units of a part,
+    int *part;                           // workspace: units of a part,
     struct Stretch *stretches;           // of the tiles on the line,
     float2 *top_sum;                     // m and the sum of each row of two sums for each part,
     float *sums;                         // and their values
@@ -138,22 +138,21 @@ template <int THREADS> __device__ inline uint32_t sum_before(uint32_t v, uint32_
 
 // Where a workgroup's part of the line begins: places x to end - 1, the first of them place `skip` of head `head` of tile u.
 struct Part {
-    int64_t x, end, part;
+    int x, end, part;                    // the whole line is shorter than 2^31
     int u, head, skip;
 
-    __device__ void cut(const Attend &a, uint32_t all)
+    __device__ void cut(const Attend &a, int all)
     {
-        const int64_t line = (int64_t)all * a.c.heads;
-        part = line < 1LL << 31 ? (int64_t)(((uint32_t)line + (uint32_t)a.parts - 1) / (uint32_t)a.parts) : (line + a.parts - 1) / a.parts;
-        part = max(max(part, min((line + 255) / 256, (int64_t)a.alone)), (int64_t)a.least);
-        x = (int64_t)blockIdx.x * part;
-        end = min(x + part, line);
+        const uint32_t line = (uint32_t)all * a.c.heads;
+        part = max(max((int)((line + a.parts - 1) / a.parts), min((int)((line + 255) / 256), a.alone)), a.least);
+        x = min((uint32_t)blockIdx.x * (uint32_t)part, line);
+        end = min((uint32_t)x + (uint32_t)part, line);
         u = head = skip = 0;
-        if (blockIdx.x == 0 && threadIdx.x == 0) *a.part = (uint64_t)part;
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.part = part;
     }
-    __device__ void start(const Attend &a, int tile, uint32_t begin, int length)
+    __device__ void start(const Attend &a, int tile, int begin, int length)
     {
-        const uint32_t into = (uint32_t)(x - (int64_t)begin * a.c.heads);
+        const uint32_t into = (uint32_t)(x - begin * a.c.heads);
         u = __builtin_amdgcn_readfirstlane(tile);
         head = __builtin_amdgcn_readfirstlane((int)(into / (uint32_t)length));
         skip = __builtin_amdgcn_readfirstlane((int)into) - head * length;
@@ -196,13 +195,13 @@ template <int M, int UNIT> __device__ Part plan_few(const Attend &a, Tile *tiles
         if (lane >= k) stop += o;
     }
     Part p;
-    p.cut(a, (uint32_t)__builtin_amdgcn_readlane((int)stop, 63));
+    p.cut(a, __builtin_amdgcn_readlane((int)stop, 63));
     if (blockIdx.x == 0 && threadIdx.x < a.tiles) a.stretches[lane] = Stretch(stop - length, units, t);
     if (threadIdx.x < a.tiles) tiles[lane] = t;
     if (p.x < p.end) {
-        const int at = __builtin_ctzll(__ballot((int64_t)stop * a.c.heads > p.x));
+        const int at = __builtin_ctzll(__ballot((int)stop * a.c.heads > p.x));
         const int n = __builtin_amdgcn_readlane(length, at);
-        p.start(a, at, (uint32_t)(__builtin_amdgcn_readlane((int)stop, at) - n), n);
+        p.start(a, at, __builtin_amdgcn_readlane((int)stop, at) - n, n);
     }
     __syncthreads();
     return p;
@@ -248,15 +247,15 @@ template <int M, int UNIT, int THREADS> __device__ Part plan(const Attend &a, ui
     if (threadIdx.x == 0) begin[a.tiles] = all;
     __syncthreads();
     Part p;
-    p.cut(a, all);
+    p.cut(a, (int)all);
     if (p.x < p.end) {
         int lo = 0, hi = a.tiles;
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
-            if ((int64_t)begin[mid] * a.c.heads <= p.x) lo = mid;
+            if ((int)begin[mid] * a.c.heads <= p.x) lo = mid;
             else hi = mid;
         }
-        p.start(a, lo, begin[lo], (int)(begin[lo + 1] - begin[lo]));
+        p.start(a, lo, (int)begin[lo], (int)(begin[lo + 1] - begin[lo]));
     }
     __syncthreads();
     return p;
@@ -307,14 +306,14 @@ template <int M, int UNIT, int THREADS> struct Segments {
                 units = units_of(t, UNIT);
                 if (units == 0) ++p.u;
             }
-            const int n = (int)min((int64_t)(units + kSetup - p.skip), p.end - p.x);
+            const int n = min(units + kSetup - p.skip, p.end - p.x);
             if (n <= 0) return false;                       // starts that do not rise: the line does not fit them
             const int from = max(p.skip - kSetup, 0), to = max(p.skip + n - kSetup, 0);
             head = p.head;
             begin = t.lo / UNIT + from;
             stop = t.lo / UNIT + to;
             // its sums are the first of the part if the item began before the part or with it
-            sums = from == 0 && to == units ? -1 : 2 * (int)blockIdx.x + (p.x - p.skip > (int64_t)blockIdx.x * p.part);
+            sums = from == 0 && to == units ? -1 : 2 * (int)blockIdx.x + (p.x - p.skip > (int)blockIdx.x * p.part);
             p.x += n;
             p.skip = 0;
             const bool any = to > from;

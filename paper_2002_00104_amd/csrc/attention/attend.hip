@@ -21,9 +21,9 @@ template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void k
     __shared__ float2 tops[kGroups];
     const Stretch t = a.stretches[blockIdx.x];
     // the parts with its first unit and its last
-    const int64_t part = (int64_t)*a.part, n = t.units + kSetup, x = (int64_t)t.begin * a.c.heads + blockIdx.y * n;
+    const int part = *a.part, n = t.units + kSetup, x = t.begin * a.c.heads + blockIdx.y * n;
     if (t.units == 0 || t.first + (int)blockIdx.z * ROWS >= t.rows) return;
-    const int64_t first = (x + kSetup) / part, last = (x + n - 1) / part;
+    const int first = (uint32_t)(x + kSetup) / (uint32_t)part, last = (uint32_t)(x + n - 1) / (uint32_t)part;
     if (first == last) return;
     const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes, turn = group % kEach, d = 4 * lane;
 #pragma unroll
@@ -41,8 +41,8 @@ template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void k
         };
         if (row < t.rows) {
 #pragma unroll 4
-            for (int64_t w = first + turn; w <= last; w += kEach) {
-                const int64_t at = (2 * w + (x > w * part)) * rows + of;
+            for (int w = first + turn; w <= last; w += kEach) {
+                const int64_t at = (int64_t)(2 * w + (x > w * part)) * rows + of;
                 add(a.top_sum[at], *(const v4f *)(a.sums + at * DP + d));
             }
         }
@@ -67,8 +67,10 @@ Shape shape_of(const pwlq_attend_args &g)
     Shape s = {};
     const int64_t group = g.q_heads / g.cache.heads, longest = !g.batch.starts ? 1 : g.longest ? g.longest : g.batch.T;
     s.channels = g.cache.D <= 64 ? 64 : g.cache.D <= 128 ? 128 : 256;
-    const int64_t rows = longest * group, most_few = s.channels == 256 ? 16 : 64;
-    s.rows = rows > most_few ? 128 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    // A tile for all rows of a sequence, so that its keys are read once.  16 sequences of 4000 rows, trees of 20 rows, in tiles of 16, 32 and 128:
+    // 93, 62 and 64 us, 57, 53 and 67 with an 8-bit cache; of 48 rows 130, 67 and 69, 77, 76 and 73.
+    const int64_t rows = longest * group;
+    s.rows = rows <= 16 ? 16 : rows <= 32 && s.channels != 256 ? 32 : 128;
     s.unit = s.rows < 128 ? 128 : s.channels == 256 ? 32 : 64;
     s.each = (int)((group + s.rows - 1) / s.rows);
     const int64_t tiles = g.batch.starts ? g.batch.T * group / s.rows + g.batch.S : g.batch.S * s.each;
@@ -76,10 +78,10 @@ Shape shape_of(const pwlq_attend_args &g)
     s.least = s.rows < 128 ? 1 : 4;
     const int64_t units = (g.batch.table_pages * g.cache.page + s.unit - 1) / s.unit, items = tiles * g.cache.heads;
     const bool enough = s.rows == 128 && items >= 1024;
-    if (tiles <= kMostTiles && g.batch.S <= kMostTiles && tiles * (units + kSetup + 1) < 1LL << 31 && !enough) {
+    if (tiles <= kMostTiles && g.batch.S <= kMostTiles && items * (units + kSetup + 1) < 1LL << 30 && !enough) {
         const int64_t all = items * ((units > 1 ? units : 1) + kSetup);
         const int64_t parts = (all + s.least - 1) / s.least;
-        const int most = s.rows < 128 ? (s.rows * s.channels > 2048 ? 256 : 512) : s.channels == 256 ? 256 : 512;    // what the chip holds at once
+        const int most = s.channels == 256 || (s.rows == 32 && s.channels == 128) ? 256 : 512;    // what the chip holds at once
         s.parts = (int)(parts < most ? parts : most);
     }
     auto place = [&](size_t bytes) {
@@ -125,7 +127,7 @@ void attend(const pwlq_attend_args &g, void *workspace, hipStream_t stream)
     a.least = s.least;
     a.alone = s.rows < 128 ? 1 : 8;
     char *const w = (char *)workspace;
-    a.part = (uint64_t *)(w + s.part);
+    a.part = (int *)(w + s.part);
     a.stretches = (Stretch *)(w + s.stretches);
     a.top_sum = (float2 *)(w + s.top_sum);
     a.sums = (float *)(w + s.sums);

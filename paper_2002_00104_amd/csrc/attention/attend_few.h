@@ -1,4 +1,4 @@
-// k_attend_few: tiles of 16 to 64 query rows, for single tokens and trees.
+// k_attend_few: tiles of 16 or 32 query rows, for single tokens and small trees.
 //
 // Bound by memory: keys and values are read once, with matrix instructions as good as idle (16 rows against 32 keys of 128
 // channels take 256 of their cycles for 16 KiB).  Each of the four wavefronts takes 32 keys of a unit of 128 by itself, with

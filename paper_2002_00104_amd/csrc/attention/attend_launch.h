@@ -11,11 +11,8 @@ template <typename T, typename C> void attend_launch(const Attend &a, int D, int
 #define PWLQ_ATTEND_AS(DP, SCORES)                                                                           \
     do {                                                                                                     \
         if (rows == 16) k_attend_few<T, C, DP, 1, SCORES><<<grid, 256, 0, stream>>>(a);                      \
-        else if (rows == 128) k_attend_many<T, C, DP, SCORES><<<grid, 256, 0, stream>>>(a);                  \
-        else if constexpr (DP != 256) {                                                                      \
-            if (rows == 32) k_attend_few<T, C, DP, 2, SCORES><<<grid, 256, 0, stream>>>(a);                  \
-            else k_attend_few<T, C, DP, 4, SCORES><<<grid, 256, 0, stream>>>(a);                             \
-        }                                                                                                    \
+        else if (DP == 256 || rows == 128) k_attend_many<T, C, DP, SCORES><<<grid, 256, 0, stream>>>(a);     \
+        else if constexpr (DP != 256) k_attend_few<T, C, DP, 2, SCORES><<<grid, 256, 0, stream>>>(a);        \
     } while (0)
 #define PWLQ_ATTEND(DP)                                       \
     do {                                                      \
