@@ -8,11 +8,14 @@ namespace pwlq_attention {
 
 template <typename T, typename C> void attend_launch(const Attend &a, int D, int rows, unsigned grid, hipStream_t stream)
 {
-#define PWLQ_ATTEND_AS(DP, SCORES)                                                                           \
-    do {                                                                                                     \
-        if (rows == 16) k_attend_few<T, C, DP, 1, SCORES><<<grid, 256, 0, stream>>>(a);                      \
-        else if (DP == 256 || rows == 128) k_attend_many<T, C, DP, SCORES><<<grid, 256, 0, stream>>>(a);     \
-        else if constexpr (DP != 256) k_attend_few<T, C, DP, 2, SCORES><<<grid, 256, 0, stream>>>(a);        \
+    // tiles of 128 rows multiply three quarters of the channels where the others are none
+#define PWLQ_ATTEND_AS(DP, SCORES)                                                                                             \
+    do {                                                                                                                       \
+        if (rows == 16) k_attend_few<T, C, DP, 1, SCORES><<<grid, 256, 0, stream>>>(a);                                        \
+        else if (DP == 256 || rows == 128) {                                                                                   \
+            if (DP != 64 && a.c.D <= DP * 3 / 4) k_attend_many<T, C, DP, DP == 64 ? DP : DP * 3 / 4, SCORES><<<grid, 256, 0, stream>>>(a); \
+            else k_attend_many<T, C, DP, DP, SCORES><<<grid, 256, 0, stream>>>(a);                                             \
+        } else if constexpr (DP != 256) k_attend_few<T, C, DP, 2, SCORES><<<grid, 256, 0, stream>>>(a);                        \
     } while (0)
 #define PWLQ_ATTEND(DP)                                       \
     do {                                                      \

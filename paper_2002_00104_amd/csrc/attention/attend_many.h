@@ -13,11 +13,12 @@
 
 namespace pwlq_attention {
 
-template <typename T, typename C, int DP> struct Many {
+// DP: channels that a row in LDS has room for, DC: those that are multiplied, no fewer than D.
+template <typename T, typename C, int DP, int DC> struct Many {
     static constexpr bool kCodes = sizeof(C) == 1, kScaled = kCodes && __is_same(T, f16);    // values scaled as they are read
     static constexpr bool kMayBeBad = !kCodes || kScaled;                          // values that are not finite
     static constexpr int kRows = 128, kKeys = DP == 256 ? 32 : 64;                 // of a unit; a wavefront has 32 rows
-    static constexpr int kSteps = DP / 16, kColumns = DP / 32, kBlocks = kKeys / 32;
+    static constexpr int kSteps = DC / 16, kColumns = DC / 32, kBlocks = kKeys / 32;
     static constexpr int kChunks = kCodes ? DP / 16 : DP / 8;                      // of 16 bytes, of a row in memory
     static constexpr int kPass = 256 / kChunks, kLoads = kKeys / kPass, kWavePass = 64 / kChunks;
     static constexpr int kTurns = kPass % 16 ? 16 / kPass : 1;                     // loads after which rows lie in a block as at first
@@ -139,10 +140,10 @@ template <typename T, typename C, int DP> struct Many {
     }
 };
 
-template <typename T, typename C, int DP, Scores SCORES>
+template <typename T, typename C, int DP, int DC, Scores SCORES>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const Attend a)
 {
-    typedef Many<T, C, DP> F;
+    typedef Many<T, C, DP, DC> F;
     typedef typename F::v8 v8;
     __shared__ __attribute__((aligned(16))) char room[F::kRoom];
     __shared__ float steps[2][F::kCodes ? 2 * F::kKeys : 4];   // of the unit that is worked on, and of the next
