@@ -142,6 +142,7 @@ struct Read {
     Batch b;
     char *k, *v;
     int64_t k_stride, k_head, v_stride, v_head;
+    int rows;                                              // of the call a workgroup takes
 };
 
 template <typename T, typename C, int LANES>
@@ -149,11 +150,13 @@ __global__ __launch_bounds__(256) void k_read(Read a)
 {
     __shared__ Row rows[kRows];
     const int wave = threadIdx.x >> 6, D = a.c.D, lane = threadIdx.x % LANES, d = 8 * lane;
-    int slot;
-    const Row r = row_of(a.c, a.b, blockIdx.x * kRows + wave, slot);
-    if ((threadIdx.x & 63) == 0) rows[wave] = r;
+    if (wave < a.rows) {
+        int slot;
+        const Row r = row_of(a.c, a.b, blockIdx.x * a.rows + wave, slot);
+        if ((threadIdx.x & 63) == 0) rows[wave] = r;
+    }
     __syncthreads();
-    for (int i = threadIdx.x / LANES; i < kRows * 2 * a.c.heads; i += 256 / LANES) {
+    for (int i = threadIdx.x / LANES; i < a.rows * 2 * a.c.heads; i += 256 / LANES) {
         const int of = i / (2 * a.c.heads), h = i - of * 2 * a.c.heads;
         const Row row = rows[of];
         const bool key = h < a.c.heads;
@@ -228,8 +231,8 @@ void append(const pwlq_append_args &g, hipStream_t stream)
 void read(const pwlq_read_args &g, hipStream_t stream)
 {
     Read a = {cache_of(g.cache), batch_of(g.batch, g.cache), (char *)g.k.data, (char *)g.v.data,
-              g.k.stride, g.k.head_stride, g.v.stride, g.v.head_stride};
-    const unsigned grid = (unsigned)((a.b.T + kRows - 1) / kRows);
+              g.k.stride, g.k.head_stride, g.v.stride, g.v.head_stride, g.batch.T >= 1024 ? kRows : 1};
+    const unsigned grid = (unsigned)((a.b.T + a.rows - 1) / a.rows);
     PWLQ_TYPES(k_read, g.k.data ? g.k.type : g.v.type, g.cache.type, a.c.D, <<<grid, 256, 0, stream>>>(a));
 }
 

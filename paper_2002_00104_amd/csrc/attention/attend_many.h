@@ -380,10 +380,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
             // as far as the pages are known that are there
             return min(stop, u + min((int)__builtin_ctzll(holes | 1ull << 63), 64 - (u * (F::kKeys / 16) - base)) / (F::kKeys / 16));
         };
+        const bool mine = t.first + 32 * wave <= last;
         while (u < end) {
             for (const int stop = whole_to(u) - 1; u < stop; ++u, at ^= kOther) {
                 load(u + 1, at ^ kOther);
-                work(u, at, std::false_type(), 0u);
+                if (mine) work(u, at, std::false_type(), 0u);
                 arrive_whole(u + 1);
             }
             const uint32_t none = lacks_of(u);

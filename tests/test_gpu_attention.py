@@ -88,7 +88,7 @@ HEADS = [(1, 1), (8, 2), (5, 5), (12, 1), (20, 1), (33, 3)]
 @pytest.mark.parametrize("packed", [False, True], ids=["16 bits", "8 bits"])
 @pytest.mark.parametrize("dtype", [BF16, F16], ids=["bf16", "f16"])
 @pytest.mark.parametrize("sizes", sorted(SIZES))
-@pytest.mark.parametrize("D", [16, 64, 80, 128, 240, 256])
+@pytest.mark.parametrize("D", [16, 64, 80, 96, 112, 128, 160, 192, 240, 256])
 def test_attend(A, sizes, D, dtype, packed):
     H, G = HEADS[zlib.crc32(repr((sizes, D)).encode()) % len(HEADS)]
     print(f"[case] attend {sizes} D={D} H={H} G={G} {dtype} {packed}", flush=True)
@@ -187,7 +187,7 @@ def test_tree_of_a_chain_is_a_prompt(A):
 
 @pytest.mark.parametrize("dtype,packed", [(BF16, False), (F16, False), (BF16, True), (F16, True)])
 @pytest.mark.parametrize("longest", [1, 8, 1000])
-@pytest.mark.parametrize("D", [80, 128, 256])
+@pytest.mark.parametrize("D", [48, 80, 128, 192, 256])
 def test_not_finite(A, dtype, packed, longest, D):
     """Infinities and NaN in keys and values reach the rows that see them, and no others."""
     g = gen("not finite", D)
