@@ -91,7 +91,11 @@ template <typename T, typename C, int DP, int DC> struct Many {
     // compiler allots to nothing and sets itself before each use of its own (here it has none).
     static __device__ void to_lds(const char *from, uint32_t offset, uint32_t to)
     {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory");
+        // the same in all lanes, said so for what is compiled with less analysis
+        const uint32_t place = __builtin_amdgcn_readfirstlane((int)to);
+        const uint64_t address = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint64_t)from) |
+                                 (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)from >> 32)) << 32;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(place), "v"(offset), "s"(address) : "memory");
     }
     // The steps that load() fetched: keys' times what makes scores of products.
     __device__ void put_steps(float *steps, float to_score, int wave, int lane) const
@@ -215,7 +219,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
             if (a.window && !t.prefix) my_begin = max(t.q.kept() + by_group(a, my_first) - a.window + 1, t.lo);
         }
         if (t.first + 32 * wave > last) my_end = 0;
-        const Common whole = common(a, t, t.first, last), my_whole = common(a, t, my_first, my_last);
+        const Common whole = common(a, t, t.first, last);
         auto lacks_of = [&](int u) { return (uint32_t)(missing >> (u * (F::kKeys / 16) - base)) & ((1u << F::kKeys / 16) - 1); };
         // What was loaded last is in LDS for all wavefronts, and nobody reads the other buffer any more.
         auto arrive_whole = [&](int u) {

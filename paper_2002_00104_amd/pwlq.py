@@ -33,6 +33,7 @@ EXPORTS = (
     "pwlq_pack_rows", "pwlq_unpack_rows", "pwlq_norm_block", "pwlq_norm_block_backward_workspace_bytes",
     "pwlq_norm_block_backward", "pwlq_adapter_workspace_bytes", "pwlq_adapter",
     "pwlq_adapter_backward_workspace_bytes", "pwlq_adapter_backward",
+    "pwlq_append", "pwlq_read", "pwlq_attend_workspace_bytes", "pwlq_attend",
     "pwlq_last_error", "pwlq_last_search_shape", "pwlq_profile_enable",
     "pwlq_profile_last_ms", "pwlq_profile_ms", "pwlq_kernel_name", "pwlq_last_search_kernel",
     "pwlq_last_kernels",
@@ -115,6 +116,8 @@ def _load() -> ctypes.CDLL:
     lib.pwlq_adapter_workspace_bytes.argtypes = [i64, i64, ci]
     lib.pwlq_adapter_backward_workspace_bytes.restype = sz
     lib.pwlq_adapter_backward_workspace_bytes.argtypes = [i64, i64, i64, ci, ci]
+    lib.pwlq_attend_workspace_bytes.restype = sz
+    lib.pwlq_attend_workspace_bytes.argtypes = [vp]
     lib.pwlq_last_error.restype = ctypes.c_char_p
     lib.pwlq_last_error.argtypes = []
     lib.pwlq_last_search_shape.restype = None
