@@ -15,7 +15,7 @@
  *   - A batch is S sequences.  Sequence s holds lengths[s] rows, those of this
  *     call included; its row `slot` is row slot % page of page
  *     table[s * table_stride + slot / page].  Lengths beyond table_pages * page
- *     (which is below 2^31) count as that.  Entries that no row needs are not
+ *     (which is at most 2^30) count as that.  Entries that no row needs are not
  *     read.  Rows on a page outside [0, pages) do not exist: nothing is written
  *     there, they read as zeros, and attention does not see them.  Sequences may
  *     share pages that no row of the call is written to.

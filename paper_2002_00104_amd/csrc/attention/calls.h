@@ -7,6 +7,7 @@ namespace {
 
 constexpr int64_t kMostCalled = 1LL << 20;     // rows, sequences
 constexpr int kMostHeads = 1024;
+constexpr int64_t kMostSlots = 1LL << 30;      // of a sequence: sums of slots, tiles and windows stay within 32 bits
 
 int check_cache(const pwlq_cache &c)
 {
@@ -22,7 +23,7 @@ int check_batch(const pwlq_batch &b, const pwlq_cache &c)
     if (b.T < 0 || b.T > kMostCalled) return fail(PWLQ_EINVAL, "T=%lld outside [0,%lld]", (long long)b.T, (long long)kMostCalled);
     if (b.S < 0 || b.S > kMostCalled) return fail(PWLQ_EINVAL, "S=%lld outside [0,%lld]", (long long)b.S, (long long)kMostCalled);
     if (!b.starts && b.T != b.S) return fail(PWLQ_EINVAL, "without starts T=%lld is not S=%lld", (long long)b.T, (long long)b.S);
-    if (b.table_pages < 0 || b.table_pages > INT32_MAX / c.page) return fail(PWLQ_EINVAL, "table_pages=%lld: a sequence of 2^31 rows or more", (long long)b.table_pages);
+    if (b.table_pages < 0 || b.table_pages > kMostSlots / c.page) return fail(PWLQ_EINVAL, "table_pages=%lld: a sequence of more than 2^30 rows", (long long)b.table_pages);
     return PWLQ_OK;
 }
 // What is read of both once there are rows.

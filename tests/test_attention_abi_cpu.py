@@ -79,6 +79,11 @@ def shared_refusals(call):
                 dict(table_pages=-1), dict(table_pages=1 << 25), dict(table_stride=31), dict(table=FAKE + 2), dict(lengths=FAKE + 1),
                 dict(starts=FAKE + 2)):
         assert call(batch=batch(**bad)) == EINVAL, bad
+    # a sequence has room for 2^30 rows at most: one page more is refused, before anything else is looked at
+    for page in (16, 64, 65536):
+        most = (1 << 30) // page
+        assert call(cache=cache(page=page), batch=batch(S=0, T=0, table_pages=most)) == 0
+        assert call(cache=cache(page=page), batch=batch(S=0, T=0, table_pages=most + 1)) == EINVAL
     assert call(batch=batch(S=0, T=0, table=None, lengths=None), cache=cache(keys=None)) == 0
     assert call(batch=batch(S=0, T=4, starts=FAKE)) == 0 and call(batch=batch(S=4, T=0, starts=FAKE)) == 0
 
