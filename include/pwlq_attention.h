@@ -101,8 +101,8 @@ int pwlq_read(const pwlq_read_args *args, void *stream);
 /*
  * Attention of q [T, q_heads, D] over the cache; head h reads head
  * h / (q_heads / heads) of the cache.  For a row at `own` and a key at `slot`:
- *     s   = scale * (q . k)
- *     s   = cap * tanh(s / cap)                        where cap > 0
+ *     s   = scale * (q . k)                            |scale| at most 2^60
+ *     s   = cap * tanh(s / cap)                        unless cap is 0; 2^-60 to 2^60
  *     s   = s - slopes[h] * |own - slot|               where slopes are given
  *     out = sum_slot softmax(s)[slot] v[slot]          over the slots it sees
  * A row sees slot < lengths[s], if

@@ -125,7 +125,10 @@ size_t pwlq_attend_workspace_bytes(const pwlq_attend_args *a)
 int pwlq_attend(const pwlq_attend_args *a, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (int rc = check_attend(a)) return rc;
-    if (!(a->cap >= 0.0f) || a->cap > 3.0e38f) return fail(PWLQ_EINVAL, "cap=%g is not a number from 0 on", (double)a->cap);
+    // beyond these the factors that the kernels make of them are no numbers of binary32
+    constexpr float most = (float)(1LL << 60);
+    if (!(a->scale >= -most && a->scale <= most)) return fail(PWLQ_EINVAL, "scale=%g outside [-2^60,2^60]", (double)a->scale);
+    if (a->cap != 0.0f && !(a->cap >= 1.0f / most && a->cap <= most)) return fail(PWLQ_EINVAL, "cap=%g is neither 0 nor within [2^-60,2^60]", (double)a->cap);
     if (a->window < 0) return fail(PWLQ_EINVAL, "window=%lld is negative", (long long)a->window);
     if (a->tree && (a->slopes || a->window || a->prefix)) return fail(PWLQ_EINVAL, "a tree goes without slopes, window and prefix");
     if (a->tree && (a->tree_words < 1 || a->tree_words > kMostCalled / 64))

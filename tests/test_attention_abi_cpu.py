@@ -159,6 +159,11 @@ def test_attend(calls):
                 dict(tree=FAKE, tree_words=1, window=5), dict(tree=FAKE, tree_words=1, slopes=FAKE), dict(tree=FAKE, tree_words=1, prefix=FAKE),
                 dict(tree=FAKE + 4, tree_words=1)):
         assert call(**bad) == EINVAL, bad
+    for bad in (dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-2.0 ** 61), dict(cap=2.0 ** -61), dict(cap=1e-44), dict(cap=2.0 ** 61),
+                dict(cap=2.9e38)):
+        assert call(**bad) == EINVAL, bad
+    for good in (dict(scale=2.0 ** 60), dict(scale=-2.0 ** 60), dict(cap=2.0 ** -60), dict(cap=2.0 ** 60)):
+        assert call(workspace=None, **good) == EWORKSPACE, good
     assert call(workspace=None) == EWORKSPACE and call(workspace=FAKE + 128) == EWORKSPACE and call(room=1000) == EWORKSPACE
     assert need() > 0 and need(batch=batch(S=0, T=0)) == 0 and need(q_heads=12) == 0 and need(cache=cache(D=8)) == 0
     # no parts, and so no workspace, where the items fill the chip by themselves
