@@ -85,7 +85,9 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n)
     PyObject *const *const m = a + kShared;
     const Tensor &k = needed("k", m[0]), &v = needed("v", m[1]), *q = tensor("q", m[2]), *out = tensor("out", m[6]);
     const Call c("keys", needed("keys", a[0]), 4);
-    untracked(nullptr, {{"k", &k}, {"v", &v}, {"q", q}});
+    untracked(nullptr, {{"keys", tensor("keys", a[0])}, {"values", tensor("values", a[1])}, {"key_step", tensor("key_step", a[2])},
+                        {"value_step", tensor("value_step", a[3])}, {"k", &k}, {"v", &v}, {"q", q},
+                        {"frequencies", tensor("frequencies", m[4])}, {"out", out}});
     if (k.dim() != 3 || !is_half(k.scalar_type())) refuse("k must be [rows, heads, D] of bfloat16 or float16");
     const ScalarType type = k.scalar_type();
     const int64_t T = k.size(0);
@@ -126,6 +128,8 @@ PyObject *read(PyObject *, PyObject *const *a, Py_ssize_t n)
     PyObject *const *const m = a + kShared;
     const Tensor &keys = needed("keys", a[0]), *k = tensor("k", m[2]), *v = tensor("v", m[3]);
     const Call c("keys", keys, 4);
+    untracked(nullptr, {{"keys", &keys}, {"values", tensor("values", a[1])}, {"key_step", tensor("key_step", a[2])},
+                        {"value_step", tensor("value_step", a[3])}, {"k", k}, {"v", v}});
     pwlq_read_args args = {};
     const int64_t rows = m[0] == Py_None ? -1 : integer(m[0]);
     if (m[0] != Py_None && rows < 0) refuse("rows is negative");
@@ -152,7 +156,8 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n)
     PyObject *const *const m = a + kShared;
     const Tensor &q = needed("q", m[0]), *given = tensor("out", m[8]), *slopes = tensor("slopes", m[4]), *tree = tensor("tree", m[7]);
     const Call c("keys", needed("keys", a[0]), 4);
-    untracked(nullptr, {{"q", &q}, {"slopes", slopes}, {"out", given}});
+    untracked(nullptr, {{"keys", tensor("keys", a[0])}, {"values", tensor("values", a[1])}, {"key_step", tensor("key_step", a[2])},
+                        {"value_step", tensor("value_step", a[3])}, {"q", &q}, {"slopes", slopes}, {"out", given}});
     if (q.dim() != 3 || !is_half(q.scalar_type()) || q.size(1) > INT32_MAX) refuse("q must be [rows, heads, D] of bfloat16 or float16");
     const ScalarType type = q.scalar_type();
     const int64_t T = q.size(0), H = q.size(1);
