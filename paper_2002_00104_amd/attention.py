@@ -11,7 +11,7 @@ A block that decodes, with the projections and norms of `block` around it:
 
 A batch is S sequences: table int32 [S, n], the pages of each; lengths int32 [S], their rows with those of the call; starts int32
 [S + 1], the first of the call's rows of each and their end, or None for one row each.  The call's rows are the last ones of
-their sequences.
+their sequences; rows from starts[S] on belong to none, and an output has there what it had (nothing in particular where a call makes it).
 
 Argument marshalling only: the work is the library's, on the current stream of the current device, where all tensors are.
 Autograd sees none of it: tensors that require gradients are refused unless a call is made under torch.no_grad().
@@ -80,5 +80,6 @@ def attend(q: Tensor, cache: Cache, table: Tensor, lengths: Tensor, *, starts: O
     A row sees its sequence up to itself, the last `window` rows of that if it is not 0, and the first prefix[s] rows (int32 [S])
     in any case.  With tree, int64 [T, words], it sees what the sequence held before the call, and of the call's rows of its
     sequence those whose bit is set: row j's is bit j % 64 of word j // 64.  A row that sees nothing is zeros.  longest: the most
-    rows of a sequence, where known; it chooses the kernel.  Returns [T, H, D] of q's type."""
+    rows of a sequence, where known; it chooses the kernel.  workspace: bytes for calls that take turns on one stream, else one is made; it
+    holds up to 69 MB, by the sizes.  Returns [T, H, D] of q's type."""
     return _pwlq_attention.attend(*cache, table, lengths, starts, q, longest, scale, cap, slopes, window, prefix, tree, out, workspace, _stream())
