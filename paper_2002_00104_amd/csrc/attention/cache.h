@@ -61,7 +61,7 @@ template <typename F> __device__ inline int find_rising(int S, int x, F at)
     while (n > 1) {
         const int step = (n + 63) / 64, i = (int)(threadIdx.x & 63) * step;
         const uint64_t below = __ballot(i < n && at(lo + min(i, n - 1)) <= x);
-        const int k = max(__popcll(below) - 1, 0);
+        const int k = max((int)__popcll(below) - 1, 0);     // it is unsigned: no place is no place before the first
         lo += k * step;
         n = min(step, n - k * step);
     }

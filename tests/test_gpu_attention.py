@@ -67,6 +67,9 @@ def run_attend(A, q, batch, cache, *, how="whole", starts=True, name="", **kw):
     kw.pop("longest", None)
     want, slack = ref.attend(q, batch, cache, scale, **kw)
     ref.check(name, got, want, slack)
+    # the same with a table that has room for more, for which keys are cut into parts
+    roomy = torch.nn.functional.pad(batch.table, (0, 20000 // batch.page + 1), value=2 ** 31 - 1).cuda()
+    ref.check(name + " roomy", A.attend(spread(q, how), on_gpu(A, cache), roomy, batch.lengths.cuda(), scale=scale, **put), want, slack)
     return got
 
 
@@ -262,7 +265,37 @@ def test_odd_starts_and_lengths(A):
         for longest in (1, 8, 1000):
             A.attend(q, cache, batch.table.cuda(), torch.tensor(lengths, dtype=torch.int32).cuda(),
                      starts=torch.tensor(starts, dtype=torch.int32).cuda(), longest=longest)
-    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("S,T", [(3, 12), (70, 200), (2100, 2500)])
+def test_rows_before_the_first_sequence(A, S, T):
+    """Starts that begin behind the first rows, fall, or are any numbers: what lies before a sequence's first row belongs to none."""
+    g = gen("no first", S)
+    batch = ref.Batch(g, [(1, 40)] * S, 16)
+    kept = make_cache(g, batch, 2, 64, BF16, False)
+    cache, table, lengths = on_gpu(A, kept), batch.table.cuda(), batch.lengths.cuda()
+    q, k = normal(g, T, 4, 64, dtype=BF16), normal(g, T, 2, 64, dtype=BF16)
+    for first in (1, 5, T, 2 ** 31 - 1):
+        starts = torch.full((S + 1,), first, dtype=torch.int32)
+        starts[-1] = max(first, T)                          # the last sequence has all rows from `first` on
+        for longest in (1, 8, 1000):
+            out = torch.full_like(q, 7.0).cuda()
+            A.attend(q.cuda(), cache, table, lengths, starts=starts.cuda(), longest=longest, out=out)
+            assert (out[:first] == 7.0).all()
+        to = tuple(torch.full_like(k, 7.0).cuda() for _ in range(2))
+        A.read(cache, table, lengths, starts=starts.cuda(), rows=T, out=to)
+        assert all((t[:first] == 7.0).all() for t in to)
+        turned = torch.full_like(q, 7.0).cuda()
+        A.append(cache, table, lengths, k.cuda(), k.cuda(), q.cuda(), starts=starts.cuda(), out=turned)
+        assert (turned[:first] == 7.0).all() and torch.equal(turned[first:].cpu(), q[first:])
+    for i in range(4):
+        starts = torch.randint(-5, T + 5, (S + 1,), generator=g, dtype=torch.int32) if i < 3 else torch.arange(S, -1, -1, dtype=torch.int32)
+        for longest in (1, 8, 1000):
+            A.attend(q.cuda(), cache, table, lengths, starts=starts.cuda(), longest=longest)
+        A.read(cache, table, lengths, starts=starts.cuda(), rows=T)
+        A.append(cache, table, lengths, k.cuda(), k.cuda(), q.cuda(), starts=starts.cuda())
+        torch.cuda.synchronize()
 
 
 @pytest.mark.parametrize("longest", [1, 8, 1000])
@@ -646,7 +679,7 @@ def test_refusals(A):
                  lambda: A.attend(q, cache, table, lengths, window=-1), lambda: A.attend(q[:1], cache, table, lengths),
                  lambda: A.attend(normal(g, 2, 3, 64, dtype=BF16).cuda(), cache, table, lengths),
                  lambda: A.attend(q, cache, table, lengths, window=3, tree=torch.ones(2, 1, dtype=torch.long, device="cuda")),
-                 lambda: A.attend(q, cache, table, lengths, workspace=torch.empty(256, dtype=torch.uint8, device="cuda")),
+                 lambda: A.attend(q, cache, torch.nn.functional.pad(table, (0, 300)), lengths, workspace=torch.empty(256, dtype=torch.uint8, device="cuda")),
                  lambda: A.append(cache, table, lengths, k, k, frequencies=torch.ones(12, device="cuda")),
                  lambda: A.append(cache, table, lengths, k, k, normal(g, 2, 3, 64, dtype=BF16).cuda()),
                  lambda: A.read(cache, table, lengths, rows=1)):
