@@ -115,7 +115,7 @@ int pwlq_read(const pwlq_read_args *args, void *stream);
  * longest: the most rows of a sequence, as far as the caller knows (0: T); it
  * decides which kernel runs and nothing else.
  * Workspace: device, 256-byte aligned, pwlq_attend_workspace_bytes(args) bytes,
- * which go by the sizes in args and read no pointer.  Calls that may run at the
+ * which read nothing that args points to.  Calls that may run at the
  * same time need workspaces of their own.
  */
 typedef struct {

@@ -60,6 +60,24 @@ template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void k
 }
 
 
+// Units of keys up to which an item is a workgroup's whole: cutting the line costs 4 to 6 us, in the join's launch and in laying the line out, so a
+// single item is cut where its units take longer than that; with more items the parts are no shorter than items are, and only the limit on
+// what one long sequence among short ones may cost holds (10 units, or 24 of many rows).  Whole and cut, in us, 8 heads of the cache of 128 channels, bfloat16:
+//   tokens of 1, 8 and 48 sequences   301 rows 9.2, 10.0; 9.4, 11.4; 15.7, 19.6      701 rows 12.4, 10.6; 12.6, 14.1; 25.7, 30.4
+//   64 rows of 1, 8 and 48            264 rows 16.0, 18.5; 16.9, 26.1; 41.4, 41.7    764 rows 23.9, 19.9; 26.1, 32.4; 65.1, 65.1
+// Tokens cost less a unit in 64 channels (7.1, 9.3 for 301 rows of 1) and more in 256 (16.7, 14.0), many rows more with 8-bit caches (19.3, 21.3 and 32.9,
+// 21.9) and in 256 channels, where a launch of several workgroups for each CU is slower than a cut one (768 items of 164 rows 84.8, 70.7).
+int64_t whole_units(int rows, int channels, bool codes, int64_t items)
+{
+    if (rows == 128) {
+        if (channels == 256 && items > 256) return 0;
+        const int64_t most = items < 144 ? 6 + items / 8 : 24;
+        return codes || channels == 256 ? most / 2 : most;
+    }
+    const int64_t most = (items < 384 ? 4 + items / 64 : 10) - (rows == 32);
+    return channels == 64 ? most * 3 / 2 : channels == 256 ? most / 2 : most;
+}
+
 struct Shape { int rows, channels, unit, tiles, each, parts, least; size_t part, stretches, top_sum, sums, bytes; };
 
 Shape shape_of(const pwlq_attend_args &g)
@@ -76,8 +94,11 @@ Shape shape_of(const pwlq_attend_args &g)
     const int64_t tiles = g.batch.starts ? g.batch.T * group / s.rows + g.batch.S : g.batch.S * s.each;
     s.tiles = (int)tiles;
     s.least = s.rows < 128 ? 1 : 4;
-    const int64_t units = (g.batch.table_pages * g.cache.page + s.unit - 1) / s.unit, items = tiles * g.cache.heads;
-    const bool enough = s.rows == 128 && items >= 1024;
+    // what an item may see: the table, or the window of its first row to its last
+    const int64_t table = g.batch.table_pages * g.cache.page, window = g.window + s.rows / group + 1;
+    const bool windowed = g.window > 0 && g.window < table && !g.prefix && window < table;
+    const int64_t units = windowed ? (window + s.unit - 1) / s.unit + 1 : (table + s.unit - 1) / s.unit, items = tiles * g.cache.heads;
+    const bool enough = (s.rows == 128 && items >= 1024) || units <= whole_units(s.rows, s.channels, g.cache.type == PWLQ_I8, items);
     if (tiles <= kMostTiles && g.batch.S <= kMostTiles && items * (units + kSetup + 1) < 1LL << 30 && !enough) {
         const int64_t all = items * ((units > 1 ? units : 1) + kSetup);
         const int64_t parts = (all + s.least - 1) / s.least;
