@@ -2,7 +2,8 @@
 //
 //   angle = position * frequency,  (a, b) -> (a cos - b sin, b cos + a sin) for each pair of channels
 //   code = rne(x * (127/a)),  step = a/127,  a the largest magnitude of a row of a head (8-bit caches)
-// Both are bound by memory: each element is read once and written once, and with few rows by latency.
+// Both are bound by memory: each element is read once and written once, and with few rows by latency.  3795 rows of 32 + 16 heads of 128
+// channels into an 8-bit cache 21.3 us (86 MB, 4.0 TB/s), read back 7.9 (23 MB); a single row 3.3 us, which is a launch.
 //
 // A workgroup takes one row of the call or several.  Their angles come first, one to a thread: binary64, reduced to a fraction
 // of a turn there, since position * frequency has no fraction left in binary32 for far positions.  All heads of a row share them,
@@ -230,6 +231,7 @@ void append(const pwlq_append_args &g, hipStream_t stream)
 
 void read(const pwlq_read_args &g, hipStream_t stream)
 {
+    // few rows one to a workgroup (64 rows 2.9 us, four to one 5.0)
     Read a = {cache_of(g.cache), batch_of(g.batch, g.cache), (char *)g.k.data, (char *)g.v.data,
               g.k.stride, g.k.head_stride, g.v.stride, g.v.head_stride, g.batch.T >= 1024 ? kRows : 1};
     const unsigned grid = (unsigned)((a.b.T + a.rows - 1) / a.rows);

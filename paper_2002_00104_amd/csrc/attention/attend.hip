@@ -13,7 +13,8 @@ extern template PWLQ_INTERNAL void attend_launch<f16, int8_t>(const Attend &, in
 namespace {
 
 // The parts of an item that workgroups left in the workspace: DP / 4 lanes a group, a workgroup for ROWS rows, each of which has a group or several;
-// these take its parts in turn, each in the order of the keys, and the first adds up what they have, in their order.
+// these take its parts in turn, each in the order of the keys, and the first adds up what they have, in their order.  3.5 us (a launch) for a token, 6 for
+// one in 512 parts, 8 for 37 MB of sums of 228 items.
 template <typename T, int DP, int ROWS> __global__ __launch_bounds__(256) void k_attend_join(const Attend a, int rows)
 {
     constexpr int kLanes = DP / 4, kGroups = 256 / kLanes, kEach = kGroups > ROWS ? kGroups / ROWS : 1;
@@ -98,6 +99,7 @@ Shape shape_of(const pwlq_attend_args &g)
     const int64_t table = g.batch.table_pages * g.cache.page, window = g.window + s.rows / group + 1;
     const bool windowed = g.window > 0 && g.window < table && !g.prefix && window < table;
     const int64_t units = windowed ? (window + s.unit - 1) / s.unit + 1 : (table + s.unit - 1) / s.unit, items = tiles * g.cache.heads;
+    // as many items as this fill the chip by themselves (a prompt of 4096 rows, 32 heads over 8: 160 us, cut into parts 190)
     const bool enough = (s.rows == 128 && items >= 1024) || units <= whole_units(s.rows, s.channels, g.cache.type == PWLQ_I8, items);
     if (tiles <= kMostTiles && g.batch.S <= kMostTiles && items * (units + kSetup + 1) < 1LL << 30 && !enough) {
         const int64_t all = items * ((units > 1 ? units : 1) + kSetup);
