@@ -233,3 +233,61 @@ def test_graphs_that_share_a_workspace(A, dtype):  # noqa: F811
             assert torch.equal(again, want[i])
         torch.cuda.synchronize()
         assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+@pytest.mark.parametrize("packed", [False, True], ids=["16 bits", "8 bits"])
+@pytest.mark.parametrize("longest", LONGEST)
+def test_the_longest_sequences(A, longest, packed):  # noqa: F811
+    """2^30 rows on one page: the last ones through a window as where the sequence is short, and all of them with equal weights."""
+    g = gen("longest")
+    page, D, most = 65536, 64, 1 << 30
+    keys, values, key_step, value_step = make_cache(g, ref.Batch(g, [(1, page)], page, spare=0), 1, D, BF16, packed)
+    cache = on_gpu(A, (keys, values, key_step, value_step))
+    q = normal(g, 9, 4, D, dtype=BF16).cuda()
+    starts = torch.tensor([0, 4, 9], dtype=torch.int32).cuda()
+    table = torch.zeros(2, most // page, dtype=torch.int32).cuda()
+    none = torch.zeros(2, dtype=torch.int32).cuda()
+    long, short = (torch.tensor([n, n - 70000], dtype=torch.int32).cuda() for n in (most, 4 * page))
+    for window in (1, 700):
+        for prefix in (None, none):                         # with one the window says nothing about how much is seen
+            a = A.attend(q, cache, table, long, starts=starts, longest=longest, window=window, prefix=prefix)
+            b = A.attend(q, cache, table[:, :4].contiguous(), short, starts=starts, longest=longest, window=window, prefix=prefix)
+            # sums in another order: a rounding of the output and of each weight, and n roundings of each of two sums
+            assert ((a.double() - b.double()).abs() <= (4 * 2.0 ** -8 + 2 * window * 2.0 ** -24) * values_of(values, value_step).abs().max()).all()
+    got = A.attend(torch.zeros_like(q[:1]), cache, table[:1], long[:1], starts=starts[:2].clamp(max=1), longest=longest)
+    mean = values_of(values, value_step).mean(0)
+    # at most 2^30 / 512 keys are summed one after the other, and the weight times a step is rounded once
+    slack = mean.abs() * 2.0 ** -8 + (2.0 ** -8 + 2.0 ** 21 * 2.0 ** -24) * values_of(values, value_step).abs().mean(0)
+    assert ((got.double().cpu() - mean).abs() <= slack).all()
+
+
+def values_of(values, step):
+    """[rows, D] in binary64 of a page of one head."""
+    v = values[0, 0].double()
+    return v if step is None else v * step[0, 0].double()[:, None]
+
+
+@pytest.mark.parametrize("packed", [False, True], ids=["16 bits", "8 bits"])
+def test_the_most_rows(A, packed):  # noqa: F811
+    """2^20 rows of a call: a sequence's, of which each sees itself only, and of as many sequences of one row."""
+    most, D = 1 << 20, 16
+    g = torch.Generator("cuda").manual_seed(7)
+    k, v, q = (torch.randn(most, n, D, generator=g, device="cuda").to(BF16) for n in (1, 1, 2))
+    for S, page in ((1, 4096), (most, 16)):
+        pages = most // page if S == 1 else 1024
+        cache = A.make_cache(pages, 1, page, D, I8 if packed else BF16)
+        n = most // S
+        starts = (torch.arange(S + 1, dtype=torch.int32) * n).cuda()
+        lengths = torch.full((S,), n, dtype=torch.int32).cuda()
+        if S == 1:
+            table = torch.randperm(pages, generator=g, device="cuda").int()[None].contiguous()
+            assert torch.equal(A.append(cache, table, lengths, k, v, q, starts=starts), q)
+        else:                                               # pages are shared, so they are written through a table of their own
+            table = (torch.arange(S, device="cuda") % pages).int()[:, None].contiguous()
+            A.append(cache, table[:pages].contiguous(), lengths[:pages], k[:pages].contiguous(), v[:pages].contiguous())
+        own = A.read(cache, table, lengths, starts=starts, rows=most, dtype=BF16)[1].expand(most, 2, D)
+        for longest in (n, 1):
+            got = A.attend(q, cache, table, lengths, starts=starts, longest=longest, window=1)
+            # one weight of 1 times the row's step, or a value times its step: rounded, and the output too
+            assert ((got.double() - own.double()).abs() <= 2.0 ** -7 * own.double().abs() + 1e-30).all()
+    assert torch.equal(A.attend(q, cache, table, lengths), A.attend(q, cache, table, lengths, starts=starts, longest=1))
