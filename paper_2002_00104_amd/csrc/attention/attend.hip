@@ -99,8 +99,11 @@ Shape shape_of(const pwlq_attend_args &g)
     const int64_t table = g.batch.table_pages * g.cache.page, window = g.window + s.rows / group + 1;
     const bool windowed = g.window > 0 && g.window < table && !g.prefix && window < table;
     const int64_t units = windowed ? (window + s.unit - 1) / s.unit + 1 : (table + s.unit - 1) / s.unit, items = tiles * g.cache.heads;
-    // as many items as this fill the chip by themselves (a prompt of 4096 rows, 32 heads over 8: 160 us, cut into parts 190)
-    const bool enough = (s.rows == 128 && items >= 1024) || units <= whole_units(s.rows, s.channels, g.cache.type == PWLQ_I8, items);
+    // Tiles of one sequence run beside each other and share its keys in the L2s as whole items, and as parts they are anywhere: where there are
+    // many, and items enough to fill the chip, they stay whole (32 heads over 8 of 128 channels, whole and cut: a prompt of 2048 rows 59 and 74 us, 1024
+    // items of 4096 156 and 184, after 4000 in 8 bits 511 and 565; of 256 channels 133 and 243).  Where they are few, parts are the better balance
+    // (100 sequences of 1128, the last 128 of one head, in 8 bits 233 and 143, in 16 167 both; 12 of 5160, the last 160 of 4 heads, in 8 bits 371 and 251).
+    const bool enough = (s.rows == 128 && items >= (rows >= 8 * 128 ? 512 : 4096)) || units <= whole_units(s.rows, s.channels, g.cache.type == PWLQ_I8, items);
     if (tiles <= kMostTiles && g.batch.S <= kMostTiles && items * (units + kSetup + 1) < 1LL << 30 && !enough) {
         const int64_t all = items * ((units > 1 ? units : 1) + kSetup);
         const int64_t parts = (all + s.least - 1) / s.least;
