@@ -80,11 +80,10 @@ template <typename T, typename C, int DP, int DC> struct Many {
             }
         }
         if constexpr (kCodes) {
-            if (wave < 2 && lane < kKeys) {
-                const int of = block + lane / 16;
-                const int64_t n = (int64_t)((uint64_t)(uint32_t)__shfl((int)rows, of) | (uint64_t)(uint32_t)__shfl((int)(rows >> 32), of) << 32);
-                step = (wave ? a.c.value_step : a.c.key_step)[n + (lane & 15)];
-            }
+            // by all lanes: the blocks' rows may be in lanes that have no step to fetch, and a lane that is off gives 0
+            const int of = (block + lane / 16) & 63;
+            const int64_t n = (int64_t)((uint64_t)(uint32_t)__shfl((int)rows, of) | (uint64_t)(uint32_t)__shfl((int)(rows >> 32), of) << 32);
+            if (wave < 2 && lane < kKeys) step = (wave ? a.c.value_step : a.c.key_step)[n + (lane & 15)];
         }
     }
     // Sixteen bytes for each lane, to LDS from `to` on in the order of the lanes.  Written out, since the compiler takes what comes to LDS this way to
