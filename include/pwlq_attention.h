@@ -110,6 +110,7 @@ int pwlq_read(const pwlq_read_args *args, void *stream);
  * or, where `tree` is given, slots before its sequence's rows of this call, and
  * row j' of those rows if bit j' % 64 of tree[t * tree_words + j' / 64] is set
  * (j' >= 64 * tree_words: not).  A tree goes without slopes, window and prefix.
+ * Scores are formed in binary32: one beyond its range is infinite, and the softmax of a row that sees plus infinity is NaN.
  * What a row does not see does not touch it, infinities and NaN included.  A row
  * that sees nothing (or only scores of minus infinity) is zeros.
  * longest: the most rows of a sequence, as far as the caller knows (0: T); it

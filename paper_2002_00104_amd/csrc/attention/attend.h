@@ -49,6 +49,8 @@ constexpr int kMostTiles = 2047;         // of a call that is split
 constexpr float kLog2e = 1.4426950408889634f;
 // The reference is moved when a score passes it by more than this, so that most tiles move no sums.  exp2(8) keeps within binary16.
 constexpr float kSlack = 8.0f;
+// Below this a reference is off by 2^-15 at most, half a unit in its last place: the weight of the score that it is of rounds to 1.
+constexpr float kFar = 1024.0f;
 
 // n / group for 0 <= n < 2^30: what per_group is too large by adds less than n / 2^40 <= 1 / group.  A division takes 25 instructions, and those that
 // run once before the first key are fetched once each, which is what they cost.

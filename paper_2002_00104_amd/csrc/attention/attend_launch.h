@@ -8,6 +8,8 @@ namespace pwlq_attention {
 
 template <typename T, typename C> void attend_launch(const Attend &a, int D, int rows, unsigned grid, hipStream_t stream)
 {
+    // plain scores have the scale as a factor of products that may be masked by then: it must leave a normal number
+    const bool tiny = fabsf(a.scale) < 0x1p-100f;
     // tiles of 128 rows multiply three quarters of the channels where the others are none
 #define PWLQ_ATTEND_AS(DP, SCORES)                                                                                             \
     do {                                                                                                                       \
@@ -20,7 +22,7 @@ template <typename T, typename C> void attend_launch(const Attend &a, int D, int
 #define PWLQ_ATTEND(DP)                                       \
     do {                                                      \
         if (a.cap > 0.0f) PWLQ_ATTEND_AS(DP, kCapped);        \
-        else if (a.slopes) PWLQ_ATTEND_AS(DP, kSloped);       \
+        else if (a.slopes || tiny) PWLQ_ATTEND_AS(DP, kSloped); \
         else PWLQ_ATTEND_AS(DP, kPlain);                      \
     } while (0)
     if (D == 64) PWLQ_ATTEND(64);

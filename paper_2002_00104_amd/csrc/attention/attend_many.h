@@ -156,8 +156,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const float to_cap = SCORES == kCapped ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
     // Plain scores stay as the product has them until the exponential, whose addition takes the factor too.  Where the scale is negative the
-    // queries change their sign; 0 times what is masked would be NaN, so the factor is next to 0 where the scale is 0.
-    const float factor = SCORES == kPlain ? fmaxf(fabsf(to_cap), 1.2e-38f) : 1.0f;
+    // queries change their sign; it is not 0 here, which times what is masked would be NaN.
+    const float factor = SCORES == kPlain ? fabsf(to_cap) : 1.0f;
 
     Segments<F::kRows, F::kKeys, 256> segments(a, (uint32_t *)room, tiles);
     if (a.c.D != DP) {
@@ -209,6 +209,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
 #pragma unroll
         for (int c = 0; c < F::kColumns; ++c) acc[c] = v16f{};
         float top = -INFINITY, reference = 0.0f, sum = 0.0f;
+        bool far = false;                                  // some row's reference is beyond kFar
 
         const int last = min(t.first + F::kRows, t.rows) - 1;
         // this wavefront's rows, and the slots that any of them may see
@@ -331,13 +332,25 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
                     for (int i = 0; i < 16; ++i) acc[c][i] *= old;
                 top = most;
                 reference = next;
+                if constexpr (SCORES == kPlain) far = __ballot(fabsf(reference) >= kFar) != 0;
+            }
+            // The reference is a rounded product, and what that is off by is in all of a row's weights, as a factor.  Far out it would be any
+            // number, so there the others are rounded products too.
+            float by = factor, less = reference;
+            if (SCORES == kPlain && far) {
+#pragma unroll
+                for (int b = 0; b < F::kBlocks; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[b][i] = s[b][i] * factor - reference;
+                by = 1.0f;
+                less = 0.0f;
             }
             v8 weight[F::kBlocks][2];
 #pragma unroll
             for (int b = 0; b < F::kBlocks; ++b) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], factor, -reference));
+                    s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], by, -less));
                     sum += s[b][i];
                 }
                 if constexpr (F::kCodes && !F::kScaled) {
