@@ -84,7 +84,8 @@ struct Shape { int rows, channels, unit, tiles, each, parts, least; size_t part,
 Shape shape_of(const pwlq_attend_args &g)
 {
     Shape s = {};
-    const int64_t group = g.q_heads / g.cache.heads, longest = !g.batch.starts ? 1 : g.longest ? g.longest : g.batch.T;
+    // longest and window may be any numbers: no more is made of them than there are rows and slots
+    const int64_t group = g.q_heads / g.cache.heads, longest = !g.batch.starts ? 1 : g.longest && g.longest < g.batch.T ? g.longest : g.batch.T;
     s.channels = g.cache.D <= 64 ? 64 : g.cache.D <= 128 ? 128 : 256;
     // A tile for all rows of a sequence, so that its keys are read once.  16 sequences of 4000 rows, trees of 20 rows, in tiles of 16, 32 and 128:
     // 93, 62 and 64 us, 57, 53 and 67 with an 8-bit cache; of 48 rows 130, 67 and 69, 77, 76 and 73.
@@ -96,7 +97,7 @@ Shape shape_of(const pwlq_attend_args &g)
     s.tiles = (int)tiles;
     s.least = s.rows < 128 ? 1 : 4;
     // what an item may see: the table, or the window of its first row to its last
-    const int64_t table = g.batch.table_pages * g.cache.page, window = g.window + s.rows / group + 1;
+    const int64_t table = g.batch.table_pages * g.cache.page, window = (g.window < table ? g.window : table) + s.rows / group + 1;
     const bool windowed = g.window > 0 && g.window < table && !g.prefix && window < table;
     const int64_t units = windowed ? (window + s.unit - 1) / s.unit + 1 : (table + s.unit - 1) / s.unit, items = tiles * g.cache.heads;
     // Tiles of one sequence run beside each other and share its keys in the L2s as whole items, and as parts they are anywhere: where there are
