@@ -41,16 +41,24 @@ struct Attend {
     int alone;                           // and where that leaves no more parts than CUs: a second workgroup there pays for longer ones
     int *part;                           // workspace: units of a part,
     struct Stretch *stretches;           // of the tiles on the line,
-    float2 *top_sum;                     // m and the sum of each row of two sums for each part,
+    float2 *top_sum;                     // m (-infinity: none) and the sum of each row of two sums for each part,
     float *sums;                         // and their values
 };
 
 constexpr int kMostTiles = 2047;         // of a call that is split
 constexpr float kLog2e = 1.4426950408889634f;
-// The reference is moved when a score passes it by more than this, so that most tiles move no sums.  exp2(8) keeps within binary16.
+// The reference is moved when a score passes it by more than this, so that most tiles move no sums.
 constexpr float kSlack = 8.0f;
 // Below this a reference is off by 2^-15 at most, half a unit in its last place: the weight of the score that it is of rounds to 1.
 constexpr float kFar = 1024.0f;
+// The reference for a largest score of `top`.  Weights of binary16 are multiples of 2^-24: many that are less, beside one of 1, would be nothing in the
+// product and something in their sum (2^20 of 2^-25: 3 % of the output).  So the largest there is 2^7, with the slack 2^15, and 2^-25 of that is lost.
+// Far out, where taking off 7 is a rounding, it is 1.
+template <typename T> __device__ inline float reference_of(float top)
+{
+    if (top == -INFINITY) return 0.0f;
+    return __is_same(T, f16) && fabsf(top) < kFar ? top - 7.0f : top;
+}
 
 // n / group for 0 <= n < 2^30: what per_group is too large by adds less than n / 2^40 <= 1 / group.  A division takes 25 instructions, and those that
 // run once before the first key are fetched once each, which is what they cost.

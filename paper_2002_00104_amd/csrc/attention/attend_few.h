@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256, DP * RB > 128 ? 1 : 2) void k_attend_few(const
                 if (__ballot(most > top[r] + kSlack)) {
                     most = fmaxf(most, __shfl_xor(most, 16));
                     most = fmaxf(top[r], fmaxf(most, __shfl_xor(most, 32)));
-                    const float next = most == -INFINITY ? 0.0f : most;
+                    const float next = reference_of<T>(most);
                     const float old = top[r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(reference[r] - next);
                     // a sum that is NaN already stays NaN
                     sum[r] *= top[r] == -INFINITY ? 1.0f : old;
@@ -239,12 +239,14 @@ __global__ __launch_bounds__(256, DP * RB > 128 ? 1 : 2) void k_attend_few(const
                     top[r] = most;
                     reference[r] = next;
                 }
-                float w[8];
+                // a unit's weights are summed by themselves: one by one they might be nothing beside what there is
+                float w[8], more = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     w[i] = __builtin_amdgcn_exp2f(x[i] - reference[r]);
-                    sum[r] += w[i];
+                    more += w[i];
                 }
+                sum[r] += more;
                 if constexpr (F::kCodes && !__is_same(T, f16)) {
                     // a row's step joins its weight: one rounding to bfloat16, of their product; a step may be NaN
 #pragma unroll
@@ -272,9 +274,10 @@ __global__ __launch_bounds__(256, DP * RB > 128 ? 1 : 2) void k_attend_few(const
             __builtin_amdgcn_wave_barrier();
         }
 
-        // the four wavefronts' sums
+        // the four wavefronts' sums, each with its reference from here on
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
+            if (top[r] != -INFINITY) top[r] = reference[r];
             sum[r] += __shfl_xor(sum[r], 16);
             sum[r] += __shfl_xor(sum[r], 32);
             if (lane < 16) top_sum[wave][16 * r + lane] = make_float2(top[r], sum[r]);

@@ -322,7 +322,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
             most *= factor;
             if (__ballot(most > top + kSlack)) {
                 most = fmaxf(top, fmaxf(most, __shfl_xor(most, 32)));
-                const float next = most == -INFINITY ? 0.0f : most;
+                const float next = reference_of<T>(most);
                 // a sum that is NaN already stays NaN
                 const float old = top == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(reference - next);
                 sum *= old;
@@ -345,13 +345,15 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
                 by = 1.0f;
                 less = 0.0f;
             }
+            // a unit's weights are summed by themselves: one by one they might be nothing beside what there is
+            float more = 0.0f;
             v8 weight[F::kBlocks][2];
 #pragma unroll
             for (int b = 0; b < F::kBlocks; ++b) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], by, -less));
-                    sum += s[b][i];
+                    more += s[b][i];
                 }
                 if constexpr (F::kCodes && !F::kScaled) {
                     // a row's step joins its weight: one rounding to bfloat16, of their product; a step may be NaN
@@ -375,6 +377,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
                     weight[b][e] = __builtin_convertvector(w, v8);
                 }
             }
+            sum += more;
 #pragma unroll
             for (int step = 0; step < 2 * F::kBlocks; ++step)
 #pragma unroll
@@ -431,7 +434,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
         if (row < t.rows) {
             const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
             const int64_t at = (int64_t)sums * F::kRows + 32 * wave + (lane & 31);
-            if (sums >= 0 && half == 0) a.top_sum[at] = make_float2(top, sum);
+            if (sums >= 0 && half == 0) a.top_sum[at] = make_float2(top == -INFINITY ? top : reference, sum);
 #pragma unroll
             for (int c = 0; c < F::kColumns; ++c)
 #pragma unroll
