@@ -217,11 +217,13 @@ template <int M, int UNIT> __device__ Part plan_few(const Attend &a, Tile *tiles
     return p;
 }
 
-// The line of more, by the workgroup, in LDS (`room`: 4 (2 S + 8) bytes with starts and 4 (tiles + 8) at least; free again after the
-// caller's next barrier).
+// The line of more, by the workgroup, in LDS (`room`: kPlanBytes, aligned to a word; free again on return): a word for each wavefront, where each tile
+// begins and the line's end, and the starts.
+constexpr int kPlanWaves = 8, kPlanBytes = 4 * (kPlanWaves + 2 * (kMostTiles + 1));
 template <int M, int UNIT, int THREADS> __device__ Part plan(const Attend &a, uint32_t *room)
 {
-    uint32_t *const slots = room, *const begin = room + 8;
+    static_assert(THREADS <= 64 * kPlanWaves, "LDS");
+    uint32_t *const slots = room, *const begin = room + kPlanWaves;
     int32_t *const starts = (int32_t *)(begin + kMostTiles + 1);
     const int each = (a.tiles + THREADS - 1) / THREADS, from = min((int)threadIdx.x * each, a.tiles), to = min(from + each, a.tiles);
     if (a.b.starts) {

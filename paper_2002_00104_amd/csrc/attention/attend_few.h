@@ -25,7 +25,7 @@ template <typename T, typename C, int DP, int RB> struct Few {
     static constexpr int kStride = 2 * DP + 64;                                    // bytes of a row of values in LDS: four rows, all banks
     static constexpr int kSumStride = DP + 4;                                      // floats of a row of sums in LDS
     static constexpr int kRoom = 4 * 32 * kStride;
-    static_assert(kRoom >= 4 * 16 * kSumStride * 4 && kRoom >= 4 * (2 * kMostTiles + 16), "LDS");
+    static_assert(kRoom >= 4 * 16 * kSumStride * 4 && kRoom >= kPlanBytes, "LDS");
     typedef typename Vec8<T>::type v8;
 
     v4u k[2][kLoads], v[kValueLoads];

@@ -27,7 +27,7 @@ template <typename T, typename C, int DP, int DC> struct Many {
     // In LDS, a stage: keys, then values.  16-bit elements have two; codes one, and then codes of keys and of values as they come.
     static constexpr int kRowBytes = 2 * DP, kPart = kKeys * kRowBytes, kStage = 2 * kPart, kCodePart = kKeys * DP;
     static constexpr int kRoom = kCodes ? kStage + 2 * kCodePart : 2 * kStage;
-    static_assert(kRoom >= 4 * (2 * kMostTiles + 16), "LDS");
+    static_assert(kRoom >= kPlanBytes, "LDS");
     typedef typename Vec8<T>::type v8;
 
     // A row's chunks of 16 bytes in LDS are in an order of its own, so that the rows that are read together lie in different banks: for keys
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_many(const At
     typedef Many<T, C, DP, DC> F;
     typedef typename F::v8 v8;
     __shared__ __attribute__((aligned(16))) char room[F::kRoom];
-    __shared__ float steps[2][F::kCodes ? 2 * F::kKeys : 4];   // of the unit that is worked on, and of the next
+    __shared__ __attribute__((aligned(16))) float steps[2][F::kCodes ? 2 * F::kKeys : 4];   // read four at a time; of the unit that is worked on, and of the next
     __shared__ int bad;                                    // a value taken out
     __shared__ Tile tiles[kFewTiles];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
