@@ -87,15 +87,16 @@ template <typename T, typename C, int DP, int DC> struct Many {
         }
     }
     // Sixteen bytes for each lane, to LDS from `to` on in the order of the lanes.  Written out, since the compiler takes what comes to LDS this way to
-    // come to all of it and would wait before every read of the other buffer; the wait is in arrive().  No register is written but m0, which the
-    // compiler allots to nothing and sets itself before each use of its own (here it has none).
+    // come to all of it and would wait before every read of the other buffer; the wait is in arrive().  It writes no register; m0, which says where to, is
+    // an operand.  Five wait states come before it, which the compiler does not count here: a scalar register that a vector instruction has written
+    // (readlane, of a scalar that was spilled too) may be read as an address then.
     static __device__ void to_lds(const char *from, uint32_t offset, uint32_t to)
     {
         // the same in all lanes, said so for what is compiled with less analysis
         const uint32_t place = __builtin_amdgcn_readfirstlane((int)to);
         const uint64_t address = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint64_t)from) |
                                  (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)from >> 32)) << 32;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(place), "v"(offset), "s"(address) : "memory");
+        asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(place), "v"(offset), "s"(address) : "memory");
     }
     // The steps that load() fetched: keys' times what makes scores of products.
     __device__ void put_steps(float *steps, float to_score, int wave, int lane) const
