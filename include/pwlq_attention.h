@@ -112,7 +112,13 @@ int pwlq_read(const pwlq_read_args *args, void *stream);
  * (j' >= 64 * tree_words: not).  A tree goes without slopes, window and prefix.
  * Scores are formed in binary32: one beyond its range is infinite, and the softmax of a row that sees plus infinity is NaN.
  * What a row does not see does not touch it, infinities and NaN included.  A row
- * that sees nothing (or only scores of minus infinity) is zeros.
+ * that sees nothing (or only scores of minus infinity) is zeros.  An infinite
+ * value that it sees makes its output infinite, or NaN where the weight is next
+ * to nothing.
+ * Roundings: a weight is rounded to the elements' type for its product with the
+ * values (with PWLQ_I8 and bfloat16 together with the value's step; with
+ * binary16 the value is, which must be within its range), the output once.
+ * With a prefix a window saves no time: keys between the two are gone through.
  * longest: the most rows of a sequence, as far as the caller knows (0: T); it
  * decides which kernel runs and nothing else.
  * Workspace: device, 256-byte aligned, pwlq_attend_workspace_bytes(args) bytes,

@@ -1,9 +1,10 @@
 // k_attend_many: tiles of 128 query rows, for prompts and larger trees.
 //
-// Bound by the matrix cores and by the exponentials beside them: a tile of 64 keys takes a wavefront's 32 rows 1024 cycles of matrix
-// instructions (128 channels) and nearly as many of vector instructions for its 2048 weights.  Two workgroups share a CU, so that one's
-// products run beside the other's exponentials.  A prompt of 4096 rows, 32 heads over 8: 160 us, 860 TFLOP/s, the matrix cores busy in 65 % of
-// the cycles at the 1.84 GHz that this load leaves.  1024 rows after 7169 in 8 bits, capped: 234 us, 560 TFLOP/s: codes and caps are vector instructions.
+// Bound by the matrix cores and by the exponentials beside them, one after the other: a tile of 64 keys takes a wavefront's 32 rows 1024 cycles of matrix
+// instructions (128 channels) and nearly as many of vector instructions for its 2048 weights.  Two workgroups share a CU, but one's products run
+// beside the other's exponentials by chance only: a prompt of 4096 rows, 32 heads over 8, takes 160 us, 860 TFLOP/s, with the matrix cores
+// busy in 47 % of the cycles and vector instructions issued in as many others.  1024 rows after 7169 in 8 bits, capped: 237 us with the join, 553 TFLOP/s, 25 and
+// 60 %: codes and caps are vector instructions.
 //
 // Keys and values of a tile are staged in LDS, twice: one is filled while the other is worked on, a barrier a tile; 16-bit elements
 // go there from memory directly, codes too, and are widened there between two barriers.  As for few

@@ -61,3 +61,29 @@ def test_long_parts(A, D, dtype):  # noqa: F811
     for kw in ({}, dict(tree=torch.tensor([[1], [3]] * n))):
         print(f"[case] parts D={D} {dtype} {sorted(kw)}", flush=True)
         run_attend(A, q, batch, cache, name=str(sorted(kw)), longest=1024, **kw)
+
+
+@pytest.mark.parametrize("dtype,packed", [(BF16, False), (F16, False), (BF16, True), (F16, True)], ids=["bf16", "f16", "bf16 codes", "f16 codes"])
+@pytest.mark.parametrize("longest", [1, 8, 1024])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_not_finite_far_from_the_start(A, D, longest, dtype, packed):  # noqa: F811
+    """Infinities and NaN among values thousands of keys into an item, seen by some of its rows, by all, and by none; whole and cut."""
+    g = gen("far from the start", D)
+    for empty in (0, 2100):
+        batch = without_page_0(ref.Batch(g, [(3, 4200), (40, 2531), (1, 1100)] + [(0, 0)] * empty, 16))
+        if packed:
+            cache = packed_cache(g, batch, 2, D)
+        else:
+            shape = (batch.pages, 2, 16, D)
+            cache = (normal(g, *shape, dtype=dtype), normal(g, *shape, dtype=dtype), None, None)
+        for s, slot, what in ((0, 4198, math.inf), (0, 3600, math.nan), (0, 100, math.inf), (1, 2510, -math.inf), (1, 2500, math.inf), (1, 2100, math.nan),
+                              (2, 400, math.nan)):
+            page, row = batch.where(s, slot, batch.pages)
+            if packed:
+                cache[1][page, 0, row], cache[3][page, 0, row] = 0, math.nan
+            else:
+                cache[1][page, 0, row, D - 3] = what
+        q = normal(g, batch.rows, 4, D, dtype=dtype, scale=0.3)
+        for window in (0, 420, 699):
+            print(f"[case] far from the start {D} {longest} {dtype} {packed} {empty} {window}", flush=True)
+            run_attend(A, q, batch, cache, name=f"window {window}", longest=longest, window=window)
